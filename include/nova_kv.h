@@ -21,6 +21,17 @@
  *                        token, then attend), in a single launch where the
  *                        shape allows.
  *
+ * Beside them stand the calls in front of that cache and those of layers kept
+ * at a higher rate:
+ *
+ *   nova_kv_rotate_qkv   norms of queries and keys for each head and the position
+ *                        rotation, from a projection's rows to the dense tensors
+ *                        that the calls above take.
+ *   nova_kv_q4_append    the same in front of a cache held in 4 bits: keys and
+ *                        values are quantized and stored on the way.
+ *   nova_kv_q4_attn      attention of one or more query tokens per sequence over
+ *                        that 4-bit cache.
+ *
  * Conventions for every call
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library
  *     never allocates, frees or synchronizes inside these calls.  All work is
@@ -365,6 +376,185 @@ nova_kv_status nova_kv_append_decode_attn_noalloc(const nova_kv_params *p, const
                                                   float *out, void *hip_stream);
 
 /*
+ * Rows of heads in the caller's memory: head h of token i of sequence b starts at
+ *
+ *   data + (b * batch_stride + i * token_stride + h * D) * (bytes of an element)
+ *
+ * with non-negative strides in elements, so q, k and v may be slices of one
+ * fused projection.  data needs an element's alignment only (rows whose
+ * base and strides are multiples of 16 bytes are read in vectors).
+ */
+typedef struct {
+    const void *data;
+    int64_t batch_stride;
+    int64_t token_stride;
+} nova_kv_rows;
+
+/*
+ * What a layer does to its heads between the projection and the cache: an
+ * optional RMS norm of every query and key head and an optional rotation of
+ * its first rotary_dim coordinates by the token's position.
+ *
+ *   norm       y_i = x_i * w_i / sqrt(mean_j x_j^2 + eps); q_norm and k_norm are
+ *              fp32 weights [D] ([Hq][D] or [Hkv][D] when *_norm_per_head is 1),
+ *              NULL = no norm on that side
+ *   rotation   with (c, s) = (cos_sin[p][j], cos_sin[p][rotary_dim / 2 + j]) for
+ *              position p and j < rotary_dim / 2:
+ *                y_a, y_b = y_a * c - y_b * s, y_b * c + y_a * s
+ *              for the pair (a, b) = (j, j + rotary_dim / 2), or (2j, 2j + 1)
+ *              when interleaved is 1.  cos_sin is fp32 [num_positions]
+ *              [rotary_dim]; rotary_dim is 0 (no rotation, cos_sin unused) or a
+ *              multiple of 8 up to D.
+ *
+ * D in {64, 128}.  cos_sin and the weights must be 16-byte aligned.
+ */
+typedef struct {
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t rotary_dim;
+    int32_t interleaved;
+    int32_t num_positions;
+    const float *cos_sin;
+    const float *q_norm;
+    const float *k_norm;
+    int32_t q_norm_per_head;
+    int32_t k_norm_per_head;
+    float eps;
+} nova_kv_rotary;
+
+/*
+ * nova_kv_rotate_qkv -- the queries, keys and values of n_new tokens per
+ * sequence as nova_kv_encode, nova_kv_decode_attn and the step take them:
+ * dense, queries and keys normed and rotated, in one launch.
+ *
+ *   q, k, v    rows of Hq, Hkv, Hkv heads, dtype `dtype` (F32 or BF16); any of
+ *              them may be NULL (with its output) and is then left out
+ *   new_lens   [B] int32 device, or NULL = n_new for every sequence: tokens
+ *              i >= new_lens[b] are padding, neither read nor written
+ *   start_pos  [B] int32 device: position of the first new token of each
+ *              sequence (may be NULL when rotary_dim is 0).  A token whose
+ *              position falls outside [0, num_positions) is left out like padding.
+ *   q_out, k_out, v_out  [B][n_new][Hq or Hkv][D] device, the same dtype, dense,
+ *              16-byte aligned.  An output may be its own input, where that is
+ *              dense too; it must not overlap the others.
+ *
+ * Norm and rotation are evaluated in fp32 and rounded once; values are copied.
+ * batch == 0 or n_new == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
+                                  const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                                  const int32_t *new_lens, const int32_t *start_pos, void *q_out, void *k_out,
+                                  void *v_out, void *hip_stream);
+
+/*
+ * A cache held in 4 bits, for layers that need more than 2 bits per element
+ * (4.25 at D = 128): every key and value of a token and KV head is a row of D
+ * 4-bit codes c_i and stands for offset + scale * c_i.
+ *
+ *   k_codes, v_codes  uint8 [num_blocks][Hkv][block_size][D / 2]: coordinate 2j in
+ *              the low and 2j + 1 in the high half of byte j; 16-byte aligned
+ *   k_sq, v_sq uint16 bf16 bit patterns [num_blocks][Hkv][block_size][2] (scale,
+ *              offset), 4-byte aligned
+ *   layout     as for the code pools: token t of sequence b in row
+ *              t % block_size of a physical block.  A block-table entry outside
+ *              [0, num_blocks) holds nothing: its tokens are not stored, and not
+ *              attended.
+ *
+ * A row x is stored with offset = bf16(min_i x_i), scale = bf16((max_i x_i - min_i x_i) / 15)
+ * (each rounded to fp32, then to bf16, to nearest even) and
+ * c_i = clamp(round_half_even((x_i - offset) / scale), 0, 15), or 0 when the stored
+ * scale is 0; evaluated in fp64.  A row that holds an infinity or a NaN, or
+ * whose scale or offset bf16 cannot hold, is stored as NaN scale and offset and
+ * codes of 0, so what attends it is NaN.
+ *
+ * At most 2^32 - 1 rows (num_blocks * Hkv * block_size) per pool.
+ */
+typedef struct {
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t num_blocks;
+    nova_kv_layout layout;
+    uint8_t *k_codes;
+    uint8_t *v_codes;
+    uint16_t *k_sq;
+    uint16_t *v_sq;
+} nova_kv_q4_cache;
+
+/*
+ * nova_kv_q4_append -- append n_new tokens per sequence to a 4-bit cache,
+ * keys normed and rotated on the way, and their queries too.
+ *
+ *   r          the layer's norms and rotation (heads and D as the cache's)
+ *   q          rows of Hq heads, or NULL (with q_out)
+ *   k, v       rows of Hkv heads
+ *   new_lens, start_pos, dtype  as in nova_kv_rotate_qkv; start_pos is required.
+ *              A token whose position falls outside [0, block_size * blocks_per_seq),
+ *              outside [0, num_positions) when rotary_dim > 0, or in a block that
+ *              holds nothing is left out like padding (nothing of it is written).
+ *              No two tokens of a call may go to the same row.
+ *   q_out      [B][n_new][Hq][D] device, dtype `dtype`, dense, 16-byte aligned:
+ *              the queries, normed and rotated in fp32 (may be q itself, where
+ *              that is dense)
+ *   k_held, v_held  NULL, or [B][n_new][Hkv][D] device, as q_out: the values that
+ *              the cache now stands for, fp32(scale * c) + offset, rounded to
+ *              dtype -- for a prompt's attention by other means over exactly what
+ *              later steps will read
+ *
+ * Keys are normed, rotated and quantized in fp64 (values: quantized), so the
+ * stored codes do not depend on the call's shape.
+ * batch == 0 or n_new == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache *cache, const nova_kv_rows *q,
+                                 const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch,
+                                 int32_t n_new, const int32_t *new_lens, const int32_t *start_pos, void *q_out,
+                                 void *k_held, void *v_held, void *hip_stream);
+
+/*
+ * Bytes of device workspace nova_kv_q4_attn needs for this shape, whatever its
+ * window.  Returns 0 on invalid input.
+ */
+size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t batch, int32_t n_q,
+                                       int32_t num_q_heads, int32_t max_seq_len);
+
+/*
+ * nova_kv_q4_attn -- causal attention of n_q query tokens per sequence (a
+ * step's single token, drafted tokens, a chunk of a prompt) over a 4-bit cache
+ * that holds their keys and values already.
+ *
+ *   q          [B][n_q][Hq][D] device, dtype q_dtype (F32 or BF16), dense, 16-byte
+ *              aligned; query head h reads KV head h / (Hq / Hkv)
+ *   q_lens     [B] int32 device, or NULL = n_q for every sequence: rows
+ *              i >= q_lens[b] are padding, and their outputs are left as they were
+ *   seq_lens   [B] int32 device: cached tokens of each sequence, the queries' own
+ *              included; precondition 0 <= seq_lens[b] <= max_seq_len (a longer one
+ *              is taken as max_seq_len, a negative one as 0).  Query i sits at
+ *              position p = seq_lens[b] - q_lens[b] + i and attends the positions
+ *              j <= p, with window W > 0 only those with j > p - W.
+ *   max_seq_len, window, sinks, softmax_scale  as in nova_kv_decode_attn
+ *   out        [B][n_q][Hq][D] device, dtype q_dtype, 16-byte aligned:
+ *                out = sum_j p_j v_j,  p = softmax({q . k_j * scale} U {sink})
+ *              over the values that the cache stands for.  A row that attends
+ *              nothing is written as zeros.
+ *   workspace  device scratch of at least nova_kv_q4_attn_workspace_bytes(...)
+ *              bytes, 256-byte aligned (may be NULL where that is 0); zero-filled
+ *              before its first use, left ready for the next call by every call
+ *              (replays of a captured call included).  Calls that share a
+ *              workspace must be ordered on one stream.
+ *
+ * Precision: a query is taken as multiples of its row's largest magnitude /
+ * 16256 (F32: / 2080768) and its products with the codes are exact; softmax
+ * statistics and sums over values in fp32; with BF16 queries the
+ * probabilities are rounded to fp16 for those sums, with F32 ones they keep 24
+ * bits.  Results do not depend on which workgroups finish first.
+ * batch == 0 or n_q == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nova_kv_dtype q_dtype, int32_t batch,
+                               int32_t n_q, int32_t num_q_heads, const int32_t *q_lens, const int32_t *seq_lens,
+                               int32_t max_seq_len, int32_t window, const float *sinks, float softmax_scale,
+                               void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * nova_kv_check_metadata -- host-side check of a call's metadata, the
  * preconditions the kernels take on trust.  All pointers are HOST arrays
  * here (layout->block_table included).  Nothing is launched; usable without
@@ -393,9 +583,10 @@ nova_kv_status nova_kv_check_metadata(const nova_kv_layout *layout, int32_t num_
 /*
  * nova_kv_set_debug -- debug mode of the entry points (process-wide; also on
  * from the start when the environment variable NOVA_KV_DEBUG is a nonzero
- * number).  When on, nova_kv_encode, nova_kv_decode_attn and
- * nova_kv_append_decode_attn (and its allocation-free variant) wait for their
- * stream, copy seq_lens / start_pos / the block table to the host and run
+ * number).  When on, nova_kv_encode, nova_kv_decode_attn,
+ * nova_kv_append_decode_attn (and its allocation-free variant),
+ * nova_kv_q4_append and nova_kv_q4_attn wait for their stream, copy seq_lens /
+ * start_pos / new_lens / the block table to the host and run
  * nova_kv_check_metadata (with num_blocks as given here, <= 0: unknown)
  * before launching; a failing check launches nothing.  This synchronizes,
  * so it is for debugging and not for graph capture.

@@ -22,6 +22,8 @@ Contents (each function cites the passage of the paper it follows):
   fp8          fp8 E4M3 snapping of the codebooks
   grouping     Theorem 2 volumes, rate allocation and distortions
   accounting   cache byte and parameter counts
+  q4           norm and rotation of heads, 4-bit rows and causal attention over
+               them (from their formulas; not in the paper)
 
 Parity status: every function is pinned by tests in ``tests/test_oracle_*.py``.
 Lloyd training is pinned by its invariants (monotone distortion, lossless on
@@ -34,4 +36,4 @@ of M_o and the raw-coordinate order all differ.  The pins of these steps are
 also run against planted mistakes, which they must catch.
 """
 
-from . import accounting, attention, calibration, codec, fp8, grouping, vq  # noqa: F401
+from . import accounting, attention, calibration, codec, fp8, grouping, q4, vq  # noqa: F401

@@ -8,4 +8,6 @@ from .api import (NOALLOC_SCRATCH_BYTES, Band, CacheLayout, NovaKVParams, append
                   append_decode_attn_noalloc, band_shape, check_metadata, set_debug,
                   code_pool_shape, decode_attn, decode_workspace_bytes, encode, prepare_append_decode,
                   prepare_decode, prepare_encode, scale_pool_shape)
+from .q4 import (Q4Cache, Rotary, prepare_q4_append, prepare_q4_attn, prepare_rotate_qkv, q4_append,  # noqa: F401
+                 q4_attn, q4_attn_workspace_bytes, q4_code_shape, q4_sq_shape, rotate_qkv)
 from ._native import NovaKVError  # noqa: F401

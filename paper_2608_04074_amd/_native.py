@@ -32,6 +32,10 @@ EXPORTED = (
     "nova_kv_decode_attn",
     "nova_kv_append_decode_attn",
     "nova_kv_append_decode_attn_noalloc",
+    "nova_kv_rotate_qkv",
+    "nova_kv_q4_append",
+    "nova_kv_q4_attn_workspace_bytes",
+    "nova_kv_q4_attn",
     "nova_kv_check_metadata",
     "nova_kv_set_debug",
     "nova_kv_status_string",
@@ -69,6 +73,44 @@ class Band(ctypes.Structure):
         ("n_rec", ctypes.c_int32),
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),
+    ]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("batch_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+    ]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("num_positions", ctypes.c_int32),
+        ("cos_sin", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p),
+        ("k_norm", ctypes.c_void_p),
+        ("q_norm_per_head", ctypes.c_int32),
+        ("k_norm_per_head", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
+class Q4Cache(ctypes.Structure):
+    _fields_ = [
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int32),
+        ("layout", Layout),
+        ("k_codes", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p),
+        ("k_sq", ctypes.c_void_p),
+        ("v_sq", ctypes.c_void_p),
     ]
 
 
@@ -119,6 +161,21 @@ def lib() -> ctypes.CDLL:
         L.nova_kv_append_decode_attn_noalloc.argtypes = [P(Params), P(Layout), vp, vp, ctypes.c_int, vp,
                                                          ctypes.c_int, i32, i32, vp, vp, vp, vp, P(Band), vp,
                                                          i32, i32, vp, ctypes.c_float, vp, vp]
+        L.nova_kv_rotate_qkv.restype = ctypes.c_int
+        # (rotary, q, k, v, dtype, batch, n_new, new_lens, start_pos, q_out, k_out, v_out, stream)
+        L.nova_kv_rotate_qkv.argtypes = [P(Rotary), P(Rows), P(Rows), P(Rows), ctypes.c_int, i32, i32, vp, vp, vp,
+                                         vp, vp, vp]
+        L.nova_kv_q4_append.restype = ctypes.c_int
+        # (rotary, cache, q, k, v, dtype, batch, n_new, new_lens, start_pos, q_out, k_held, v_held, stream)
+        L.nova_kv_q4_append.argtypes = [P(Rotary), P(Q4Cache), P(Rows), P(Rows), P(Rows), ctypes.c_int, i32, i32,
+                                        vp, vp, vp, vp, vp, vp]
+        L.nova_kv_q4_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.nova_kv_q4_attn_workspace_bytes.argtypes = [P(Q4Cache), i32, i32, i32, i32]
+        L.nova_kv_q4_attn.restype = ctypes.c_int
+        # (cache, q, q_dtype, batch, n_q, num_q_heads, q_lens, seq_lens, max_seq_len, window, sinks,
+        #  softmax_scale, out, workspace, bytes, stream)
+        L.nova_kv_q4_attn.argtypes = [P(Q4Cache), vp, ctypes.c_int, i32, i32, i32, vp, vp, i32, i32, vp,
+                                      ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
         L.nova_kv_check_metadata.restype = ctypes.c_int
         # (layout with a host block table, num_blocks, batch, seq_lens, max_seq_len, start_pos, n_new)
         L.nova_kv_check_metadata.argtypes = [P(Layout), i32, i32, vp, i32, vp, i32]

@@ -24,26 +24,30 @@ novakv::CacheLayout to_layout(const nova_kv_layout *lay) {
 
 }  // namespace
 
-namespace {
+namespace novakv {
 
 // ---- debug mode: the metadata copied to the host and checked before a launch
 nova_kv_status debug_check(const nova_kv_layout *lay, int32_t batch, const int32_t *seq_lens, int32_t max_seq_len,
-                           const int32_t *start_pos, int32_t n_new, hipStream_t stream) {
+                           const int32_t *start_pos, int32_t n_new, hipStream_t stream, const int32_t *new_lens,
+                           int32_t num_blocks) {
   if (!debug_enabled() || batch <= 0) return NOVA_KV_OK;
   hipError_t e = hipStreamSynchronize(stream);  // the metadata may be written by earlier work on the stream
   auto to_host = [&](const int32_t *d, size_t n, std::vector<int32_t> &h) {
     h.resize(n);
     if (e == hipSuccess) e = hipMemcpy(h.data(), d, n * sizeof(int32_t), hipMemcpyDeviceToHost);
   };
-  std::vector<int32_t> lens, starts, table;
+  std::vector<int32_t> lens, starts, table, counts;
   if (seq_lens) to_host(seq_lens, batch, lens);
   if (start_pos) to_host(start_pos, batch, starts);
+  if (new_lens) to_host(new_lens, batch, counts);
   if (lay->block_table) to_host(lay->block_table, static_cast<size_t>(batch) * lay->blocks_per_seq, table);
   if (e != hipSuccess) return fail(NOVA_KV_ERR_HIP, "debug mode: metadata copy: %s", hipGetErrorString(e));
   nova_kv_layout hl = *lay;
   hl.block_table = lay->block_table ? table.data() : nullptr;
-  const nova_kv_status st = check_metadata(&hl, debug_num_blocks(), batch, seq_lens ? lens.data() : nullptr,
-                                           max_seq_len, start_pos ? starts.data() : nullptr, n_new);
+  const nova_kv_status st = check_metadata(&hl, num_blocks > 0 ? num_blocks : debug_num_blocks(), batch,
+                                           seq_lens ? lens.data() : nullptr, max_seq_len,
+                                           start_pos ? starts.data() : nullptr, n_new,
+                                           new_lens ? counts.data() : nullptr);
   if (st != NOVA_KV_OK) {
     std::string d = "debug mode: ";
     d += nova_kv_last_error();
@@ -51,6 +55,12 @@ nova_kv_status debug_check(const nova_kv_layout *lay, int32_t batch, const int32
   }
   return NOVA_KV_OK;
 }
+
+}  // namespace novakv
+
+using novakv::debug_check;
+
+namespace {
 
 // ---- the allocation-free step: a fixed scratch array per GPU
 //

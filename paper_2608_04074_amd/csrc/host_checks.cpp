@@ -120,6 +120,102 @@ nova_kv_status check_sq(const nova_kv_params *p, const void *v_sq) {
   return NOVA_KV_OK;
 }
 
+nova_kv_status check_rotary(const nova_kv_rotary *r, bool with_q, bool with_k) {
+  if (!r) return fail(NOVA_KV_ERR_INVALID_ARG, "rotary is NULL");
+  if (r->num_kv_heads <= 0 || r->num_q_heads <= 0 || r->num_q_heads % r->num_kv_heads != 0)
+    return fail(NOVA_KV_ERR_INVALID_ARG, "num_q_heads (%d) must be a positive multiple of num_kv_heads (%d)",
+                r->num_q_heads, r->num_kv_heads);
+  if (r->num_q_heads > (1 << 16)) return fail(NOVA_KV_ERR_UNSUPPORTED, "num_q_heads > 65536");
+  if (r->head_dim != 64 && r->head_dim != 128)
+    return fail(NOVA_KV_ERR_UNSUPPORTED, "head_dim %d unsupported (64 or 128)", r->head_dim);
+  if (r->rotary_dim < 0 || r->rotary_dim > r->head_dim)
+    return fail(NOVA_KV_ERR_INVALID_ARG, "rotary_dim %d outside [0, %d]", r->rotary_dim, r->head_dim);
+  if (r->rotary_dim % 8 != 0)
+    return fail(NOVA_KV_ERR_UNSUPPORTED, "rotary_dim %d unsupported (a multiple of 8)", r->rotary_dim);
+  if (r->interleaved != 0 && r->interleaved != 1)
+    return fail(NOVA_KV_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  if (r->rotary_dim > 0) {
+    if (!r->cos_sin || r->num_positions <= 0)
+      return fail(NOVA_KV_ERR_INVALID_ARG, "cos_sin is NULL or num_positions not > 0");
+    if (!aligned(r->cos_sin, 16)) return fail(NOVA_KV_ERR_INVALID_ARG, "cos_sin must be 16-byte aligned");
+  }
+  if ((with_q && r->q_norm && !aligned(r->q_norm, 16)) || (with_k && r->k_norm && !aligned(r->k_norm, 16)))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "norm weights must be 16-byte aligned");
+  if ((r->q_norm_per_head & ~1) || (r->k_norm_per_head & ~1))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "q_norm_per_head and k_norm_per_head must be 0 or 1");
+  if ((r->q_norm || r->k_norm) && !(r->eps >= 0.f)) return fail(NOVA_KV_ERR_INVALID_ARG, "eps must be >= 0");
+  return NOVA_KV_OK;
+}
+
+nova_kv_status check_rows(const char *name, const nova_kv_rows *rows, const void *out, nova_kv_dtype dtype,
+                          bool need_out) {
+  if (!rows) {
+    if (out) return fail(NOVA_KV_ERR_INVALID_ARG, "an output of %s without its rows", name);
+    return NOVA_KV_OK;
+  }
+  if (!rows->data || (need_out && !out)) return fail(NOVA_KV_ERR_INVALID_ARG, "%s: data or output is NULL", name);
+  if (!aligned(rows->data, dtype == NOVA_KV_BF16 ? 2 : 4))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "%s: data must be aligned to its elements", name);
+  if (out && !aligned(out, 16)) return fail(NOVA_KV_ERR_INVALID_ARG, "%s: the output must be 16-byte aligned", name);
+  if (rows->batch_stride < 0 || rows->token_stride < 0 || rows->batch_stride > (1LL << 40) ||
+      rows->token_stride > (1LL << 40))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "%s: strides outside [0, 2^40]", name);
+  return NOVA_KV_OK;
+}
+
+nova_kv_status check_overlaps(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
+                              const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                              const void *q_out, const void *k_out, const void *v_out) {
+  const char *names[3] = {"q", "k", "v"};
+  const nova_kv_rows *rows[3] = {q, k, v};
+  const void *outs[3] = {q_out, k_out, v_out};
+  // the addresses [lo, hi) of each input and output, in 128 bits (strides reach 2^40 elements)
+  typedef unsigned __int128 wide;
+  wide in_lo[3] = {}, in_hi[3] = {}, out_lo[3] = {}, out_hi[3] = {};
+  bool dense[3] = {};
+  const int elem = dtype == NOVA_KV_BF16 ? 2 : 4;
+  for (int i = 0; i < 3; ++i) {
+    const long long width = static_cast<long long>(i == 0 ? r->num_q_heads : r->num_kv_heads) * r->head_dim;
+    if (rows[i]) {
+      in_lo[i] = reinterpret_cast<uintptr_t>(rows[i]->data);
+      in_hi[i] = in_lo[i] + (static_cast<wide>(batch - 1) * rows[i]->batch_stride +
+                             static_cast<wide>(n_new - 1) * rows[i]->token_stride + width) * elem;
+      dense[i] = (n_new == 1 || rows[i]->token_stride == width) && (batch == 1 || rows[i]->batch_stride == n_new * width);
+    }
+    if (outs[i]) {
+      out_lo[i] = reinterpret_cast<uintptr_t>(outs[i]);
+      out_hi[i] = out_lo[i] + static_cast<wide>(batch) * n_new * width * elem;
+    }
+  }
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 3; ++i) {
+      if (i != o && out_lo[o] < out_hi[i] && out_lo[i] < out_hi[o])
+        return fail(NOVA_KV_ERR_INVALID_ARG, "the outputs of %s and %s overlap", names[o], names[i]);
+      if (out_lo[o] < in_hi[i] && in_lo[i] < out_hi[o] && !(i == o && dense[i] && in_lo[i] == out_lo[o]))
+        return fail(NOVA_KV_ERR_INVALID_ARG, "the output of %s overlaps the rows of %s", names[o], names[i]);
+    }
+  }
+  return NOVA_KV_OK;
+}
+
+nova_kv_status check_q4_cache(const nova_kv_q4_cache *c) {
+  if (!c) return fail(NOVA_KV_ERR_INVALID_ARG, "cache is NULL");
+  if (c->num_kv_heads <= 0) return fail(NOVA_KV_ERR_INVALID_ARG, "num_kv_heads must be > 0");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(NOVA_KV_ERR_UNSUPPORTED, "head_dim %d unsupported (64 or 128)", c->head_dim);
+  const nova_kv_status st = check_layout(&c->layout);
+  if (st != NOVA_KV_OK) return st;
+  if (c->num_blocks <= 0) return fail(NOVA_KV_ERR_INVALID_ARG, "num_blocks must be > 0");
+  const long long rows = static_cast<long long>(c->num_blocks) * c->layout.block_size;  // < 2^61
+  if (rows > 0xffffffffLL / c->num_kv_heads)
+    return fail(NOVA_KV_ERR_UNSUPPORTED, "a pool of more than 2^32 - 1 rows");
+  if (!c->k_codes || !c->v_codes || !c->k_sq || !c->v_sq) return fail(NOVA_KV_ERR_INVALID_ARG, "a cache pool is NULL");
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "code pools must be 16-byte aligned");
+  if (!aligned(c->k_sq, 4) || !aligned(c->v_sq, 4))
+    return fail(NOVA_KV_ERR_INVALID_ARG, "k_sq and v_sq must be 4-byte aligned");
+  return NOVA_KV_OK;
+}
 
 namespace {
 
@@ -131,7 +227,7 @@ long long capacity_of(const nova_kv_layout *lay) {
 
 nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch,
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
-                              int32_t n_new) {
+                              int32_t n_new, const int32_t *new_lens) {
   nova_kv_status st = check_layout(lay);
   if (st != NOVA_KV_OK) return st;
   if (batch < 0 || n_new < 0) return fail(NOVA_KV_ERR_INVALID_ARG, "batch and n_new must be >= 0");
@@ -166,9 +262,10 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
   for (int b = 0; b < batch; ++b) {
     long long w0 = 0, w1 = 0;  // written positions [w0, w1)
     if (start_pos) {
+      const int32_t count = !new_lens ? n_new : new_lens[b] < 0 ? 0 : new_lens[b] < n_new ? new_lens[b] : n_new;
       w0 = start_pos[b];
-      w1 = w0 + n_new;
-      if (n_new > 0 && (w0 < 0 || w1 > cap))
+      w1 = w0 + count;
+      if (count > 0 && (w0 < 0 || w1 > cap))
         return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d writes positions [%lld, %lld) outside [0, %lld)", b, w0,
                     w1, cap);
     } else if (step_write && seq_lens[b] > 0) {

@@ -38,11 +38,26 @@ nova_kv_status check_scales(const nova_kv_params *p, const void *k_scales);
 nova_kv_status check_band(const nova_kv_band *band);
 nova_kv_status check_sq(const nova_kv_params *p, const void *v_sq);
 
+// The norms and rotation of a layer's heads (nova_kv_rotary), for the sides that
+// a call has.
+nova_kv_status check_rotary(const nova_kv_rotary *r, bool with_q, bool with_k);
+// Rows of heads (NULL: absent) and the dense output that belongs to them.
+nova_kv_status check_rows(const char *name, const nova_kv_rows *rows, const void *out, nova_kv_dtype dtype,
+                          bool need_out);
+// An output may be its own input, where that is dense, and overlaps no other
+// input and no other output.
+nova_kv_status check_overlaps(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
+                              const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                              const void *q_out, const void *k_out, const void *v_out);
+// A 4-bit cache.
+nova_kv_status check_q4_cache(const nova_kv_q4_cache *c);
+
 // Host copies of a call's metadata, checked against the layout (see
-// nova_kv_check_metadata): block_table is a host array here.
+// nova_kv_check_metadata): block_table is a host array here.  With new_lens a
+// sequence writes only its first new_lens[b] (at most n_new) positions.
 nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch,
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
-                              int32_t n_new);
+                              int32_t n_new, const int32_t *new_lens = nullptr);
 
 // Debug mode (nova_kv_set_debug; initially on when the environment variable
 // NOVA_KV_DEBUG is a nonzero number): entry points copy their metadata to

@@ -1,0 +1,464 @@
+// Attention over a cache held in 4 bits (nova_kv_q4_attn).
+//
+// A row of the cache is k = offset + scale * c with 4-bit codes c, so
+//   q . k_j = scale_j (q . c_j) + offset_j sum(q)
+//   out     = (sum_j (p_j scale'_j) c'_j + sum_j p_j offset'_j) / sum_j p_j
+// and both products run on the matrix cores over the codes themselves.
+//
+// Scores: on the 8-bit integer cores, exact. A word's codes are two words of
+// bytes (three instructions for eight codes); the query is a fixed-point number
+// of two digits of 7 bits (three for fp32 queries) of its row's largest
+// magnitude.
+//
+// Values: on the fp16 cores, as c - 8: a nibble masked in place under the bits of
+// 1024 is the fp16 number 1024 + c (1024 + 16 c, its bits four higher), from which a
+// packed subtraction leaves c - 8 (16 (c - 8)) exactly. (The nibble alone would be
+// a denormal that the cores multiply exactly too, but they align it with the sum
+// so far by its exponent field, ten bits above its value, and cut those bits off
+// the sum: 1e-5 of an output, towards one side.)
+#include <algorithm>
+#include <type_traits>
+
+#include "lut_common.h"
+#include "q4_internal.h"
+
+namespace novakv {
+
+namespace {
+
+using lut::add_rows16;
+using lut::add_rows32;
+using lut::float4_t;
+using lut::half8_t;
+using lut::max_rows16;
+using lut::max_rows32;
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kRound = 32;    // tokens a wave takes at a time
+// The fp16 cores add the products of eight slots after cutting them about 24 bits
+// below the largest, then round to nearest (measured). A sum of small multiples of
+// one unit is therefore exact; one of products far apart loses what lies below
+// the cut, towards one side, which fp32 outputs would show. So with fp32
+// queries a probability is split into two fixed-point parts of 11 bits and the rest.
+constexpr float kNone = -__builtin_inff();
+
+__device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdgcn_exp2f(x); }
+
+typedef int int4_t __attribute__((ext_vector_type(4)));
+
+// Codes k and k + 4 of a word less 8, as two fp16 numbers in a word (times 16 for odd k).
+template <int K>
+__device__ __forceinline__ uint32_t value_pair(const uint32_t w) {
+  const uint32_t x = K < 2 ? w : w >> 8;
+  const uint32_t pair = (x & (K % 2 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+  const lut::half2_t bias = __builtin_bit_cast(lut::half2_t, K % 2 ? 0x64806480u : 0x64086408u);
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(lut::half2_t, pair) - bias);
+}
+
+// Coordinate of a lane's output value: tile t, accumulator register i, lane row j.
+template <int D>
+__device__ __forceinline__ int out_coord(const int t, const int i, const int j) {
+  const int m = 4 * j + i;
+  return D == 128 ? 8 * m + t : 8 * (m & 7) + 4 * (m >> 3) + t;
+}
+
+template <int D, bool WIDE, int NT, int WT>
+__global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
+  constexpr int kSteps = D / 64;          // matrix steps of a score
+  constexpr int kTiles = D / 16;          // output tiles
+  constexpr int kKeyWords = D / 32;       // words of a lane's part of a key row
+  constexpr int kDigits = WIDE ? 3 : 2;   // 7-bit digits of a query
+  constexpr float kTopQ = WIDE ? 127.f * 128 * 128 : 127.f * 128;  // the largest fixed-point number
+  constexpr int kProbParts = WIDE ? 3 : 1;  // and of a probability
+  // log2 of the largest scaled probability after a rescale, and how far it may
+  // grow before the next one: 2^14 fits fp16, 2^11 units of 1 are 11 bits
+  constexpr float kTop = WIDE ? 10.f : 6.f, kSlack = WIDE ? 1.f : 8.f;
+  constexpr int kRowGroups = kWaves / WT; // waves on rows of their own
+  constexpr int kRows = 16 * NT * kRowGroups;
+  constexpr int kStride = D + 4;
+
+  __shared__ __align__(16) uint32_t s_rows[kWaves][kRound];
+  __shared__ __align__(16) uint32_t s_sq[kWaves][2 * kRound];
+  __shared__ float s_ref[kWaves][16 * NT], s_sum[kWaves][16 * NT];
+  __shared__ __align__(16) float s_out[WT > 1 ? 16 * NT * kStride : 4];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+  const int tw = wave % WT, rw = wave / WT;
+
+  int wg = blockIdx.x;
+  const int split = wg % a.n_split;
+  wg /= a.n_split;
+  const int tile = wg % a.row_tiles;
+  const int unit = wg / a.row_tiles;
+  const int b = unit / a.num_kv_heads, kv = unit - b * a.num_kv_heads;
+
+  const int S = min(max(a.seq_lens[b], 0), a.max_seq_len);
+  const int nb = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
+  const int rows_valid = nb * a.gqa;
+  const int wg_row0 = tile * kRows;
+  if (wg_row0 >= rows_valid) return;
+  const int wg_row1 = min(wg_row0 + kRows, rows_valid);
+  // attended positions of query token i: [first_pos(i), S - nb + i]
+  auto last_pos = [&](const int row) { return S - nb + row / a.gqa; };
+  auto first_pos = [&](const int row) { return a.window > 0 ? max(0, last_pos(row) + 1 - a.window) : 0; };
+  const int hi = last_pos(wg_row1 - 1) + 1, lo = first_pos(wg_row0);
+  const int base = lo & ~(kRound - 1);
+  const int span = max(0, hi - base);
+  const int per = ((span + a.n_split - 1) / a.n_split + kRound * WT - 1) / (kRound * WT) * (kRound * WT);
+  const int t0 = min(base + split * per, base + span), t1 = min(t0 + per, base + span);
+
+  // this wave's rows
+  const int row0 = wg_row0 + rw * 16 * NT;
+  const int row1 = min(row0 + 16 * NT, rows_valid);
+  const bool idle = row0 >= rows_valid;
+  const int inner_lo = idle ? 0 : first_pos(row1 - 1), inner_hi = idle ? 0 : last_pos(row0) + 1;
+
+  int4_t qf[NT][kDigits][kSteps];
+  float alpha[NT], qsum[NT], ref[NT], sum[NT], off_sum[NT];
+  int row_lo[NT], row_hi[NT];
+  float4_t acc[NT][kTiles];
+  for (int t = 0; t < NT; ++t) {
+    const int row = row0 + 16 * t + n;
+    const bool on = row < rows_valid;
+    const int i = row / a.gqa, g = row - i * a.gqa;
+    row_hi[t] = on ? last_pos(row) + 1 : 0;
+    row_lo[t] = on ? first_pos(row) : 0;
+    float x[kKeyWords][8];
+    float top = 0.f;
+    bool finite = true;
+    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + g) * D + 8 * kKeyWords * j;
+    for (int s = 0; s < kKeyWords; ++s) {
+      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+      if (on) {
+        if constexpr (!WIDE) {
+          const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 8 * s);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+          for (int e = 0; e < 4; ++e) {
+            x[s][2 * e] = __uint_as_float(u[e] << 16);
+            x[s][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+          }
+        } else {
+          const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 8 * s);
+          const float4 u = f[0], v = f[1];
+          x[s][0] = u.x, x[s][1] = u.y, x[s][2] = u.z, x[s][3] = u.w;
+          x[s][4] = v.x, x[s][5] = v.y, x[s][6] = v.z, x[s][7] = v.w;
+        }
+      }
+      for (int e = 0; e < 8; ++e) {
+        finite = finite && fabsf(x[s][e]) < __builtin_inff();
+        top = fmaxf(top, fabsf(x[s][e]));
+      }
+    }
+    top = max_rows32(max_rows16(finite ? top : __builtin_inff()));
+    const bool usable = top < __builtin_inff();
+    const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
+    int total = 0;
+    for (int s = 0; s < kSteps; ++s)
+      for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
+    for (int s = 0; s < kKeyWords; ++s) {
+      for (int e = 0; e < 8; ++e) {
+        int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
+        total += f;
+        // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
+        for (int d = 0; d < kDigits; ++d) {
+          const int digit = d == kDigits - 1 ? f : ((f + 64) & 127) - 64;
+          f = (f - digit) >> 7;
+          qf[t][d][s / 2][2 * (s % 2) + e % 2] |= (digit & 255) << (8 * (e / 2));
+        }
+      }
+    }
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    qsum[t] = static_cast<float>(total);
+    alpha[t] = usable ? a.qscale / to_fixed : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    ref[t] = kNone;
+    sum[t] = off_sum[t] = 0.f;
+    for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const size_t heads_rows = static_cast<size_t>(a.num_kv_heads) * a.layout.block_size;
+  const uint32_t *k_sq = reinterpret_cast<const uint32_t *>(a.k_sq), *v_sq = reinterpret_cast<const uint32_t *>(a.v_sq);
+  for (int tb = t0 + kRound * tw; tb < t1 && !idle; tb += kRound * WT) {
+    // row, scale and offset of token tb + lane % 32 (key: lanes 0..31, value: 32..63);
+    // a token outside the span or in a block that holds nothing takes row 0 and counts as masked
+    const int tok = tb + (lane & 31);
+    bool ok = tok < t1 && tok >= lo;
+    uint32_t row = 0;
+    if (ok) {
+      const int blk = tok / a.layout.block_size;
+      const long long logical = static_cast<long long>(b) * a.layout.blocks_per_seq + blk;
+      const long long phys = a.layout.block_table ? a.layout.block_table[logical] : logical;
+      ok = phys >= 0 && phys < a.num_blocks;
+      if (ok)
+        row = static_cast<uint32_t>(phys * heads_rows + static_cast<size_t>(kv) * a.layout.block_size +
+                                    (tok - blk * a.layout.block_size));
+    }
+    const uint32_t valid = static_cast<uint32_t>(__ballot(ok));
+    s_rows[wave][lane & 31] = row;
+    s_sq[wave][lane] = ok ? (lane < 32 ? k_sq[row] : v_sq[row]) : 0u;
+    __builtin_amdgcn_wave_barrier();
+    uint32_t kw[2][kKeyWords];
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t *p = a.k_codes + static_cast<size_t>(s_rows[wave][16 * h + n]) * (D / 2) + 4 * kKeyWords * j;
+      if constexpr (D == 128) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+        kw[h][0] = w.x, kw[h][1] = w.y, kw[h][2] = w.z, kw[h][3] = w.w;
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        kw[h][0] = w.x, kw[h][1] = w.y;
+      }
+    }
+    // the lane's 8 tokens: 4j + i and 16 + 4j + i, as its scores have them
+    uint32_t vw[8], ksq[8], vsq[8];
+    for (int e = 0; e < 8; ++e) {
+      const int m = 16 * (e >> 2) + 4 * j + (e & 3);
+      vw[e] = *reinterpret_cast<const uint32_t *>(a.v_codes + static_cast<size_t>(s_rows[wave][m]) * (D / 2) +
+                                                  4 * (n & (D / 8 - 1)));
+      ksq[e] = s_sq[wave][m];
+      vsq[e] = s_sq[wave][32 + m];
+    }
+    __builtin_amdgcn_wave_barrier();
+
+    const bool inner = valid == 0xffffffffu && tb >= inner_lo && tb + kRound <= inner_hi;
+    float vs[8], top_vs = 0x1p-100f;
+    for (int e = 0; e < 8; ++e) {
+      vs[e] = __uint_as_float(vsq[e] << 16);
+      top_vs = fmaxf(top_vs, vs[e]);
+    }
+    const float log_vs = __builtin_amdgcn_logf(top_vs);
+    int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
+    for (int h = 0; h < 2; ++h)
+      for (int s = 0; s < kKeyWords; ++s) {
+        kc[h][s / 2][2 * (s % 2)] = static_cast<int>(kw[h][s] & 0x0f0f0f0fu);
+        kc[h][s / 2][2 * (s % 2) + 1] = static_cast<int>((kw[h][s] >> 4) & 0x0f0f0f0fu);
+      }
+    half8_t pf[NT][kProbParts];
+    for (int t = 0; t < NT; ++t) {
+      int4_t d[2][kDigits];
+      for (int h = 0; h < 2; ++h)
+        for (int x = 0; x < kDigits; ++x) {
+          d[h][x] = int4_t{0, 0, 0, 0};
+          for (int s = 0; s < kSteps; ++s) d[h][x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[h][x], 0, 0, 0);
+        }
+      float z[8], top = kNone;
+      uint32_t masked = 0;
+      for (int e = 0; e < 8; ++e) {
+        const float ks = __uint_as_float(ksq[e] << 16), ko = __uint_as_float(ksq[e] & 0xffff0000u);
+        const int4_t(&dig)[kDigits] = d[e >> 2];
+        float dot = static_cast<float>((dig[1][e & 3] << 7) + dig[0][e & 3]);
+        if constexpr (WIDE) dot = __builtin_fmaf(16384.f, static_cast<float>(dig[2][e & 3]), dot);
+        z[e] = ks * dot + ko * qsum[t];
+        if (!inner) {
+          const int m = 16 * (e >> 2) + 4 * j + (e & 3);
+          const bool seen = ((valid >> m) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
+          if (!seen) masked |= 1u << e;
+          z[e] = seen ? z[e] : kNone;
+        }
+        top = fmaxf(top, z[e]);
+      }
+      const float bound = top * alpha[t] + log_vs;
+      if (__any(bound > ref[t] + (kTop + kSlack))) {
+        const float most = max_rows32(max_rows16(bound));
+        const float next = fmaxf(ref[t], most - kTop);
+        const float f = next == kNone ? 1.f : exp2_raw(ref[t] - next);
+        ref[t] = next;
+        sum[t] *= f;
+        off_sum[t] *= f;
+        for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+      }
+      const float r = ref[t] == kNone ? 0.f : ref[t];
+      for (int e = 0; e < 8; ++e) {
+        const float p = exp2_raw(__builtin_fmaf(z[e], alpha[t], -r));
+        const float offset = __uint_as_float(vsq[e] & 0xffff0000u);
+        float ps = p * vs[e], po = p * __builtin_fmaf(8.f, vs[e], offset);
+        if (!inner && ((masked >> e) & 1u)) ps = po = 0.f;  // whatever a hidden token's scale and offset are
+        sum[t] += p;
+        off_sum[t] += po;
+        if constexpr (WIDE) {  // units of 1, units of 2^-11, what is left
+          const float high = rintf(ps), rest = ps - high, mid = rintf(rest * 0x1p11f) * 0x1p-11f;
+          pf[t][0][e] = static_cast<_Float16>(high);
+          pf[t][1][e] = static_cast<_Float16>(mid);
+          pf[t][2][e] = static_cast<_Float16>(rest - mid);
+        } else {
+          pf[t][0][e] = static_cast<_Float16>(ps);
+        }
+      }
+    }
+
+    // the same coordinate's codes of two tokens in one word
+    uint32_t vo[kTiles][4];
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w0 = vw[2 * e], w1 = vw[2 * e + 1];
+      if constexpr (D == 128) {
+        const uint32_t low = __builtin_amdgcn_perm(w1, w0, 0x05040100u), high = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
+        vo[0][e] = value_pair<0>(low), vo[1][e] = value_pair<1>(low), vo[2][e] = value_pair<2>(low), vo[3][e] = value_pair<3>(low);
+        vo[4][e] = value_pair<0>(high), vo[5][e] = value_pair<1>(high), vo[6][e] = value_pair<2>(high), vo[7][e] = value_pair<3>(high);
+      } else {  // lanes 0..7 of a row take a word's low four nibbles, lanes 8..15 its high ones
+        const uint32_t half = __builtin_amdgcn_perm(w1, w0, n < 8 ? 0x05040100u : 0x07060302u);
+        vo[0][e] = value_pair<0>(half), vo[1][e] = value_pair<1>(half), vo[2][e] = value_pair<2>(half), vo[3][e] = value_pair<3>(half);
+      }
+    }
+    for (int o = 0; o < kTiles; ++o) {
+      const half8_t c = __builtin_bit_cast(half8_t, make_uint4(vo[o][0], vo[o][1], vo[o][2], vo[o][3]));
+      for (int t = 0; t < NT; ++t)
+        for (int x = 0; x < kProbParts; ++x)
+          acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, pf[t][x], acc[t][o], 0, 0, 0);
+    }
+  }
+
+  // the wave's partials
+  for (int t = 0; t < NT; ++t) {
+    sum[t] = add_rows32(add_rows16(sum[t]));
+    off_sum[t] = add_rows32(add_rows16(off_sum[t]));
+    if (sum[t] != sum[t]) ref[t] = fmaxf(ref[t], 0.f);  // NaN logits move no reference, but attend
+    for (int o = 0; o < kTiles; ++o)
+      for (int i = 0; i < 4; ++i) acc[t][o][i] = acc[t][o][i] * (o % 2 ? 0.0625f : 1.f) + off_sum[t];
+  }
+  if constexpr (WT > 1) {
+    // merge over the waves: the largest reference, then one wave's share after the other's
+    for (int t = 0; t < NT; ++t)
+      if (j == 0) s_ref[wave][16 * t + n] = ref[t], s_sum[wave][16 * t + n] = sum[t];
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == wave)
+        for (int t = 0; t < NT; ++t) {
+          float most = kNone;
+          for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][16 * t + n]);
+          const float f = ref[t] == kNone ? 0.f : exp2_raw(ref[t] - most);
+          for (int o = 0; o < kTiles; ++o)
+            for (int i = 0; i < 4; ++i) {
+              float &dst = s_out[(16 * t + n) * kStride + out_coord<D>(o, i, j)];
+              const float v = ref[t] == kNone ? 0.f : acc[t][o][i] * f;
+              dst = w == 0 ? v : dst + v;
+            }
+        }
+      __syncthreads();
+    }
+    for (int x = threadIdx.x; x < 16 * NT * (D / 4); x += kThreads) {
+      const int r = x / (D / 4), c = 4 * (x % (D / 4));
+      const int row = wg_row0 + r;
+      if (row >= rows_valid) continue;
+      float most = kNone, l = 0.f;
+      for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][r]);
+      for (int u = 0; u < kWaves; ++u)
+        if (s_ref[u][r] != kNone) l += s_sum[u][r] * exp2_raw(s_ref[u][r] - most);
+      const float4 v = *reinterpret_cast<const float4 *>(&s_out[r * kStride + c]);
+      const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
+      if (a.n_split > 1) {
+        float *p = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * kRows * (D + 2);
+        *reinterpret_cast<float4 *>(p + r * D + c) = v;
+        if (c == 0) p[kRows * D + 2 * r] = most, p[kRows * D + 2 * r + 1] = l;
+      } else {
+        if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - most);
+        const float f = most == kNone ? 0.f : 1.f / l;
+        const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D + c;
+        const float o[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
+        for (int e = 0; e < 4; ++e) {
+          if (a.q_bf16) static_cast<__bf16 *>(a.out)[at + e] = static_cast<__bf16>(most == kNone ? 0.f : o[e]);
+          else static_cast<float *>(a.out)[at + e] = most == kNone ? 0.f : o[e];
+        }
+      }
+    }
+  } else {
+    for (int t = 0; t < NT; ++t) {
+      const int row = row0 + 16 * t + n;
+      if (row >= rows_valid) continue;
+      const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
+      if (a.n_split > 1) {
+        const int r = row - wg_row0;
+        float *p = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * kRows * (D + 2);
+        for (int o = 0; o < kTiles; ++o)
+          for (int e = 0; e < 4; ++e) p[r * D + out_coord<D>(o, e, j)] = ref[t] == kNone ? 0.f : acc[t][o][e];
+        if (j == 0) p[kRows * D + 2 * r] = ref[t], p[kRows * D + 2 * r + 1] = sum[t];
+      } else {
+        float l = sum[t];
+        if (a.sinks && ref[t] != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - ref[t]);
+        const float f = 1.f / l;
+        const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D;
+        for (int o = 0; o < kTiles; ++o)
+          for (int e = 0; e < 4; ++e) {
+            const float v = ref[t] == kNone ? 0.f : acc[t][o][e] * f;
+            const size_t to = at + out_coord<D>(o, e, j);
+            if (a.q_bf16) static_cast<__bf16 *>(a.out)[to] = static_cast<__bf16>(v);
+            else static_cast<float *>(a.out)[to] = v;
+          }
+      }
+    }
+  }
+}
+
+// The splits' partials of a row, one workgroup of D threads per row.
+template <int D>
+__global__ __launch_bounds__(D) void q4_combine_kernel(const Q4AttnArgs a, const int tile_rows) {
+  const int r = blockIdx.x % tile_rows;
+  int wg = blockIdx.x / tile_rows;
+  const int tile = wg % a.row_tiles, unit = wg / a.row_tiles;
+  const int b = unit / a.num_kv_heads, kv = unit - b * a.num_kv_heads;
+  const int nb = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
+  const int row = tile * tile_rows + r;
+  if (row >= nb * a.gqa) return;
+  const size_t slot = static_cast<size_t>(tile_rows) * (D + 2);
+  const float *p = a.part + (static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split * slot;
+  const float *ml = p + static_cast<size_t>(tile_rows) * D + 2 * r;
+  float most = kNone;
+  for (int s = 0; s < a.n_split; ++s) most = fmaxf(most, ml[s * slot]);
+  float l = 0.f, v = 0.f;
+  for (int s = 0; s < a.n_split; ++s) {
+    const float m = ml[s * slot];
+    if (m == kNone) continue;
+    const float f = exp2_raw(m - most);
+    l += f * ml[s * slot + 1];
+    v += f * p[s * slot + r * D + threadIdx.x];
+  }
+  const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
+  if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - most);
+  v = most == kNone ? 0.f : v / l;
+  const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D + threadIdx.x;
+  if (a.q_bf16) static_cast<__bf16 *>(a.out)[at] = static_cast<__bf16>(v);
+  else static_cast<float *>(a.out)[at] = v;
+}
+
+}  // namespace
+
+// Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the
+// workgroup's waves sharing the tokens; more rows take 128 a workgroup, 32 a
+// wave.  The span is split to reach about two workgroups a CU.
+Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads,
+                        const int head_dim, const int max_seq_len, const int window) {
+  Q4AttnPlan p{};
+  const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
+  p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
+  const long long tiles = static_cast<long long>(batch) * num_kv_heads * p.row_tiles;
+  const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
+  const long long want = std::max<long long>(1, 512 / tiles), most = std::max<long long>(1, (span + 255) / 256);
+  p.n_split = static_cast<int>(std::min(want, most));
+  auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
+  if (p.n_split > 1) {
+    p.off_part = up(static_cast<size_t>(tiles) * sizeof(int));
+    p.total = p.off_part + up(static_cast<size_t>(tiles) * p.n_split * p.tile_rows * (head_dim + 2) * sizeof(float));
+  }
+  return p;
+}
+
+hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
+  const unsigned tiles = static_cast<unsigned>(a.batch) * a.num_kv_heads * a.row_tiles;
+  auto go = [&](auto d, auto wide, auto nt, auto wt) {
+    q4_attn_kernel<d(), wide(), nt(), wt()><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n_split == 1) return e;
+    q4_combine_kernel<d()><<<tiles * plan.tile_rows, d(), 0, stream>>>(a, plan.tile_rows);
+    return hipGetLastError();
+  };
+  auto by_rows = [&](auto d, auto wide) {
+    using std::integral_constant;
+    if (plan.tile_rows == 16) return go(d, wide, integral_constant<int, 1>{}, integral_constant<int, 4>{});
+    if (plan.tile_rows == 32) return go(d, wide, integral_constant<int, 2>{}, integral_constant<int, 4>{});
+    return go(d, wide, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  };
+  auto by_type = [&](auto d) { return a.q_bf16 ? by_rows(d, std::false_type{}) : by_rows(d, std::true_type{}); };
+  return a.head_dim == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
+}
+
+}  // namespace novakv
