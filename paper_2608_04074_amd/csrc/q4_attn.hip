@@ -62,7 +62,7 @@ __device__ __forceinline__ int out_coord(const int t, const int i, const int j) 
   return D == 128 ? 8 * m + t : 8 * (m & 7) + 4 * (m >> 3) + t;
 }
 
-template <int D, bool WIDE, int NT, int WT>
+template <int D, bool WIDE, int NT, int WT, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   constexpr int kSteps = D / 64;          // matrix steps of a score
   constexpr int kTiles = D / 16;          // output tiles
@@ -77,8 +77,8 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   constexpr int kRows = 16 * NT * kRowGroups;
   constexpr int kStride = D + 4;
 
-  __shared__ __align__(16) uint32_t s_rows[kWaves][kRound];
-  __shared__ __align__(16) uint32_t s_sq[kWaves][2 * kRound];
+  __shared__ __align__(16) uint32_t s_rows[ALIGNED ? 1 : kWaves][kRound];
+  __shared__ __align__(16) float s_scale[kWaves][2 * kRound], s_offset[kWaves][2 * kRound];
   __shared__ float s_ref[kWaves][16 * NT], s_sum[kWaves][16 * NT];
   __shared__ __align__(16) float s_out[WT > 1 ? 16 * NT * kStride : 4];
 
@@ -177,61 +177,118 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  const size_t heads_rows = static_cast<size_t>(a.num_kv_heads) * a.layout.block_size;
-  const uint32_t *k_sq = reinterpret_cast<const uint32_t *>(a.k_sq), *v_sq = reinterpret_cast<const uint32_t *>(a.v_sq);
-  for (int tb = t0 + kRound * tw; tb < t1 && !idle; tb += kRound * WT) {
-    // row, scale and offset of token tb + lane % 32 (key: lanes 0..31, value: 32..63);
-    // a token outside the span or in a block that holds nothing takes row 0 and counts as masked
-    const int tok = tb + (lane & 31);
-    bool ok = tok < t1 && tok >= lo;
-    uint32_t row = 0;
-    if (ok) {
-      const int blk = tok / a.layout.block_size;
-      const long long logical = static_cast<long long>(b) * a.layout.blocks_per_seq + blk;
-      const long long phys = a.layout.block_table ? a.layout.block_table[logical] : logical;
-      ok = phys >= 0 && phys < a.num_blocks;
-      if (ok)
-        row = static_cast<uint32_t>(phys * heads_rows + static_cast<size_t>(kv) * a.layout.block_size +
-                                    (tok - blk * a.layout.block_size));
+  // Rounds of 32 tokens, the codes, scales and offsets of one requested while
+  // the round before is computed, its block-table entries one round earlier.
+  const int bs = a.layout.block_size, bps = a.layout.blocks_per_seq;
+  const uint32_t block_rows = static_cast<uint32_t>(a.num_kv_heads) * bs, head_row = static_cast<uint32_t>(kv) * bs;
+  const int32_t *table = a.layout.block_table ? a.layout.block_table + static_cast<size_t>(b) * bps : nullptr;
+  const uint32_t *sq = reinterpret_cast<const uint32_t *>(lane < 32 ? a.k_sq : a.v_sq);
+  const uint32_t k_lane = n * (D / 2) + 4 * kKeyWords * j, v_lane = 4 * j * (D / 2) + 4 * (n & (D / 8 - 1));
+  constexpr int kStep = kRound * WT;
+  int look = t0 + kRound * tw + (lane & 31);  // the lane's token of the round that is looked up next
+  int look_blk = look / bs, look_row = look - look_blk * bs;
+  const int step_blk = kStep / bs, step_row = kStep - step_blk * bs;
+  int phys = -1, phys_tok = 0, phys_row = 0;
+  auto look_up = [&]() {
+    phys = -1;
+    phys_tok = look;
+    phys_row = look_row;
+    if (look_blk < bps) {
+      const long long own = static_cast<long long>(b) * bps + look_blk;
+      phys = table ? table[look_blk] : own < a.num_blocks ? static_cast<int>(own) : -1;
     }
-    const uint32_t valid = static_cast<uint32_t>(__ballot(ok));
-    s_rows[wave][lane & 31] = row;
-    s_sq[wave][lane] = ok ? (lane < 32 ? k_sq[row] : v_sq[row]) : 0u;
-    __builtin_amdgcn_wave_barrier();
-    uint32_t kw[2][kKeyWords];
-    for (int h = 0; h < 2; ++h) {
-      const uint8_t *p = a.k_codes + static_cast<size_t>(s_rows[wave][16 * h + n]) * (D / 2) + 4 * kKeyWords * j;
-      if constexpr (D == 128) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(p);
-        kw[h][0] = w.x, kw[h][1] = w.y, kw[h][2] = w.z, kw[h][3] = w.w;
-      } else {
-        const uint2 w = *reinterpret_cast<const uint2 *>(p);
-        kw[h][0] = w.x, kw[h][1] = w.y;
+    look += kStep;
+    look_blk += step_blk;
+    look_row += step_row;
+    if (look_row >= bs) look_row -= bs, ++look_blk;
+  };
+  struct Round {
+    uint32_t kw[2][kKeyWords], vw[8], sq;
+    bool ok;
+  };
+  // Requests the round that was looked up. A token outside the span counts as
+  // masked; one in a block that holds nothing too, in its place a row at the
+  // pool's start is read.
+  auto request = [&](Round &r) {
+    const bool held = static_cast<uint32_t>(phys) < static_cast<uint32_t>(a.num_blocks);
+    r.ok = held && phys_tok < t1 && phys_tok >= lo;
+    uint32_t row = static_cast<uint32_t>(phys) * block_rows + head_row + phys_row;
+    if constexpr (ALIGNED) {  // blocks of a multiple of 16 rows: a half round's rows follow each other
+      if (!held) row = lane & 15;
+      for (int h = 0; h < 2; ++h) {
+        const size_t first = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(row, 16 * h))) * (D / 2);
+        const uint8_t *k = a.k_codes + first, *v = a.v_codes + first;
+        if constexpr (D == 128) {
+          const uint4 w = *reinterpret_cast<const uint4 *>(k + k_lane);
+          r.kw[h][0] = w.x, r.kw[h][1] = w.y, r.kw[h][2] = w.z, r.kw[h][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2 *>(k + k_lane);
+          r.kw[h][0] = w.x, r.kw[h][1] = w.y;
+        }
+        for (int e = 0; e < 4; ++e) r.vw[4 * h + e] = *reinterpret_cast<const uint32_t *>(v + (v_lane + e * (D / 2)));
       }
+    } else {
+      if (!r.ok) row = 0;
+      s_rows[wave][lane & 31] = row;
+      __builtin_amdgcn_wave_barrier();
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t *k = a.k_codes + static_cast<size_t>(s_rows[wave][16 * h + n]) * (D / 2) + 4 * kKeyWords * j;
+        if constexpr (D == 128) {
+          const uint4 w = *reinterpret_cast<const uint4 *>(k);
+          r.kw[h][0] = w.x, r.kw[h][1] = w.y, r.kw[h][2] = w.z, r.kw[h][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2 *>(k);
+          r.kw[h][0] = w.x, r.kw[h][1] = w.y;
+        }
+        for (int e = 0; e < 4; ++e)
+          r.vw[4 * h + e] = *reinterpret_cast<const uint32_t *>(
+              a.v_codes + static_cast<size_t>(s_rows[wave][16 * h + 4 * j + e]) * (D / 2) + 4 * (n & (D / 8 - 1)));
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    // the lane's 8 tokens: 4j + i and 16 + 4j + i, as its scores have them
-    uint32_t vw[8], ksq[8], vsq[8];
-    for (int e = 0; e < 8; ++e) {
-      const int m = 16 * (e >> 2) + 4 * j + (e & 3);
-      vw[e] = *reinterpret_cast<const uint32_t *>(a.v_codes + static_cast<size_t>(s_rows[wave][m]) * (D / 2) +
-                                                  4 * (n & (D / 8 - 1)));
-      ksq[e] = s_sq[wave][m];
-      vsq[e] = s_sq[wave][32 + m];
+    r.sq = sq[row];
+  };
+
+  Round cur, next;
+  if (!idle && t0 + kRound * tw < t1) {
+    look_up();
+    request(cur);
+    look_up();
+  }
+  for (int tb = t0 + kRound * tw; tb < t1 && !idle; tb += kStep) {
+    request(next);  // past the last round: rows at the pool's start or of a block's end, masked
+    look_up();
+
+    const uint32_t valid = static_cast<uint32_t>(__ballot(cur.ok));
+    {
+      float scale = __uint_as_float(cur.sq << 16), offset = __uint_as_float(cur.sq & 0xffff0000u);
+      if (lane >= 32) offset = __builtin_fmaf(8.f, scale, offset);  // values count from code 8
+      s_scale[wave][lane] = cur.ok ? scale : 0.f;
+      s_offset[wave][lane] = cur.ok ? offset : 0.f;
+    }
+    __builtin_amdgcn_wave_barrier();
+    // of the lane's 8 tokens, 4j + i and 16 + 4j + i, as its scores have them
+    float ks[8], ko[8], vs[8], vo8[8];
+    for (int h = 0; h < 2; ++h) {
+      const float4 x[4] = {*reinterpret_cast<const float4 *>(&s_scale[wave][16 * h + 4 * j]),
+                           *reinterpret_cast<const float4 *>(&s_offset[wave][16 * h + 4 * j]),
+                           *reinterpret_cast<const float4 *>(&s_scale[wave][32 + 16 * h + 4 * j]),
+                           *reinterpret_cast<const float4 *>(&s_offset[wave][32 + 16 * h + 4 * j])};
+      float *to[4] = {ks, ko, vs, vo8};
+      for (int y = 0; y < 4; ++y)
+        to[y][4 * h] = x[y].x, to[y][4 * h + 1] = x[y].y, to[y][4 * h + 2] = x[y].z, to[y][4 * h + 3] = x[y].w;
     }
     __builtin_amdgcn_wave_barrier();
 
     const bool inner = valid == 0xffffffffu && tb >= inner_lo && tb + kRound <= inner_hi;
-    float vs[8], top_vs = 0x1p-100f;
-    for (int e = 0; e < 8; ++e) {
-      vs[e] = __uint_as_float(vsq[e] << 16);
-      top_vs = fmaxf(top_vs, vs[e]);
-    }
+    float top_vs = 0x1p-100f;
+    for (int e = 0; e < 8; ++e) top_vs = fmaxf(top_vs, vs[e]);
     const float log_vs = __builtin_amdgcn_logf(top_vs);
     int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
     for (int h = 0; h < 2; ++h)
       for (int s = 0; s < kKeyWords; ++s) {
-        kc[h][s / 2][2 * (s % 2)] = static_cast<int>(kw[h][s] & 0x0f0f0f0fu);
-        kc[h][s / 2][2 * (s % 2) + 1] = static_cast<int>((kw[h][s] >> 4) & 0x0f0f0f0fu);
+        kc[h][s / 2][2 * (s % 2)] = static_cast<int>(cur.kw[h][s] & 0x0f0f0f0fu);
+        kc[h][s / 2][2 * (s % 2) + 1] = static_cast<int>((cur.kw[h][s] >> 4) & 0x0f0f0f0fu);
       }
     half8_t pf[NT][kProbParts];
     for (int t = 0; t < NT; ++t) {
@@ -244,11 +301,10 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
       float z[8], top = kNone;
       uint32_t masked = 0;
       for (int e = 0; e < 8; ++e) {
-        const float ks = __uint_as_float(ksq[e] << 16), ko = __uint_as_float(ksq[e] & 0xffff0000u);
         const int4_t(&dig)[kDigits] = d[e >> 2];
         float dot = static_cast<float>((dig[1][e & 3] << 7) + dig[0][e & 3]);
         if constexpr (WIDE) dot = __builtin_fmaf(16384.f, static_cast<float>(dig[2][e & 3]), dot);
-        z[e] = ks * dot + ko * qsum[t];
+        z[e] = ks[e] * dot + ko[e] * qsum[t];
         if (!inner) {
           const int m = 16 * (e >> 2) + 4 * j + (e & 3);
           const bool seen = ((valid >> m) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
@@ -270,8 +326,7 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
       const float r = ref[t] == kNone ? 0.f : ref[t];
       for (int e = 0; e < 8; ++e) {
         const float p = exp2_raw(__builtin_fmaf(z[e], alpha[t], -r));
-        const float offset = __uint_as_float(vsq[e] & 0xffff0000u);
-        float ps = p * vs[e], po = p * __builtin_fmaf(8.f, vs[e], offset);
+        float ps = p * vs[e], po = p * vo8[e];
         if (!inner && ((masked >> e) & 1u)) ps = po = 0.f;  // whatever a hidden token's scale and offset are
         sum[t] += p;
         off_sum[t] += po;
@@ -289,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
     // the same coordinate's codes of two tokens in one word
     uint32_t vo[kTiles][4];
     for (int e = 0; e < 4; ++e) {
-      const uint32_t w0 = vw[2 * e], w1 = vw[2 * e + 1];
+      const uint32_t w0 = cur.vw[2 * e], w1 = cur.vw[2 * e + 1];
       if constexpr (D == 128) {
         const uint32_t low = __builtin_amdgcn_perm(w1, w0, 0x05040100u), high = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
         vo[0][e] = value_pair<0>(low), vo[1][e] = value_pair<1>(low), vo[2][e] = value_pair<2>(low), vo[3][e] = value_pair<3>(low);
@@ -305,6 +360,7 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
         for (int x = 0; x < kProbParts; ++x)
           acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, pf[t][x], acc[t][o], 0, 0, 0);
     }
+    cur = next;
   }
 
   // the wave's partials
@@ -445,7 +501,9 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
 hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
   const unsigned tiles = static_cast<unsigned>(a.batch) * a.num_kv_heads * a.row_tiles;
   auto go = [&](auto d, auto wide, auto nt, auto wt) {
-    q4_attn_kernel<d(), wide(), nt(), wt()><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
+    // blocks of a multiple of 16 rows: a round needs two addresses instead of ten a lane
+    if (a.layout.block_size % 16 == 0) q4_attn_kernel<d(), wide(), nt(), wt(), true><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
+    else q4_attn_kernel<d(), wide(), nt(), wt(), false><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_split == 1) return e;
     q4_combine_kernel<d()><<<tiles * plan.tile_rows, d(), 0, stream>>>(a, plan.tile_rows);
