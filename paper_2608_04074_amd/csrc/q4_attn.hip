@@ -41,6 +41,12 @@ constexpr int kRound = 32;    // tokens a wave takes at a time
 // the cut, towards one side, which fp32 outputs would show. So with fp32
 // queries a probability is split into two fixed-point parts of 11 bits and the rest.
 constexpr float kNone = -__builtin_inff();
+// Most splits of a tile's span: their weights lie in LDS (16 or 32 rows, 128 rows).
+constexpr int kMaxSplits = 96, kMaxSplitsTiled = 32;
+// Arrival counters of a workspace: a span is split only where fewer tiles than
+// that run, so no call's partials lie on another shape's counters.
+constexpr int kTargetGroups = 512, kMaxCounters = 1024;
+static_assert(kTargetGroups <= kMaxCounters, "a split launch has at most kTargetGroups / 2 tiles");
 
 __device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -62,6 +68,34 @@ __device__ __forceinline__ int out_coord(const int t, const int i, const int j) 
   return D == 128 ? 8 * m + t : 8 * (m & 7) + 4 * (m >> 3) + t;
 }
 
+// Split partials meet through memory as device-coherent words (lut_common.h).
+__device__ __forceinline__ void publish4(float *p, const float4 v) {
+  uint64_t *w = reinterpret_cast<uint64_t *>(p);
+  const uint64_t lo = (static_cast<uint64_t>(__float_as_uint(v.y)) << 32) | __float_as_uint(v.x);
+  const uint64_t hi = (static_cast<uint64_t>(__float_as_uint(v.w)) << 32) | __float_as_uint(v.z);
+  __hip_atomic_store(w, lo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(w + 1, hi, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void publish2(float *p, const float x, const float y) {
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (static_cast<uint64_t>(__float_as_uint(y)) << 32) | __float_as_uint(x),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 fetch2(const float *p) {
+  const uint64_t w = __hip_atomic_load(reinterpret_cast<uint64_t *>(const_cast<float *>(p)), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float(static_cast<uint32_t>(w)), __uint_as_float(static_cast<uint32_t>(w >> 32)));
+}
+
+__device__ __forceinline__ void store_out(const Q4AttnArgs &a, const size_t at, const float4 v) {
+  if (a.q_bf16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const bf16x4 o = {static_cast<__bf16>(v.x), static_cast<__bf16>(v.y), static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
+    *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at) = o;
+  } else {
+    *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
+  }
+}
+
 template <int D, bool WIDE, int NT, int WT, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   constexpr int kSteps = D / 64;          // matrix steps of a score
@@ -76,11 +110,15 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   constexpr int kRowGroups = kWaves / WT; // waves on rows of their own
   constexpr int kRows = 16 * NT * kRowGroups;
   constexpr int kStride = D + 4;
+  // LDS of the merge over waves, then of the splits' weights and sums
+  constexpr int kMergeFloats = WT > 1 ? kWaves * 16 * NT * kStride : 2 * kRows * kMaxSplitsTiled;
 
   __shared__ __align__(16) uint32_t s_rows[ALIGNED ? 1 : kWaves][kRound];
   __shared__ __align__(16) float s_scale[kWaves][2 * kRound], s_offset[kWaves][2 * kRound];
   __shared__ float s_ref[kWaves][16 * NT], s_sum[kWaves][16 * NT];
-  __shared__ __align__(16) float s_out[WT > 1 ? 16 * NT * kStride : 4];
+  __shared__ __align__(16) float s_merge[kMergeFloats];
+  __shared__ float s_inv[kRows];
+  __shared__ int s_last;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
@@ -371,108 +409,133 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
     for (int o = 0; o < kTiles; ++o)
       for (int i = 0; i < 4; ++i) acc[t][o][i] = acc[t][o][i] * (o % 2 ? 0.0625f : 1.f) + off_sum[t];
   }
-  if constexpr (WT > 1) {
-    // merge over the waves: the largest reference, then one wave's share after the other's
-    for (int t = 0; t < NT; ++t)
+  const int rows_here = wg_row1 - wg_row0;
+  const size_t slot = static_cast<size_t>(kRows) * (D + 2);
+  float *part = nullptr;
+  if (a.n_split > 1) part = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * slot;
+  auto head_of = [&](const int r) { return kv * a.gqa + (wg_row0 + r) % a.gqa; };
+  auto out_at = [&](const int r) {
+    return ((static_cast<size_t>(b) * a.n_q + (wg_row0 + r) / a.gqa) * a.num_q_heads + head_of(r)) * D;
+  };
+  // 1 / the sum of a row's weights with its sink; 0 where nothing is attended
+  auto inverse = [&](const int r, const float most, float l) {
+    if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head_of(r)] * 1.44269504088896341f - most);
+    return most == kNone ? 0.f : 1.f / l;
+  };
+  auto scaled = [](const float4 v, const float f) { return make_float4(v.x * f, v.y * f, v.z * f, v.w * f); };
+  // a lane's values in chunks of four coordinates
+  auto chunk = [&](const int t, const int x) {
+    const int o = 4 * (x / 4), i = x % 4;
+    return make_float4(acc[t][o][i], acc[t][o + 1][i], acc[t][o + 2][i], acc[t][o + 3][i]);
+  };
+  auto chunk_coord = [&](const int x) { return out_coord<D>(4 * (x / 4), x % 4, j); };
+  if constexpr (WT > 1) {  // over the waves, which hold the same rows
+    for (int t = 0; t < NT; ++t) {
+      float *row = s_merge + (wave * 16 * NT + 16 * t + n) * kStride;
+      for (int x = 0; x < kTiles; ++x) *reinterpret_cast<float4 *>(row + chunk_coord(x)) = chunk(t, x);
       if (j == 0) s_ref[wave][16 * t + n] = ref[t], s_sum[wave][16 * t + n] = sum[t];
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) {
-      if (w == wave)
-        for (int t = 0; t < NT; ++t) {
-          float most = kNone;
-          for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][16 * t + n]);
-          const float f = ref[t] == kNone ? 0.f : exp2_raw(ref[t] - most);
-          for (int o = 0; o < kTiles; ++o)
-            for (int i = 0; i < 4; ++i) {
-              float &dst = s_out[(16 * t + n) * kStride + out_coord<D>(o, i, j)];
-              const float v = ref[t] == kNone ? 0.f : acc[t][o][i] * f;
-              dst = w == 0 ? v : dst + v;
-            }
-        }
-      __syncthreads();
     }
-    for (int x = threadIdx.x; x < 16 * NT * (D / 4); x += kThreads) {
+    __syncthreads();
+    for (int x = threadIdx.x; x < rows_here * (D / 4); x += kThreads) {
       const int r = x / (D / 4), c = 4 * (x % (D / 4));
-      const int row = wg_row0 + r;
-      if (row >= rows_valid) continue;
       float most = kNone, l = 0.f;
       for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][r]);
-      for (int u = 0; u < kWaves; ++u)
-        if (s_ref[u][r] != kNone) l += s_sum[u][r] * exp2_raw(s_ref[u][r] - most);
-      const float4 v = *reinterpret_cast<const float4 *>(&s_out[r * kStride + c]);
-      const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
-      if (a.n_split > 1) {
-        float *p = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * kRows * (D + 2);
-        *reinterpret_cast<float4 *>(p + r * D + c) = v;
-        if (c == 0) p[kRows * D + 2 * r] = most, p[kRows * D + 2 * r + 1] = l;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int u = 0; u < kWaves; ++u) {
+        if (s_ref[u][r] == kNone) continue;
+        const float f = exp2_raw(s_ref[u][r] - most);
+        const float4 y = *reinterpret_cast<const float4 *>(s_merge + (u * 16 * NT + r) * kStride + c);
+        l += f * s_sum[u][r];
+        v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+      }
+      if (part) {
+        publish4(part + r * D + c, v);
+        if (c == 0) publish2(part + kRows * D + 2 * r, most, l);
       } else {
-        if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - most);
-        const float f = most == kNone ? 0.f : 1.f / l;
-        const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D + c;
-        const float o[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
-        for (int e = 0; e < 4; ++e) {
-          if (a.q_bf16) static_cast<__bf16 *>(a.out)[at + e] = static_cast<__bf16>(most == kNone ? 0.f : o[e]);
-          else static_cast<float *>(a.out)[at + e] = most == kNone ? 0.f : o[e];
-        }
+        store_out(a, out_at(r) + c, scaled(v, inverse(r, most, l)));
       }
     }
   } else {
     for (int t = 0; t < NT; ++t) {
-      const int row = row0 + 16 * t + n;
-      if (row >= rows_valid) continue;
-      const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
-      if (a.n_split > 1) {
-        const int r = row - wg_row0;
-        float *p = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * kRows * (D + 2);
-        for (int o = 0; o < kTiles; ++o)
-          for (int e = 0; e < 4; ++e) p[r * D + out_coord<D>(o, e, j)] = ref[t] == kNone ? 0.f : acc[t][o][e];
-        if (j == 0) p[kRows * D + 2 * r] = ref[t], p[kRows * D + 2 * r + 1] = sum[t];
-      } else {
-        float l = sum[t];
-        if (a.sinks && ref[t] != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - ref[t]);
-        const float f = 1.f / l;
-        const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D;
-        for (int o = 0; o < kTiles; ++o)
-          for (int e = 0; e < 4; ++e) {
-            const float v = ref[t] == kNone ? 0.f : acc[t][o][e] * f;
-            const size_t to = at + out_coord<D>(o, e, j);
-            if (a.q_bf16) static_cast<__bf16 *>(a.out)[to] = static_cast<__bf16>(v);
-            else static_cast<float *>(a.out)[to] = v;
-          }
+      const int r = row0 + 16 * t + n - wg_row0;
+      if (r >= rows_here) continue;
+      const float f = part ? 1.f : inverse(r, ref[t], sum[t]);
+      for (int x = 0; x < kTiles; ++x) {
+        if (part) publish4(part + r * D + chunk_coord(x), chunk(t, x));
+        else store_out(a, out_at(r) + chunk_coord(x), scaled(chunk(t, x), f));
       }
+      if (part && j == 0) publish2(part + kRows * D + 2 * r, ref[t], sum[t]);
     }
   }
-}
+  if (!part) return;
 
-// The splits' partials of a row, one workgroup of D threads per row.
-template <int D>
-__global__ __launch_bounds__(D) void q4_combine_kernel(const Q4AttnArgs a, const int tile_rows) {
-  const int r = blockIdx.x % tile_rows;
-  int wg = blockIdx.x / tile_rows;
-  const int tile = wg % a.row_tiles, unit = wg / a.row_tiles;
-  const int b = unit / a.num_kv_heads, kv = unit - b * a.num_kv_heads;
-  const int nb = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
-  const int row = tile * tile_rows + r;
-  if (row >= nb * a.gqa) return;
-  const size_t slot = static_cast<size_t>(tile_rows) * (D + 2);
-  const float *p = a.part + (static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split * slot;
-  const float *ml = p + static_cast<size_t>(tile_rows) * D + 2 * r;
-  float most = kNone;
-  for (int s = 0; s < a.n_split; ++s) most = fmaxf(most, ml[s * slot]);
-  float l = 0.f, v = 0.f;
-  for (int s = 0; s < a.n_split; ++s) {
-    const float m = ml[s * slot];
-    if (m == kNone) continue;
-    const float f = exp2_raw(m - most);
-    l += f * ml[s * slot + 1];
-    v += f * p[s * slot + r * D + threadIdx.x];
+  // Over the splits: the last one to arrive merges them, in their order.
+  __builtin_amdgcn_s_waitcnt(0);  // this thread's words have landed
+  __syncthreads();
+  int *counter = a.counters + static_cast<size_t>(unit) * a.row_tiles + tile;
+  if (threadIdx.x == 0)
+    s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.n_split - 1;
+  __syncthreads();
+  if (!s_last) return;
+  if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const float *parts = part - split * slot;
+  float2 *weight = reinterpret_cast<float2 *>(s_merge);
+  for (int r = threadIdx.x / 16; r < rows_here; r += kThreads / 16) {  // 16 lanes a row
+    float most = kNone, l = 0.f;
+    for (int x = n; x < a.n_split; x += 16) {
+      const float2 ml = fetch2(parts + x * slot + kRows * D + 2 * r);
+      weight[r * a.n_split + x] = ml;
+      most = fmaxf(most, ml.x);
+    }
+    most = fmaxf(most, lut::row_ror<1>(most));
+    most = fmaxf(most, lut::row_ror<2>(most));
+    most = fmaxf(most, lut::row_ror<4>(most));
+    most = fmaxf(most, lut::row_ror<8>(most));
+    for (int x = n; x < a.n_split; x += 16) {
+      const float2 ml = weight[r * a.n_split + x];
+      const float f = ml.x == kNone ? 0.f : exp2_raw(ml.x - most);
+      l += f == 0.f ? 0.f : f * ml.y;
+      weight[r * a.n_split + x].x = f;
+    }
+    l += lut::row_ror<1>(l);
+    l += lut::row_ror<2>(l);
+    l += lut::row_ror<4>(l);
+    l += lut::row_ror<8>(l);
+    if (n == 0) s_inv[r] = inverse(r, most, l);
   }
-  const int i = row / a.gqa, head = kv * a.gqa + row - i * a.gqa;
-  if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head] * 1.44269504088896341f - most);
-  v = most == kNone ? 0.f : v / l;
-  const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + head) * D + threadIdx.x;
-  if (a.q_bf16) static_cast<__bf16 *>(a.out)[at] = static_cast<__bf16>(v);
-  else static_cast<float *>(a.out)[at] = v;
+  __syncthreads();
+  // the threads in groups that share the splits where there are fewer chunks than threads
+  const int items = rows_here * (D / 4);
+  const int groups = min(8, max(1, kThreads / items));
+  const int group = threadIdx.x / items;
+  float4 *sums = reinterpret_cast<float4 *>(weight + rows_here * a.n_split + (rows_here * a.n_split & 1));
+  for (int x = groups > 1 ? static_cast<int>(threadIdx.x) % items : threadIdx.x; x < items && group < groups; x += kThreads) {
+    const int r = x / (D / 4), c = 4 * (x % (D / 4));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int u = groups > 1 ? group : 0; u < a.n_split; u += groups) {
+      const float f = weight[r * a.n_split + u].x;
+      const float2 y = fetch2(parts + u * slot + r * D + c), z = fetch2(parts + u * slot + r * D + c + 2);
+      if (f != 0.f) v.x += f * y.x, v.y += f * y.y, v.z += f * z.x, v.w += f * z.y;
+    }
+    if (groups > 1) {
+      sums[group * items + x] = v;
+      break;
+    }
+    store_out(a, out_at(r) + c, scaled(v, s_inv[r]));
+  }
+  if (groups > 1) {
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < items) {
+      const int r = threadIdx.x / (D / 4), c = 4 * (threadIdx.x % (D / 4));
+      float4 v = sums[threadIdx.x];
+      for (int g = 1; g < groups; ++g) {
+        const float4 y = sums[g * items + threadIdx.x];
+        v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+      }
+      store_out(a, out_at(r) + c, scaled(v, s_inv[r]));
+    }
+  }
 }
 
 }  // namespace
@@ -488,11 +551,11 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
   p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
   const long long tiles = static_cast<long long>(batch) * num_kv_heads * p.row_tiles;
   const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
-  const long long want = std::max<long long>(1, 512 / tiles), most = std::max<long long>(1, (span + 255) / 256);
-  p.n_split = static_cast<int>(std::min(want, most));
+  const long long want = std::max<long long>(1, kTargetGroups / tiles), most = std::max<long long>(1, (span + 255) / 256);
+  p.n_split = static_cast<int>(std::min({want, most, p.tile_rows == 128 ? kMaxSplitsTiled * 1LL : kMaxSplits * 1LL}));
   auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
-  if (p.n_split > 1) {
-    p.off_part = up(static_cast<size_t>(tiles) * sizeof(int));
+  if (p.n_split > 1) {  // at most kMaxCounters tiles; the counters of all shapes lie at the workspace's start
+    p.off_part = kMaxCounters * sizeof(int);
     p.total = p.off_part + up(static_cast<size_t>(tiles) * p.n_split * p.tile_rows * (head_dim + 2) * sizeof(float));
   }
   return p;
@@ -504,9 +567,6 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream
     // blocks of a multiple of 16 rows: a round needs two addresses instead of ten a lane
     if (a.layout.block_size % 16 == 0) q4_attn_kernel<d(), wide(), nt(), wt(), true><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
     else q4_attn_kernel<d(), wide(), nt(), wt(), false><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.n_split == 1) return e;
-    q4_combine_kernel<d()><<<tiles * plan.tile_rows, d(), 0, stream>>>(a, plan.tile_rows);
     return hipGetLastError();
   };
   auto by_rows = [&](auto d, auto wide) {
