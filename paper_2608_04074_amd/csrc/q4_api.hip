@@ -138,7 +138,7 @@ size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t ba
   if (!cache || batch <= 0 || n_q <= 0 || num_q_heads <= 0 || max_seq_len <= 0 || cache->num_kv_heads <= 0 ||
       cache->head_dim <= 0 || num_q_heads % cache->num_kv_heads != 0)
     return 0;
-  return novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim, max_seq_len, 0).total;
+  return novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim, 1, max_seq_len, 0).total;
 }
 
 nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nova_kv_dtype q_dtype, int32_t batch,
@@ -170,12 +170,12 @@ nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nov
     if (rows > (1 << 24) || static_cast<long long>(batch) * cache->num_kv_heads * ((rows + 15) / 16) > (1 << 23))
       return fail(NOVA_KV_ERR_UNSUPPORTED, "too many query rows in a call");
     const novakv::Q4AttnPlan plan = novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim,
-                                                         max_seq_len, window);
+                                                         q_dtype == NOVA_KV_BF16, max_seq_len, window);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if ((st = novakv::debug_check(&cache->layout, batch, seq_lens, max_seq_len, nullptr, 0, stream, nullptr,
                                   cache->num_blocks)) != NOVA_KV_OK)
       return st;
-    if (plan.total > 0) {
+    if (plan.n_split > 1) {
       if (!workspace || workspace_bytes < plan.total)
         return fail(NOVA_KV_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", plan.total,
                     workspace ? workspace_bytes : static_cast<size_t>(0));
@@ -207,8 +207,8 @@ nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nov
     a.n_split = plan.n_split;
     a.row_tiles = plan.row_tiles;
     char *ws = static_cast<char *>(workspace);
-    a.counters = plan.total > 0 ? reinterpret_cast<int *>(ws) : nullptr;
-    a.part = plan.total > 0 ? reinterpret_cast<float *>(ws + plan.off_part) : nullptr;
+    a.counters = plan.n_split > 1 ? reinterpret_cast<int *>(ws) : nullptr;
+    a.part = plan.n_split > 1 ? reinterpret_cast<float *>(ws + plan.off_part) : nullptr;
     const hipError_t e = novakv::launch_q4_attn(a, plan, stream);
     if (e != hipSuccess) return fail(NOVA_KV_ERR_HIP, "4-bit attention launch: %s", hipGetErrorString(e));
     return ok();

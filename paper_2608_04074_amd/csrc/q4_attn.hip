@@ -10,12 +10,11 @@
 // of two digits of 7 bits (three for fp32 queries) of its row's largest
 // magnitude.
 //
-// Values: on the fp16 cores, as c - 8: a nibble masked in place under the bits of
-// 1024 is the fp16 number 1024 + c (1024 + 16 c, its bits four higher), from which a
-// packed subtraction leaves c - 8 (16 (c - 8)) exactly. (The nibble alone would be
-// a denormal that the cores multiply exactly too, but they align it with the sum
-// so far by its exponent field, ten bits above its value, and cut those bits off
-// the sum: 1e-5 of an output, towards one side.)
+// Values: on the fp16 cores, as (c - 8) * 2^-9: a nibble masked in place is the fp16
+// denormal c * 2^-24 (c * 2^-20, its bits four higher), which one packed multiply-add
+// scales and centres exactly. (The cores multiply the denormal itself exactly
+// too, but align it with the sum so far by its exponent field, ten bits above its
+// value, and cut those bits off the sum: 1e-5 of an output, towards one side.)
 #include <algorithm>
 #include <type_traits>
 
@@ -33,7 +32,6 @@ using lut::half8_t;
 using lut::max_rows16;
 using lut::max_rows32;
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRound = 32;    // tokens a wave takes at a time
 // The fp16 cores add the products of eight slots after cutting them about 24 bits
 // below the largest, then round to nearest (measured). A sum of small multiples of
@@ -43,22 +41,21 @@ constexpr int kRound = 32;    // tokens a wave takes at a time
 constexpr float kNone = -__builtin_inff();
 // Most splits of a tile's span: their weights lie in LDS (16 or 32 rows, 128 rows).
 constexpr int kMaxSplits = 96, kMaxSplitsTiled = 32;
-// Arrival counters of a workspace: a span is split only where fewer tiles than
-// that run, so no call's partials lie on another shape's counters.
-constexpr int kTargetGroups = 512, kMaxCounters = 1024;
-static_assert(kTargetGroups <= kMaxCounters, "a split launch has at most kTargetGroups / 2 tiles");
+// Arrival counters of a workspace: a span is split only where at most this many
+// workgroups run, so no call's partials lie on another shape's counters.
+constexpr int kMaxCounters = 1024;
 
 __device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdgcn_exp2f(x); }
 
 typedef int int4_t __attribute__((ext_vector_type(4)));
 
-// Codes k and k + 4 of a word less 8, as two fp16 numbers in a word (times 16 for odd k).
+// Codes k and k + 4 of a word as (c - 8) * 2^-9, two fp16 numbers in a word.
 template <int K>
 __device__ __forceinline__ uint32_t value_pair(const uint32_t w) {
-  const uint32_t x = K < 2 ? w : w >> 8;
-  const uint32_t pair = (x & (K % 2 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
-  const lut::half2_t bias = __builtin_bit_cast(lut::half2_t, K % 2 ? 0x64806480u : 0x64086408u);
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(lut::half2_t, pair) - bias);
+  const uint32_t x = (K < 2 ? w : w >> 8) & (K % 2 ? 0x00f000f0u : 0x000f000fu);
+  const _Float16 up = K % 2 ? 0x1p11f : 0x1p15f, centre = -0x1p-6f;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(lut::half2_t, x), lut::half2_t{up, up},
+                                                                lut::half2_t{centre, centre}));
 }
 
 // Coordinate of a lane's output value: tile t, accumulator register i, lane row j.
@@ -96,8 +93,12 @@ __device__ __forceinline__ void store_out(const Q4AttnArgs &a, const size_t at, 
   }
 }
 
-template <int D, bool WIDE, int NT, int WT, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
+// D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows a wave. W: waves of a
+// workgroup. TILED: each wave has rows of its own and all tokens, else the waves
+// share the rows and divide the tokens. ALIGNED: blocks of a multiple of 16 rows.
+template <int D, bool WIDE, int NT, int W, bool TILED, bool ALIGNED>
+__global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ? 2 : 3) void q4_attn_kernel(const Q4AttnArgs a) {
+  constexpr int kWaves = W, kThreads = 64 * W, WT = TILED ? 1 : W;
   constexpr int kSteps = D / 64;          // matrix steps of a score
   constexpr int kTiles = D / 16;          // output tiles
   constexpr int kKeyWords = D / 32;       // words of a lane's part of a key row
@@ -151,69 +152,6 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   const int row1 = min(row0 + 16 * NT, rows_valid);
   const bool idle = row0 >= rows_valid;
   const int inner_lo = idle ? 0 : first_pos(row1 - 1), inner_hi = idle ? 0 : last_pos(row0) + 1;
-
-  int4_t qf[NT][kDigits][kSteps];
-  float alpha[NT], qsum[NT], ref[NT], sum[NT], off_sum[NT];
-  int row_lo[NT], row_hi[NT];
-  float4_t acc[NT][kTiles];
-  for (int t = 0; t < NT; ++t) {
-    const int row = row0 + 16 * t + n;
-    const bool on = row < rows_valid;
-    const int i = row / a.gqa, g = row - i * a.gqa;
-    row_hi[t] = on ? last_pos(row) + 1 : 0;
-    row_lo[t] = on ? first_pos(row) : 0;
-    float x[kKeyWords][8];
-    float top = 0.f;
-    bool finite = true;
-    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + g) * D + 8 * kKeyWords * j;
-    for (int s = 0; s < kKeyWords; ++s) {
-      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-      if (on) {
-        if constexpr (!WIDE) {
-          const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 8 * s);
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-          for (int e = 0; e < 4; ++e) {
-            x[s][2 * e] = __uint_as_float(u[e] << 16);
-            x[s][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-          }
-        } else {
-          const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 8 * s);
-          const float4 u = f[0], v = f[1];
-          x[s][0] = u.x, x[s][1] = u.y, x[s][2] = u.z, x[s][3] = u.w;
-          x[s][4] = v.x, x[s][5] = v.y, x[s][6] = v.z, x[s][7] = v.w;
-        }
-      }
-      for (int e = 0; e < 8; ++e) {
-        finite = finite && fabsf(x[s][e]) < __builtin_inff();
-        top = fmaxf(top, fabsf(x[s][e]));
-      }
-    }
-    top = max_rows32(max_rows16(finite ? top : __builtin_inff()));
-    const bool usable = top < __builtin_inff();
-    const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
-    int total = 0;
-    for (int s = 0; s < kSteps; ++s)
-      for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
-    for (int s = 0; s < kKeyWords; ++s) {
-      for (int e = 0; e < 8; ++e) {
-        int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
-        total += f;
-        // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
-        for (int d = 0; d < kDigits; ++d) {
-          const int digit = d == kDigits - 1 ? f : ((f + 64) & 127) - 64;
-          f = (f - digit) >> 7;
-          qf[t][d][s / 2][2 * (s % 2) + e % 2] |= (digit & 255) << (8 * (e / 2));
-        }
-      }
-    }
-    total += __shfl_xor(total, 16);
-    total += __shfl_xor(total, 32);
-    qsum[t] = static_cast<float>(total);
-    alpha[t] = usable ? a.qscale / to_fixed : __builtin_nanf("");  // a row that is not finite: NaN outputs
-    ref[t] = kNone;
-    sum[t] = off_sum[t] = 0.f;
-    for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
-  }
 
   // Rounds of 32 tokens, the codes, scales and offsets of one requested while
   // the round before is computed, its block-table entries one round earlier.
@@ -288,12 +226,77 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   };
 
   Round cur, next;
-  if (!idle && t0 + kRound * tw < t1) {
+  const bool any = !idle && t0 + kRound * tw < t1;
+  if (any) {
     look_up();
     request(cur);
     look_up();
   }
-  for (int tb = t0 + kRound * tw; tb < t1 && !idle; tb += kStep) {
+
+  int4_t qf[NT][kDigits][kSteps];
+  float alpha[NT], qsum[NT], ref[NT], sum[NT], off_sum[NT];
+  int row_lo[NT], row_hi[NT];
+  float4_t acc[NT][kTiles];
+  for (int t = 0; t < NT; ++t) {
+    const int row = row0 + 16 * t + n;
+    const bool on = row < rows_valid;
+    const int i = row / a.gqa, g = row - i * a.gqa;
+    row_hi[t] = on ? last_pos(row) + 1 : 0;
+    row_lo[t] = on ? first_pos(row) : 0;
+    float x[kKeyWords][8];
+    float top = 0.f;
+    bool finite = true;
+    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + g) * D + 8 * kKeyWords * j;
+    for (int s = 0; s < kKeyWords; ++s) {
+      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+      if (on) {
+        if constexpr (!WIDE) {
+          const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 8 * s);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+          for (int e = 0; e < 4; ++e) {
+            x[s][2 * e] = __uint_as_float(u[e] << 16);
+            x[s][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+          }
+        } else {
+          const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 8 * s);
+          const float4 u = f[0], v = f[1];
+          x[s][0] = u.x, x[s][1] = u.y, x[s][2] = u.z, x[s][3] = u.w;
+          x[s][4] = v.x, x[s][5] = v.y, x[s][6] = v.z, x[s][7] = v.w;
+        }
+      }
+      for (int e = 0; e < 8; ++e) {
+        finite = finite && fabsf(x[s][e]) < __builtin_inff();
+        top = fmaxf(top, fabsf(x[s][e]));
+      }
+    }
+    top = max_rows32(max_rows16(finite ? top : __builtin_inff()));
+    const bool usable = top < __builtin_inff();
+    const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
+    int total = 0;
+    for (int s = 0; s < kSteps; ++s)
+      for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
+    for (int s = 0; s < kKeyWords; ++s) {
+      for (int e = 0; e < 8; ++e) {
+        int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
+        total += f;
+        // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
+        for (int d = 0; d < kDigits; ++d) {
+          const int digit = d == kDigits - 1 ? f : ((f + 64) & 127) - 64;
+          f = (f - digit) >> 7;
+          qf[t][d][s / 2][2 * (s % 2) + e % 2] |= (digit & 255) << (8 * (e / 2));
+        }
+      }
+    }
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    qsum[t] = static_cast<float>(total);
+    alpha[t] = usable ? a.qscale / to_fixed : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    ref[t] = kNone;
+    sum[t] = off_sum[t] = 0.f;
+    for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int tb = t0 + kRound * tw; any && tb < t1; tb += kStep) {
     request(next);  // past the last round: rows at the pool's start or of a block's end, masked
     look_up();
 
@@ -336,21 +339,25 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
           d[h][x] = int4_t{0, 0, 0, 0};
           for (int s = 0; s < kSteps; ++s) d[h][x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[h][x], 0, 0, 0);
         }
-      float z[8], top = kNone;
-      uint32_t masked = 0;
+      float z[8], top = kNone, scale[8], offset[8];
       for (int e = 0; e < 8; ++e) {
         const int4_t(&dig)[kDigits] = d[e >> 2];
         float dot = static_cast<float>((dig[1][e & 3] << 7) + dig[0][e & 3]);
         if constexpr (WIDE) dot = __builtin_fmaf(16384.f, static_cast<float>(dig[2][e & 3]), dot);
         z[e] = ks[e] * dot + ko[e] * qsum[t];
-        if (!inner) {
+        scale[e] = vs[e];
+        offset[e] = vo8[e];
+      }
+      if (!inner) {
+        for (int e = 0; e < 8; ++e) {
           const int m = 16 * (e >> 2) + 4 * j + (e & 3);
           const bool seen = ((valid >> m) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
-          if (!seen) masked |= 1u << e;
           z[e] = seen ? z[e] : kNone;
+          scale[e] = seen ? scale[e] : 0.f;  // whatever a hidden token's scale and offset are
+          offset[e] = seen ? offset[e] : 0.f;
         }
-        top = fmaxf(top, z[e]);
       }
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, z[e]);
       const float bound = top * alpha[t] + log_vs;
       if (__any(bound > ref[t] + (kTop + kSlack))) {
         const float most = max_rows32(max_rows16(bound));
@@ -364,10 +371,9 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
       const float r = ref[t] == kNone ? 0.f : ref[t];
       for (int e = 0; e < 8; ++e) {
         const float p = exp2_raw(__builtin_fmaf(z[e], alpha[t], -r));
-        float ps = p * vs[e], po = p * vo8[e];
-        if (!inner && ((masked >> e) & 1u)) ps = po = 0.f;  // whatever a hidden token's scale and offset are
+        const float ps = p * scale[e];
         sum[t] += p;
-        off_sum[t] += po;
+        off_sum[t] += p * offset[e];
         if constexpr (WIDE) {  // units of 1, units of 2^-11, what is left
           const float high = rintf(ps), rest = ps - high, mid = rintf(rest * 0x1p11f) * 0x1p-11f;
           pf[t][0][e] = static_cast<_Float16>(high);
@@ -379,24 +385,25 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
       }
     }
 
-    // the same coordinate's codes of two tokens in one word
-    uint32_t vo[kTiles][4];
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t w0 = cur.vw[2 * e], w1 = cur.vw[2 * e + 1];
-      if constexpr (D == 128) {
-        const uint32_t low = __builtin_amdgcn_perm(w1, w0, 0x05040100u), high = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
-        vo[0][e] = value_pair<0>(low), vo[1][e] = value_pair<1>(low), vo[2][e] = value_pair<2>(low), vo[3][e] = value_pair<3>(low);
-        vo[4][e] = value_pair<0>(high), vo[5][e] = value_pair<1>(high), vo[6][e] = value_pair<2>(high), vo[7][e] = value_pair<3>(high);
-      } else {  // lanes 0..7 of a row take a word's low four nibbles, lanes 8..15 its high ones
-        const uint32_t half = __builtin_amdgcn_perm(w1, w0, n < 8 ? 0x05040100u : 0x07060302u);
-        vo[0][e] = value_pair<0>(half), vo[1][e] = value_pair<1>(half), vo[2][e] = value_pair<2>(half), vo[3][e] = value_pair<3>(half);
-      }
-    }
-    for (int o = 0; o < kTiles; ++o) {
-      const half8_t c = __builtin_bit_cast(half8_t, make_uint4(vo[o][0], vo[o][1], vo[o][2], vo[o][3]));
+    __builtin_amdgcn_sched_barrier(0);  // the codes of values stay packed until here
+    // The same coordinate's codes of two tokens in one word: the low half of the
+    // tokens' words, then the high one (head_dim 64: lanes 0..7 of a row take the
+    // low one, lanes 8..15 the high one).
+    auto values = [&](auto k, const int o, const uint32_t *pair) {
+      const half8_t c = __builtin_bit_cast(half8_t, make_uint4(value_pair<k()>(pair[0]), value_pair<k()>(pair[1]),
+                                                               value_pair<k()>(pair[2]), value_pair<k()>(pair[3])));
       for (int t = 0; t < NT; ++t)
         for (int x = 0; x < kProbParts; ++x)
           acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, pf[t][x], acc[t][o], 0, 0, 0);
+    };
+    for (int half = 0; half < D / 64; ++half) {
+      const uint32_t pick = D == 128 ? (half ? 0x07060302u : 0x05040100u) : n < 8 ? 0x05040100u : 0x07060302u;
+      uint32_t pair[4];
+      for (int e = 0; e < 4; ++e) pair[e] = __builtin_amdgcn_perm(cur.vw[2 * e + 1], cur.vw[2 * e], pick);
+      values(std::integral_constant<int, 0>{}, 4 * half, pair);
+      values(std::integral_constant<int, 1>{}, 4 * half + 1, pair);
+      values(std::integral_constant<int, 2>{}, 4 * half + 2, pair);
+      values(std::integral_constant<int, 3>{}, 4 * half + 3, pair);
     }
     cur = next;
   }
@@ -407,7 +414,7 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
     off_sum[t] = add_rows32(add_rows16(off_sum[t]));
     if (sum[t] != sum[t]) ref[t] = fmaxf(ref[t], 0.f);  // NaN logits move no reference, but attend
     for (int o = 0; o < kTiles; ++o)
-      for (int i = 0; i < 4; ++i) acc[t][o][i] = acc[t][o][i] * (o % 2 ? 0.0625f : 1.f) + off_sum[t];
+      for (int i = 0; i < 4; ++i) acc[t][o][i] = acc[t][o][i] * 0x1p9f + off_sum[t];
   }
   const int rows_here = wg_row1 - wg_row0;
   const size_t slot = static_cast<size_t>(kRows) * (D + 2);
@@ -480,13 +487,33 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
   if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const float *parts = part - split * slot;
   float2 *weight = reinterpret_cast<float2 *>(s_merge);
+  // All words are requested before any is used: the statistics, and each
+  // thread's first values (in groups that share the splits where there are fewer
+  // chunks than threads).
+  const int items = rows_here * (D / 4);
+  const int groups = min(8, max(1, kThreads / items));
+  const int group = groups > 1 ? static_cast<int>(threadIdx.x) / items : 0;
+  const int item = groups > 1 ? static_cast<int>(threadIdx.x) % items : static_cast<int>(threadIdx.x);
+  constexpr int kAhead = 8;
+  float4 v[kAhead];
+  auto fetch_values = [&](const int x, const int first) {
+    const float *src = parts + (x / (D / 4)) * D + 4 * (x % (D / 4));
+    for (int y = 0; y < kAhead; ++y) {
+      const int u = min(first + y * groups, a.n_split - 1);
+      const float2 lo2 = fetch2(src + u * slot), hi2 = fetch2(src + u * slot + 2);
+      v[y] = make_float4(lo2.x, lo2.y, hi2.x, hi2.y);
+    }
+  };
+  const bool mine = group < groups && item < items;
+  for (int x = threadIdx.x; x < rows_here * a.n_split; x += kThreads) {
+    const int r = x / a.n_split, u = x - r * a.n_split;
+    weight[x] = fetch2(parts + u * slot + kRows * D + 2 * r);
+  }
+  if (mine) fetch_values(item, group);
+  __syncthreads();
   for (int r = threadIdx.x / 16; r < rows_here; r += kThreads / 16) {  // 16 lanes a row
     float most = kNone, l = 0.f;
-    for (int x = n; x < a.n_split; x += 16) {
-      const float2 ml = fetch2(parts + x * slot + kRows * D + 2 * r);
-      weight[r * a.n_split + x] = ml;
-      most = fmaxf(most, ml.x);
-    }
+    for (int x = n; x < a.n_split; x += 16) most = fmaxf(most, weight[r * a.n_split + x].x);
     most = fmaxf(most, lut::row_ror<1>(most));
     most = fmaxf(most, lut::row_ror<2>(most));
     most = fmaxf(most, lut::row_ror<4>(most));
@@ -504,79 +531,119 @@ __global__ __launch_bounds__(kThreads) void q4_attn_kernel(const Q4AttnArgs a) {
     if (n == 0) s_inv[r] = inverse(r, most, l);
   }
   __syncthreads();
-  // the threads in groups that share the splits where there are fewer chunks than threads
-  const int items = rows_here * (D / 4);
-  const int groups = min(8, max(1, kThreads / items));
-  const int group = threadIdx.x / items;
   float4 *sums = reinterpret_cast<float4 *>(weight + rows_here * a.n_split + (rows_here * a.n_split & 1));
-  for (int x = groups > 1 ? static_cast<int>(threadIdx.x) % items : threadIdx.x; x < items && group < groups; x += kThreads) {
+  for (int x = item; mine && x < items; x += kThreads) {
     const int r = x / (D / 4), c = 4 * (x % (D / 4));
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int u = groups > 1 ? group : 0; u < a.n_split; u += groups) {
-      const float f = weight[r * a.n_split + u].x;
-      const float2 y = fetch2(parts + u * slot + r * D + c), z = fetch2(parts + u * slot + r * D + c + 2);
-      if (f != 0.f) v.x += f * y.x, v.y += f * y.y, v.z += f * z.x, v.w += f * z.y;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int first = group; first < a.n_split; first += kAhead * groups) {
+      if (x != item || first != group) fetch_values(x, first);
+      for (int y = 0; y < kAhead; ++y) {
+        const int u = first + y * groups;
+        const float f = u < a.n_split ? weight[r * a.n_split + u].x : 0.f;
+        if (f != 0.f) o.x += f * v[y].x, o.y += f * v[y].y, o.z += f * v[y].z, o.w += f * v[y].w;
+      }
     }
     if (groups > 1) {
-      sums[group * items + x] = v;
+      sums[group * items + x] = o;
       break;
     }
-    store_out(a, out_at(r) + c, scaled(v, s_inv[r]));
+    store_out(a, out_at(r) + c, scaled(o, s_inv[r]));
   }
   if (groups > 1) {
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < items) {
       const int r = threadIdx.x / (D / 4), c = 4 * (threadIdx.x % (D / 4));
-      float4 v = sums[threadIdx.x];
+      float4 o = sums[threadIdx.x];
       for (int g = 1; g < groups; ++g) {
         const float4 y = sums[g * items + threadIdx.x];
-        v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+        o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
       }
-      store_out(a, out_at(r) + c, scaled(v, s_inv[r]));
+      store_out(a, out_at(r) + c, scaled(o, s_inv[r]));
     }
   }
 }
 
 }  // namespace
 
+namespace {
+
+int most_splits(const int tile_rows, const long long tiles, const long long span) {
+  const long long limit = tile_rows == 128 ? kMaxSplitsTiled : kMaxSplits;
+  return static_cast<int>(std::max<long long>(1, std::min({limit, (span + 127) / 128, kMaxCounters / tiles})));
+}
+
+}  // namespace
+
 // Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the
-// workgroup's waves sharing the tokens; more rows take 128 a workgroup, 32 a
-// wave.  The span is split to reach about two workgroups a CU.
+// workgroup's waves dividing the tokens; more rows take 128 a workgroup, 32 a
+// wave.
 Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads,
-                        const int head_dim, const int max_seq_len, const int window) {
+                        const int head_dim, const int q_bf16, const int max_seq_len, const int window) {
   Q4AttnPlan p{};
   const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
   p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
   p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
   const long long tiles = static_cast<long long>(batch) * num_kv_heads * p.row_tiles;
   const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
-  const long long want = std::max<long long>(1, kTargetGroups / tiles), most = std::max<long long>(1, (span + 255) / 256);
-  p.n_split = static_cast<int>(std::min({want, most, p.tile_rows == 128 ? kMaxSplitsTiled * 1LL : kMaxSplits * 1LL}));
-  auto up = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
-  if (p.n_split > 1) {  // at most kMaxCounters tiles; the counters of all shapes lie at the workspace's start
-    p.off_part = kMaxCounters * sizeof(int);
-    p.total = p.off_part + up(static_cast<size_t>(tiles) * p.n_split * p.tile_rows * (head_dim + 2) * sizeof(float));
+  const bool tiled = p.tile_rows == 128;
+  // A launch in rounds of the workgroups that the CUs hold, each with its setup
+  // and tail beside its tokens; splits add the merge. In ns.
+  auto consider = [&](const int waves, const int per_cu, const int setup, const double token) {
+    const int step = kRound * (tiled ? 1 : waves);
+    for (int n = 1; n <= most_splits(p.tile_rows, tiles, span); ++n) {
+      const long long chunk = ((span + n - 1) / n + step - 1) / step * step;
+      if (n > 1 && chunk * (n - 1) >= span + step) break;
+      const long long rounds = (tiles * n + 256 * per_cu - 1) / (256 * per_cu);
+      // fewer workgroups than CUs: a workgroup has its CU to itself
+      const double share = static_cast<double>(std::min<long long>(per_cu, (tiles * n + 255) / 256));
+      const double cost = rounds * (setup + chunk * token * share) + (n > 1 ? 3500 + 50.0 * n : 0);
+      if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n;
+    }
+  };
+  if (tiled) {
+    consider(4, 1, 8000, 40);
+  } else {
+    consider(4, p.tile_rows == 16 ? 3 : 2, 6000, 9);
+    consider(p.tile_rows == 16 && q_bf16 ? 12 : 8, 1, 6500, 6.6);
+  }
+  // the counters of all shapes lie at the workspace's start; its size covers
+  // every window and type
+  const int most = most_splits(p.tile_rows, tiles, max_seq_len);
+  p.off_part = kMaxCounters * sizeof(int);
+  if (most > 1) {
+    const size_t part = static_cast<size_t>(tiles) * most * p.tile_rows * (head_dim + 2) * sizeof(float);
+    p.total = p.off_part + ((part + 255) & ~static_cast<size_t>(255));
   }
   return p;
 }
 
 hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
   const unsigned tiles = static_cast<unsigned>(a.batch) * a.num_kv_heads * a.row_tiles;
-  auto go = [&](auto d, auto wide, auto nt, auto wt) {
+  auto go = [&](auto d, auto wide, auto nt, auto w, auto tiled) {
     // blocks of a multiple of 16 rows: a round needs two addresses instead of ten a lane
-    if (a.layout.block_size % 16 == 0) q4_attn_kernel<d(), wide(), nt(), wt(), true><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
-    else q4_attn_kernel<d(), wide(), nt(), wt(), false><<<tiles * a.n_split, kThreads, 0, stream>>>(a);
+    if (a.layout.block_size % 16 == 0)
+      q4_attn_kernel<d(), wide(), nt(), w(), tiled(), true><<<tiles * a.n_split, 64 * w(), 0, stream>>>(a);
+    else
+      q4_attn_kernel<d(), wide(), nt(), w(), tiled(), false><<<tiles * a.n_split, 64 * w(), 0, stream>>>(a);
     return hipGetLastError();
   };
+  using std::false_type;
+  using std::integral_constant;
+  using std::true_type;
+  constexpr integral_constant<int, 1> one{};
+  constexpr integral_constant<int, 2> two{};
+  constexpr integral_constant<int, 4> w4{};
+  constexpr integral_constant<int, 8> w8{};
+  constexpr integral_constant<int, 12> w12{};
   auto by_rows = [&](auto d, auto wide) {
-    using std::integral_constant;
-    if (plan.tile_rows == 16) return go(d, wide, integral_constant<int, 1>{}, integral_constant<int, 4>{});
-    if (plan.tile_rows == 32) return go(d, wide, integral_constant<int, 2>{}, integral_constant<int, 4>{});
-    return go(d, wide, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+    if (plan.tile_rows == 128) return go(d, wide, two, w4, true_type{});
+    if (plan.tile_rows == 32) return plan.waves == 4 ? go(d, wide, two, w4, false_type{}) : go(d, wide, two, w8, false_type{});
+    if (plan.waves == 4) return go(d, wide, one, w4, false_type{});
+    if constexpr (wide()) return go(d, wide, one, w8, false_type{});
+    else return go(d, wide, one, w12, false_type{});
   };
-  auto by_type = [&](auto d) { return a.q_bf16 ? by_rows(d, std::false_type{}) : by_rows(d, std::true_type{}); };
-  return a.head_dim == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
+  auto by_type = [&](auto d) { return a.q_bf16 ? by_rows(d, false_type{}) : by_rows(d, true_type{}); };
+  return a.head_dim == 128 ? by_type(integral_constant<int, 128>{}) : by_type(integral_constant<int, 64>{});
 }
 
 }  // namespace novakv

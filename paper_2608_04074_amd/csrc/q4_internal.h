@@ -55,10 +55,12 @@ struct Q4AttnArgs {
 // head) in tiles of tile_rows, each tile's span in n_split splits.
 struct Q4AttnPlan {
   int tile_rows, row_tiles, n_split;
-  size_t off_part, total;  // workspace: arrival counters, then the split partials; total 0 when n_split is 1
+  int waves;    // of a workgroup
+  double cost;  // estimated time, ns
+  size_t off_part, total;  // workspace: arrival counters, then the split partials (needed when n_split > 1)
 };
-Q4AttnPlan plan_q4_attn(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int max_seq_len,
-                        int window);
+Q4AttnPlan plan_q4_attn(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int q_bf16,
+                        int max_seq_len, int window);
 hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream);
 
 }  // namespace novakv
