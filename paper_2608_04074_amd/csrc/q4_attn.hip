@@ -16,6 +16,7 @@
 // too, but align it with the sum so far by its exponent field, ten bits above its
 // value, and cut those bits off the sum: 1e-5 of an output, towards one side.)
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "lut_common.h"
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const int tw = wave % WT, rw = wave / WT;
 
-  int wg = blockIdx.x;
+  int wg = lut::xcd_contiguous(blockIdx.x, gridDim.x);
   const int split = wg % a.n_split;
   wg /= a.n_split;
   const int tile = wg % a.row_tiles;
@@ -586,25 +587,37 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
   const long long tiles = static_cast<long long>(batch) * num_kv_heads * p.row_tiles;
   const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
   const bool tiled = p.tile_rows == 128;
-  // A launch in rounds of the workgroups that the CUs hold, each with its setup
-  // and tail beside its tokens; splits add the merge. In ns.
-  auto consider = [&](const int waves, const int per_cu, const int setup, const double token) {
-    const int step = kRound * (tiled ? 1 : waves);
+  // A launch takes rounds of the workgroups that the CUs hold, each its setup
+  // and tail beside its tokens; splits add the merge, by rows. Fitted to sweeps
+  // over both (8 KV heads of 128, bf16, us): one sequence of 128K tokens 36.2 in
+  // 32 splits of 12 waves, 38.6 in 64 of 4 waves, 46.2 in 32 of 4; of 2000 tokens
+  // 15.2 in 3 of 12, 10.4 in 16 of 4; 32 x 8192 55.6 whole by 12 waves, 57.2 in 3 of
+  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12.
+  const double size = head_dim == 128 ? 1.0 : 0.75;
+  const double row_ns = static_cast<double>(std::min<long long>(rows, p.tile_rows));
+  // token[k - 1]: ns of a CU for a token where k workgroups share it
+  auto consider = [&](const int waves, const int setup, const std::initializer_list<double> token, const double merge) {
+    const int step = kRound * (tiled ? 1 : waves), per_cu = static_cast<int>(token.size());
     for (int n = 1; n <= most_splits(p.tile_rows, tiles, span); ++n) {
       const long long chunk = ((span + n - 1) / n + step - 1) / step * step;
-      if (n > 1 && chunk * (n - 1) >= span + step) break;
-      const long long rounds = (tiles * n + 256 * per_cu - 1) / (256 * per_cu);
-      // fewer workgroups than CUs: a workgroup has its CU to itself
-      const double share = static_cast<double>(std::min<long long>(per_cu, (tiles * n + 255) / 256));
-      const double cost = rounds * (setup + chunk * token * share) + (n > 1 ? 3500 + 50.0 * n : 0);
+      const long long groups = tiles * n, rounds = (groups + 256 * per_cu - 1) / (256 * per_cu);
+      const int share = static_cast<int>(std::min<long long>(per_cu, (groups + 255) / 256));
+      const double each = chunk * size * token.begin()[share - 1] * share;
+      const double cost = rounds * (setup + each) + (n > 1 ? 3500 + merge * row_ns * n : 0);
       if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n;
     }
   };
   if (tiled) {
-    consider(4, 1, 8000, 40);
+    consider(4, 8000, {40}, 10);
+  } else if (p.tile_rows == 32) {
+    consider(4, 10000, {13}, 10);
+    consider(8, 10000, {8.5}, 10);
+  } else if (q_bf16) {
+    consider(4, 6500, {9, 6.2, 5.7}, 10);
+    consider(12, 7000, {5.8}, 5);
   } else {
-    consider(4, p.tile_rows == 16 ? 3 : 2, 6000, 9);
-    consider(p.tile_rows == 16 && q_bf16 ? 12 : 8, 1, 6500, 6.6);
+    consider(4, 6500, {9.9, 8}, 10);
+    consider(8, 7000, {7.5}, 5);
   }
   // the counters of all shapes lie at the workspace's start; its size covers
   // every window and type
