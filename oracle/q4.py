@@ -67,8 +67,9 @@ def unpack_codes(packed):
 def attend(q, kc, ksq, vc, vsq, pos, window=0, sinks=None, scale=None):
     """One KV head of one sequence: q [m][G][D] at positions pos [m] over codes kc, vc [S][D]
     and (scale, offset) values ksq, vsq [S][2] -> (out [m][G][D], and what a bound of the error is
-    made of: sum_j p_j s_j c_j, the largest sum of a logit's magnitudes, max |q_i| times the
-    largest norm of a key times the scale, the largest magnitude of a value's parts)."""
+    made of: sum_j p_j s_j c_j; the largest sum of a logit's magnitudes; max |q_i| times the
+    largest norm of a key times the scale; the norm of q, and |sum q|, times the largest
+    magnitude of a key's parts and the scale; the largest magnitude of a value's parts)."""
     q = np.asarray(q, dtype=np.float64)
     m, G, D = q.shape
     S = kc.shape[0]
@@ -76,7 +77,7 @@ def attend(q, kc, ksq, vc, vsq, pos, window=0, sinks=None, scale=None):
     j = np.arange(S)
     seen = (j <= pos[:, None]) & ((window == 0) | (j > pos[:, None] - window))
     out, coded = np.zeros_like(q), np.zeros_like(q)
-    mags, norms = np.zeros((m, G)), np.zeros((m, G))
+    mags, norms, key_mags, key_sums = (np.zeros((m, G)) for _ in range(4))
     vmax = np.zeros(m)
     for i in range(m):
         at = np.flatnonzero(seen[i])
@@ -86,6 +87,8 @@ def attend(q, kc, ksq, vc, vsq, pos, window=0, sinks=None, scale=None):
         z = (q[i] @ (ko[:, None] + ks[:, None] * c).T) * scale                     # [G][n]
         mags[i] = (np.abs(q[i]) @ (np.abs(ko)[:, None] + ks[:, None] * c).T).max(1) * scale
         norms[i] = np.abs(q[i]).max(-1) * np.linalg.norm(ko[:, None] + ks[:, None] * c, axis=1).max() * scale
+        part = (15 * ks + np.abs(ko)).max() * scale
+        key_mags[i], key_sums[i] = part * np.linalg.norm(q[i], axis=-1), part * np.abs(q[i].sum(-1))
         sink = -np.inf * np.ones(G) if sinks is None else np.asarray(sinks, dtype=np.float64)
         top = np.maximum(z.max(1), sink)
         e = np.exp(z - top[:, None])
@@ -94,4 +97,4 @@ def attend(q, kc, ksq, vc, vsq, pos, window=0, sinks=None, scale=None):
         out[i] = p @ (sc + vsq[at, 1][:, None])
         coded[i] = p @ sc
         vmax[i] = (15 * vsq[at, 0] + np.abs(vsq[at, 1])).max()
-    return out, coded, mags, norms, vmax
+    return out, coded, mags, norms, key_mags, key_sums, vmax

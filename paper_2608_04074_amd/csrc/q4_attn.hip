@@ -19,87 +19,21 @@
 #include <initializer_list>
 #include <type_traits>
 
-#include "lut_common.h"
-#include "q4_internal.h"
+#include "q4_common.h"
 
 namespace novakv {
 
 namespace {
 
-using lut::add_rows16;
-using lut::add_rows32;
-using lut::float4_t;
-using lut::half8_t;
-using lut::max_rows16;
-using lut::max_rows32;
+using namespace q4;
 
 constexpr int kRound = 32;    // tokens a wave takes at a time
-// The fp16 cores add the products of eight slots after cutting them about 24 bits
-// below the largest, then round to nearest (measured). A sum of small multiples of
-// one unit is therefore exact; one of products far apart loses what lies below
-// the cut, towards one side, which fp32 outputs would show. So with fp32
-// queries a probability is split into two fixed-point parts of 11 bits and the rest.
-constexpr float kNone = -__builtin_inff();
-// Most splits of a tile's span: their weights lie in LDS (16 or 32 rows, 128 rows).
-constexpr int kMaxSplits = 96, kMaxSplitsTiled = 32;
-// Arrival counters of a workspace: a span is split only where at most this many
-// workgroups run, so no call's partials lie on another shape's counters.
-constexpr int kMaxCounters = 1024;
-
-__device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdgcn_exp2f(x); }
-
-typedef int int4_t __attribute__((ext_vector_type(4)));
-
-// Codes k and k + 4 of a word as (c - 8) * 2^-9, two fp16 numbers in a word.
-template <int K>
-__device__ __forceinline__ uint32_t value_pair(const uint32_t w) {
-  const uint32_t x = (K < 2 ? w : w >> 8) & (K % 2 ? 0x00f000f0u : 0x000f000fu);
-  const _Float16 up = K % 2 ? 0x1p11f : 0x1p15f, centre = -0x1p-6f;
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(lut::half2_t, x), lut::half2_t{up, up},
-                                                                lut::half2_t{centre, centre}));
-}
-
-// Coordinate of a lane's output value: tile t, accumulator register i, lane row j.
-template <int D>
-__device__ __forceinline__ int out_coord(const int t, const int i, const int j) {
-  const int m = 4 * j + i;
-  return D == 128 ? 8 * m + t : 8 * (m & 7) + 4 * (m >> 3) + t;
-}
-
-// Split partials meet through memory as device-coherent words (lut_common.h).
-__device__ __forceinline__ void publish4(float *p, const float4 v) {
-  uint64_t *w = reinterpret_cast<uint64_t *>(p);
-  const uint64_t lo = (static_cast<uint64_t>(__float_as_uint(v.y)) << 32) | __float_as_uint(v.x);
-  const uint64_t hi = (static_cast<uint64_t>(__float_as_uint(v.w)) << 32) | __float_as_uint(v.z);
-  __hip_atomic_store(w, lo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store(w + 1, hi, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void publish2(float *p, const float x, const float y) {
-  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (static_cast<uint64_t>(__float_as_uint(y)) << 32) | __float_as_uint(x),
-                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 fetch2(const float *p) {
-  const uint64_t w = __hip_atomic_load(reinterpret_cast<uint64_t *>(const_cast<float *>(p)), __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float(static_cast<uint32_t>(w)), __uint_as_float(static_cast<uint32_t>(w >> 32)));
-}
-
-__device__ __forceinline__ void store_out(const Q4AttnArgs &a, const size_t at, const float4 v) {
-  if (a.q_bf16) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const bf16x4 o = {static_cast<__bf16>(v.x), static_cast<__bf16>(v.y), static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
-    *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(a.out) + at) = o;
-  } else {
-    *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
-  }
-}
-
 // D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows a wave. W: waves of a
 // workgroup. TILED: each wave has rows of its own and all tokens, else the waves
 // share the rows and divide the tokens. ALIGNED: blocks of a multiple of 16 rows.
 template <int D, bool WIDE, int NT, int W, bool TILED, bool ALIGNED>
 __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ? 2 : 3) void q4_attn_kernel(const Q4AttnArgs a) {
-  constexpr int kWaves = W, kThreads = 64 * W, WT = TILED ? 1 : W;
+  constexpr int kWaves = W, WT = TILED ? 1 : W;
   constexpr int kSteps = D / 64;          // matrix steps of a score
   constexpr int kTiles = D / 16;          // output tiles
   constexpr int kKeyWords = D / 32;       // words of a lane's part of a key row
@@ -111,14 +45,12 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   constexpr float kTop = WIDE ? 10.f : 6.f, kSlack = WIDE ? 1.f : 8.f;
   constexpr int kRowGroups = kWaves / WT; // waves on rows of their own
   constexpr int kRows = 16 * NT * kRowGroups;
-  constexpr int kStride = D + 4;
-  // LDS of the merge over waves, then of the splits' weights and sums
-  constexpr int kMergeFloats = WT > 1 ? kWaves * 16 * NT * kStride : 2 * kRows * kMaxSplitsTiled;
+  using Lds = FinishLds<D, NT, W, TILED>;
 
   __shared__ __align__(16) uint32_t s_rows[ALIGNED ? 1 : kWaves][kRound];
   __shared__ __align__(16) float s_scale[kWaves][2 * kRound], s_offset[kWaves][2 * kRound];
   __shared__ float s_ref[kWaves][16 * NT], s_sum[kWaves][16 * NT];
-  __shared__ __align__(16) float s_merge[kMergeFloats];
+  __shared__ __align__(16) float s_merge[Lds::kMerge];
   __shared__ float s_inv[kRows];
   __shared__ int s_last;
 
@@ -126,33 +58,15 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const int tw = wave % WT, rw = wave / WT;
 
-  int wg = lut::xcd_contiguous(blockIdx.x, gridDim.x);
-  const int split = wg % a.n_split;
-  wg /= a.n_split;
-  const int tile = wg % a.row_tiles;
-  const int unit = wg / a.row_tiles;
-  const int b = unit / a.num_kv_heads, kv = unit - b * a.num_kv_heads;
-
-  const int S = min(max(a.seq_lens[b], 0), a.max_seq_len);
-  const int nb = a.q_lens ? min(max(a.q_lens[b], 0), a.n_q) : a.n_q;
-  const int rows_valid = nb * a.gqa;
-  const int wg_row0 = tile * kRows;
-  if (wg_row0 >= rows_valid) return;
-  const int wg_row1 = min(wg_row0 + kRows, rows_valid);
-  // attended positions of query token i: [first_pos(i), S - nb + i]
-  auto last_pos = [&](const int row) { return S - nb + row / a.gqa; };
-  auto first_pos = [&](const int row) { return a.window > 0 ? max(0, last_pos(row) + 1 - a.window) : 0; };
-  const int hi = last_pos(wg_row1 - 1) + 1, lo = first_pos(wg_row0);
-  const int base = lo & ~(kRound - 1);
-  const int span = max(0, hi - base);
-  const int per = ((span + a.n_split - 1) / a.n_split + kRound * WT - 1) / (kRound * WT) * (kRound * WT);
-  const int t0 = min(base + split * per, base + span), t1 = min(t0 + per, base + span);
+  Tile g;
+  if (!find_tile(a, kRows, kRound * WT, g)) return;
+  const int b = g.b, kv = g.kv, rows_valid = g.rows_valid, lo = g.lo, t0 = g.t0, t1 = g.t1;
 
   // this wave's rows
-  const int row0 = wg_row0 + rw * 16 * NT;
+  const int row0 = g.row0 + rw * 16 * NT;
   const int row1 = min(row0 + 16 * NT, rows_valid);
   const bool idle = row0 >= rows_valid;
-  const int inner_lo = idle ? 0 : first_pos(row1 - 1), inner_hi = idle ? 0 : last_pos(row0) + 1;
+  const int inner_lo = idle ? 0 : g.first_pos(a, row1 - 1), inner_hi = idle ? 0 : g.last_pos(a, row0) + 1;
 
   // Rounds of 32 tokens, the codes, scales and offsets of one requested while
   // the round before is computed, its block-table entries one round earlier.
@@ -241,13 +155,13 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + 16 * t + n;
     const bool on = row < rows_valid;
-    const int i = row / a.gqa, g = row - i * a.gqa;
-    row_hi[t] = on ? last_pos(row) + 1 : 0;
-    row_lo[t] = on ? first_pos(row) : 0;
+    const int i = row / a.gqa, h = row - i * a.gqa;
+    row_hi[t] = on ? g.last_pos(a, row) + 1 : 0;
+    row_lo[t] = on ? g.first_pos(a, row) : 0;
     float x[kKeyWords][8];
     float top = 0.f;
     bool finite = true;
-    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + g) * D + 8 * kKeyWords * j;
+    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + h) * D + 8 * kKeyWords * j;
     for (int s = 0; s < kKeyWords; ++s) {
       for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
       if (on) {
@@ -291,7 +205,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
     qsum[t] = static_cast<float>(total);
-    alpha[t] = usable ? a.qscale / to_fixed : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    alpha[t] = usable ? fmaxf(a.qscale / to_fixed, 0x1p-126f) : __builtin_nanf("");  // a row that is not finite: NaN outputs
     ref[t] = kNone;
     sum[t] = off_sum[t] = 0.f;
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -417,151 +331,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     for (int o = 0; o < kTiles; ++o)
       for (int i = 0; i < 4; ++i) acc[t][o][i] = acc[t][o][i] * 0x1p9f + off_sum[t];
   }
-  const int rows_here = wg_row1 - wg_row0;
-  const size_t slot = static_cast<size_t>(kRows) * (D + 2);
-  float *part = nullptr;
-  if (a.n_split > 1) part = a.part + ((static_cast<size_t>(unit) * a.row_tiles + tile) * a.n_split + split) * slot;
-  auto head_of = [&](const int r) { return kv * a.gqa + (wg_row0 + r) % a.gqa; };
-  auto out_at = [&](const int r) {
-    return ((static_cast<size_t>(b) * a.n_q + (wg_row0 + r) / a.gqa) * a.num_q_heads + head_of(r)) * D;
-  };
-  // 1 / the sum of a row's weights with its sink; 0 where nothing is attended
-  auto inverse = [&](const int r, const float most, float l) {
-    if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head_of(r)] * 1.44269504088896341f - most);
-    return most == kNone ? 0.f : 1.f / l;
-  };
-  auto scaled = [](const float4 v, const float f) { return make_float4(v.x * f, v.y * f, v.z * f, v.w * f); };
-  // a lane's values in chunks of four coordinates
-  auto chunk = [&](const int t, const int x) {
-    const int o = 4 * (x / 4), i = x % 4;
-    return make_float4(acc[t][o][i], acc[t][o + 1][i], acc[t][o + 2][i], acc[t][o + 3][i]);
-  };
-  auto chunk_coord = [&](const int x) { return out_coord<D>(4 * (x / 4), x % 4, j); };
-  if constexpr (WT > 1) {  // over the waves, which hold the same rows
-    for (int t = 0; t < NT; ++t) {
-      float *row = s_merge + (wave * 16 * NT + 16 * t + n) * kStride;
-      for (int x = 0; x < kTiles; ++x) *reinterpret_cast<float4 *>(row + chunk_coord(x)) = chunk(t, x);
-      if (j == 0) s_ref[wave][16 * t + n] = ref[t], s_sum[wave][16 * t + n] = sum[t];
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < rows_here * (D / 4); x += kThreads) {
-      const int r = x / (D / 4), c = 4 * (x % (D / 4));
-      float most = kNone, l = 0.f;
-      for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][r]);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int u = 0; u < kWaves; ++u) {
-        if (s_ref[u][r] == kNone) continue;
-        const float f = exp2_raw(s_ref[u][r] - most);
-        const float4 y = *reinterpret_cast<const float4 *>(s_merge + (u * 16 * NT + r) * kStride + c);
-        l += f * s_sum[u][r];
-        v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
-      }
-      if (part) {
-        publish4(part + r * D + c, v);
-        if (c == 0) publish2(part + kRows * D + 2 * r, most, l);
-      } else {
-        store_out(a, out_at(r) + c, scaled(v, inverse(r, most, l)));
-      }
-    }
-  } else {
-    for (int t = 0; t < NT; ++t) {
-      const int r = row0 + 16 * t + n - wg_row0;
-      if (r >= rows_here) continue;
-      const float f = part ? 1.f : inverse(r, ref[t], sum[t]);
-      for (int x = 0; x < kTiles; ++x) {
-        if (part) publish4(part + r * D + chunk_coord(x), chunk(t, x));
-        else store_out(a, out_at(r) + chunk_coord(x), scaled(chunk(t, x), f));
-      }
-      if (part && j == 0) publish2(part + kRows * D + 2 * r, ref[t], sum[t]);
-    }
-  }
-  if (!part) return;
-
-  // Over the splits: the last one to arrive merges them, in their order.
-  __builtin_amdgcn_s_waitcnt(0);  // this thread's words have landed
-  __syncthreads();
-  int *counter = a.counters + static_cast<size_t>(unit) * a.row_tiles + tile;
-  if (threadIdx.x == 0)
-    s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.n_split - 1;
-  __syncthreads();
-  if (!s_last) return;
-  if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const float *parts = part - split * slot;
-  float2 *weight = reinterpret_cast<float2 *>(s_merge);
-  // All words are requested before any is used: the statistics, and each
-  // thread's first values (in groups that share the splits where there are fewer
-  // chunks than threads).
-  const int items = rows_here * (D / 4);
-  const int groups = min(8, max(1, kThreads / items));
-  const int group = groups > 1 ? static_cast<int>(threadIdx.x) / items : 0;
-  const int item = groups > 1 ? static_cast<int>(threadIdx.x) % items : static_cast<int>(threadIdx.x);
-  constexpr int kAhead = 8;
-  float4 v[kAhead];
-  auto fetch_values = [&](const int x, const int first) {
-    const float *src = parts + (x / (D / 4)) * D + 4 * (x % (D / 4));
-    for (int y = 0; y < kAhead; ++y) {
-      const int u = min(first + y * groups, a.n_split - 1);
-      const float2 lo2 = fetch2(src + u * slot), hi2 = fetch2(src + u * slot + 2);
-      v[y] = make_float4(lo2.x, lo2.y, hi2.x, hi2.y);
-    }
-  };
-  const bool mine = group < groups && item < items;
-  for (int x = threadIdx.x; x < rows_here * a.n_split; x += kThreads) {
-    const int r = x / a.n_split, u = x - r * a.n_split;
-    weight[x] = fetch2(parts + u * slot + kRows * D + 2 * r);
-  }
-  if (mine) fetch_values(item, group);
-  __syncthreads();
-  for (int r = threadIdx.x / 16; r < rows_here; r += kThreads / 16) {  // 16 lanes a row
-    float most = kNone, l = 0.f;
-    for (int x = n; x < a.n_split; x += 16) most = fmaxf(most, weight[r * a.n_split + x].x);
-    most = fmaxf(most, lut::row_ror<1>(most));
-    most = fmaxf(most, lut::row_ror<2>(most));
-    most = fmaxf(most, lut::row_ror<4>(most));
-    most = fmaxf(most, lut::row_ror<8>(most));
-    for (int x = n; x < a.n_split; x += 16) {
-      const float2 ml = weight[r * a.n_split + x];
-      const float f = ml.x == kNone ? 0.f : exp2_raw(ml.x - most);
-      l += f == 0.f ? 0.f : f * ml.y;
-      weight[r * a.n_split + x].x = f;
-    }
-    l += lut::row_ror<1>(l);
-    l += lut::row_ror<2>(l);
-    l += lut::row_ror<4>(l);
-    l += lut::row_ror<8>(l);
-    if (n == 0) s_inv[r] = inverse(r, most, l);
-  }
-  __syncthreads();
-  float4 *sums = reinterpret_cast<float4 *>(weight + rows_here * a.n_split + (rows_here * a.n_split & 1));
-  for (int x = item; mine && x < items; x += kThreads) {
-    const int r = x / (D / 4), c = 4 * (x % (D / 4));
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int first = group; first < a.n_split; first += kAhead * groups) {
-      if (x != item || first != group) fetch_values(x, first);
-      for (int y = 0; y < kAhead; ++y) {
-        const int u = first + y * groups;
-        const float f = u < a.n_split ? weight[r * a.n_split + u].x : 0.f;
-        if (f != 0.f) o.x += f * v[y].x, o.y += f * v[y].y, o.z += f * v[y].z, o.w += f * v[y].w;
-      }
-    }
-    if (groups > 1) {
-      sums[group * items + x] = o;
-      break;
-    }
-    store_out(a, out_at(r) + c, scaled(o, s_inv[r]));
-  }
-  if (groups > 1) {
-    __syncthreads();
-    if (static_cast<int>(threadIdx.x) < items) {
-      const int r = threadIdx.x / (D / 4), c = 4 * (threadIdx.x % (D / 4));
-      float4 o = sums[threadIdx.x];
-      for (int g = 1; g < groups; ++g) {
-        const float4 y = sums[g * items + threadIdx.x];
-        o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
-      }
-      store_out(a, out_at(r) + c, scaled(o, s_inv[r]));
-    }
-  }
+  finish_rows<D, NT, W, TILED>(a, g, {s_merge, s_ref, s_sum, s_inv, &s_last}, wave, lane, acc, ref, sum);
 }
 
 }  // namespace
@@ -597,7 +367,7 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
   const double row_ns = static_cast<double>(std::min<long long>(rows, p.tile_rows));
   // token[k - 1]: ns of a CU for a token where k workgroups share it
   auto consider = [&](const int waves, const int setup, const std::initializer_list<double> token, const double merge) {
-    const int step = kRound * (tiled ? 1 : waves), per_cu = static_cast<int>(token.size());
+    const int step = tiled ? (q_bf16 ? 64 : kRound) : kRound * waves, per_cu = static_cast<int>(token.size());
     for (int n = 1; n <= most_splits(p.tile_rows, tiles, span); ++n) {
       const long long chunk = ((span + n - 1) / n + step - 1) / step * step;
       const long long groups = tiles * n, rounds = (groups + 256 * per_cu - 1) / (256 * per_cu);
@@ -640,6 +410,7 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream
       q4_attn_kernel<d(), wide(), nt(), w(), tiled(), false><<<tiles * a.n_split, 64 * w(), 0, stream>>>(a);
     return hipGetLastError();
   };
+  if (a.q_bf16 && plan.tile_rows == 128) return launch_q4_tile(a, plan, stream);
   using std::false_type;
   using std::integral_constant;
   using std::true_type;
@@ -649,7 +420,8 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream
   constexpr integral_constant<int, 8> w8{};
   constexpr integral_constant<int, 12> w12{};
   auto by_rows = [&](auto d, auto wide) {
-    if (plan.tile_rows == 128) return go(d, wide, two, w4, true_type{});
+    if constexpr (wide())
+      if (plan.tile_rows == 128) return go(d, wide, two, w4, true_type{});
     if (plan.tile_rows == 32) return plan.waves == 4 ? go(d, wide, two, w4, false_type{}) : go(d, wide, two, w8, false_type{});
     if (plan.waves == 4) return go(d, wide, one, w4, false_type{});
     if constexpr (wide()) return go(d, wide, one, w8, false_type{});

@@ -1,0 +1,332 @@
+// Attention of many query rows over a cache held in 4 bits (nova_kv_q4_attn with
+// bf16 queries and more than 32 rows per KV head: chunks of prompts).
+//
+// A workgroup of four waves takes 128 rows, 32 a wave, and 64 tokens at a time. The
+// waves unpack the tokens' rows once, between them, to fp16 keys and values in
+// LDS, in the order in which the matrix cores take them, the next 64 while these
+// are used. Unpacked, a score needs no more than its multiply-add into the
+// exponent, and a probability no scale: 7.5 vector instructions each, where
+// q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
+// of keys and values).
+//
+// Keys and values are divided by a power of two at or above the largest
+// magnitude of the 64 tokens (each side its own), which the exponent takes back:
+// fp16 then rounds them by at most 2^-12 of it, below what bf16 queries and
+// outputs show (2^-9 of theirs).
+#include <type_traits>
+
+#include "q4_common.h"
+
+namespace novakv {
+
+namespace {
+
+using namespace q4;
+
+constexpr int kWaves = 4, kRowTiles = 2, kTokens = 64;
+constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability after a rescale, and how far it may grow
+
+// A power of two's exponent at or above a magnitude.
+__device__ __forceinline__ int exponent_of(const float mag) { return mag > 0x1p-100f ? min(ilogbf(mag) + 1, 127) : -99; }
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArgs a) {
+  constexpr int kSteps = D / 32, kTiles = D / 16, kKeyWords = D / 32;
+  constexpr int kKeys = 4 * kSteps * 64, kBuffer = kKeys + 2 * kTiles * 64;  // fragments of 16 bytes: keys, then values
+  using Lds = FinishLds<D, kRowTiles, kWaves, true>;
+  static_assert(2 * kBuffer * 16 >= Lds::kMerge * 4, "the splits' weights take the tokens' place");
+  __shared__ half8_t s_tokens[2][kBuffer];
+  __shared__ uint32_t s_rows[kWaves][32];
+  __shared__ __align__(16) uint32_t s_pack[kWaves][64];
+  __shared__ float s_mag[3][2][2];     // [round mod 3][32 tokens][keys, values]
+  __shared__ uint32_t s_valid[3][2];
+  __shared__ float s_inv[Lds::kRows];
+  __shared__ int s_last;
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+  const int group = wave >> 1, part = wave & 1;  // the wave unpacks 16 keys and half of the coordinates of 32 values
+  Tile g;
+  if (!find_tile(a, Lds::kRows, kTokens, g)) return;
+  const int b = g.b, kv = g.kv;
+  const int row0 = g.row0 + 16 * kRowTiles * wave, row1 = min(row0 + 16 * kRowTiles, g.rows_valid);
+  const bool idle = row0 >= g.rows_valid;
+  const int wave_lo = idle ? 0 : g.first_pos(a, row0), wave_hi = idle ? 0 : g.last_pos(a, row1 - 1) + 1;
+  const int inner_lo = idle ? 0 : g.first_pos(a, row1 - 1), inner_hi = idle ? 0 : g.last_pos(a, row0) + 1;
+
+  // Requests of the tokens' codes, scales and offsets: lane l holds row, scale and
+  // offset of token l % 32 of the wave's 32 (key: l < 32, value: l >= 32).
+  const int bs = a.layout.block_size, bps = a.layout.blocks_per_seq;
+  const uint32_t block_rows = static_cast<uint32_t>(a.num_kv_heads) * bs, head_row = static_cast<uint32_t>(kv) * bs;
+  const int32_t *table = a.layout.block_table ? a.layout.block_table + static_cast<size_t>(b) * bps : nullptr;
+  const uint32_t *sq = reinterpret_cast<const uint32_t *>(lane < 32 ? a.k_sq : a.v_sq);
+  int look = g.t0 + 32 * group + (lane & 31);
+  int look_blk = look / bs, look_row = look - look_blk * bs;
+  const int step_blk = kTokens / bs, step_row = kTokens - step_blk * bs;
+  int phys = -1, phys_tok = 0, phys_row = 0;
+  auto look_up = [&]() {
+    phys = -1;
+    phys_tok = look;
+    phys_row = look_row;
+    if (look_blk < bps) {
+      const long long own = static_cast<long long>(b) * bps + look_blk;
+      phys = table ? table[look_blk] : own < a.num_blocks ? static_cast<int>(own) : -1;
+    }
+    look += kTokens;
+    look_blk += step_blk;
+    look_row += step_row;
+    if (look_row >= bs) look_row -= bs, ++look_blk;
+  };
+  struct Round {
+    uint32_t kw[kKeyWords], vw[8], sq;
+    bool ok;
+  };
+  auto request = [&](Round &r) {
+    r.ok = static_cast<uint32_t>(phys) < static_cast<uint32_t>(a.num_blocks) && phys_tok < g.t1 && phys_tok >= g.lo;
+    const uint32_t row = r.ok ? static_cast<uint32_t>(phys) * block_rows + head_row + phys_row : 0u;  // hidden: row 0 is read
+    s_rows[wave][lane & 31] = row;
+    __builtin_amdgcn_wave_barrier();
+    const uint8_t *k = a.k_codes + static_cast<size_t>(s_rows[wave][16 * part + n]) * (D / 2) + 4 * kKeyWords * j;
+    if constexpr (D == 128) {
+      const uint4 w = *reinterpret_cast<const uint4 *>(k);
+      r.kw[0] = w.x, r.kw[1] = w.y, r.kw[2] = w.z, r.kw[3] = w.w;
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2 *>(k);
+      r.kw[0] = w.x, r.kw[1] = w.y;
+    }
+    for (int e = 0; e < 8; ++e)
+      r.vw[e] = *reinterpret_cast<const uint32_t *>(
+          a.v_codes + static_cast<size_t>(s_rows[wave][16 * (e >> 2) + 4 * j + (e & 3)]) * (D / 2) + 4 * (n & (D / 8 - 1)));
+    __builtin_amdgcn_wave_barrier();
+    r.sq = sq[row];
+  };
+  // scale and offset (from code 8 on) of the lane's token, 0 for hidden tokens
+  auto scale_of = [&](const Round &r, float &scale, float &offset) {
+    scale = r.ok ? __uint_as_float(r.sq << 16) : 0.f;
+    offset = r.ok ? __builtin_fmaf(8.f, scale, __uint_as_float(r.sq & 0xffff0000u)) : 0.f;
+    return 8.f * fabsf(scale) + fabsf(offset);  // the largest magnitude a coordinate can have; not finite: NaN or infinity
+  };
+  auto announce = [&](const Round &r, const int slot) {
+    float scale, offset, mag = scale_of(r, scale, offset);
+    mag = mag < __builtin_inff() ? mag : 0.f;
+    mag = fmaxf(mag, lut::row_ror<8>(mag));
+    mag = fmaxf(mag, lut::row_ror<4>(mag));
+    mag = fmaxf(mag, lut::row_ror<2>(mag));
+    mag = fmaxf(mag, lut::row_ror<1>(mag));
+    mag = max_rows16(mag);  // over the 32 lanes of a side
+    const uint32_t valid = static_cast<uint32_t>(__ballot(r.ok));
+    if (part == 0 && (lane & 31) == 0) s_mag[slot][group][lane >> 5] = mag;
+    if (part == 0 && lane == 0) s_valid[slot][group] = valid;
+  };
+  auto exponents = [&](const int slot, int &ek, int &ev) {
+    ek = exponent_of(fmaxf(s_mag[slot][0][0], s_mag[slot][1][0]));
+    ev = exponent_of(fmaxf(s_mag[slot][0][1], s_mag[slot][1][1]));
+  };
+  auto unpack = [&](const Round &r, const int slot, half8_t *to) {
+    int ek, ev;
+    exponents(slot, ek, ev);
+    float scale, offset;
+    const bool odd = !(scale_of(r, scale, offset) < __builtin_inff());
+    // A value that is not finite would reach the rows it is hidden from (0 * NaN): its
+    // token's key becomes NaN instead, and the value 0.
+    const uint64_t odds = __ballot(odd);
+    const uint32_t any_odd = static_cast<uint32_t>(odds) | static_cast<uint32_t>(odds >> 32);
+    const bool token_odd = (any_odd >> (lane & 31)) & 1u;
+    const float unit = ldexpf(1.f, -(lane < 32 ? ek : ev));
+    scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 512.f);
+    offset = token_odd ? 0.f : offset * unit;
+    const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
+    s_pack[wave][lane] = __builtin_bit_cast(uint32_t, both);
+    __builtin_amdgcn_wave_barrier();
+    auto place = [](const uint32_t codes, const uint32_t scales, const uint32_t offsets) {
+      return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(lut::half2_t, codes), __builtin_bit_cast(lut::half2_t, scales),
+                                                                    __builtin_bit_cast(lut::half2_t, offsets)));
+    };
+    {  // key 16 part + n of the 32: fragment (token tile, step) holds eight coordinates of it a lane
+      const uint32_t p = s_pack[wave][16 * part + n];
+      const uint32_t s2 = __builtin_amdgcn_perm(p, p, 0x01000100u), o2 = __builtin_amdgcn_perm(p, p, 0x03020302u);
+      for (int i = 0; i < kKeyWords; ++i) {
+        const int word = kKeyWords * j + i;
+        const uint32_t w = r.kw[i];
+        to[(wave * kSteps + word / 4) * 64 + 16 * (word % 4) + n] = __builtin_bit_cast(
+            half8_t, make_uint4(place(value_pair<0>(w), s2, o2), place(value_pair<1>(w), s2, o2),
+                                place(value_pair<2>(w), s2, o2), place(value_pair<3>(w), s2, o2)));
+      }
+    }
+    // values: fragment (32 tokens, output tile) holds eight tokens of a coordinate a lane
+    uint32_t s2[4], o2[4], pair[4];
+    const uint32_t pick = D == 128 ? (part ? 0x07060302u : 0x05040100u) : n < 8 ? 0x05040100u : 0x07060302u;
+    for (int h = 0; h < 2; ++h) {
+      const uint4 p = *reinterpret_cast<const uint4 *>(&s_pack[wave][32 + 16 * h + 4 * j]);
+      s2[2 * h] = __builtin_amdgcn_perm(p.y, p.x, 0x05040100u), o2[2 * h] = __builtin_amdgcn_perm(p.y, p.x, 0x07060302u);
+      s2[2 * h + 1] = __builtin_amdgcn_perm(p.w, p.z, 0x05040100u), o2[2 * h + 1] = __builtin_amdgcn_perm(p.w, p.z, 0x07060302u);
+    }
+    __builtin_amdgcn_wave_barrier();
+    for (int e = 0; e < 4; ++e) pair[e] = __builtin_amdgcn_perm(r.vw[2 * e + 1], r.vw[2 * e], pick);
+    auto put = [&](auto k, const int o) {
+      to[kKeys + (group * kTiles + o) * 64 + lane] = __builtin_bit_cast(
+          half8_t, make_uint4(place(value_pair<k()>(pair[0]), s2[0], o2[0]), place(value_pair<k()>(pair[1]), s2[1], o2[1]),
+                              place(value_pair<k()>(pair[2]), s2[2], o2[2]), place(value_pair<k()>(pair[3]), s2[3], o2[3])));
+    };
+    using std::integral_constant;
+    if constexpr (D == 128) {
+      put(integral_constant<int, 0>{}, 4 * part);
+      put(integral_constant<int, 1>{}, 4 * part + 1);
+      put(integral_constant<int, 2>{}, 4 * part + 2);
+      put(integral_constant<int, 3>{}, 4 * part + 3);
+    } else if (part == 0) {
+      put(integral_constant<int, 0>{}, 0);
+      put(integral_constant<int, 1>{}, 1);
+    } else {
+      put(integral_constant<int, 2>{}, 2);
+      put(integral_constant<int, 3>{}, 3);
+    }
+  };
+
+  const bool any = g.t0 < g.t1;
+  Round cur, next;
+  if (any) {
+    look_up();
+    request(cur);
+    look_up();
+  }
+
+  // queries, times a power of two that brings the row's largest magnitude to [2^13, 2^14)
+  half8_t qf[kRowTiles][kSteps];
+  float alpha[kRowTiles], ref[kRowTiles], sum[kRowTiles];
+  int row_lo[kRowTiles], row_hi[kRowTiles];
+  float4_t acc[kRowTiles][kTiles];
+  for (int t = 0; t < kRowTiles; ++t) {
+    const int row = row0 + 16 * t + n;
+    const bool on = row < g.rows_valid;
+    const int i = row / a.gqa, h = row - i * a.gqa;
+    row_hi[t] = on ? g.last_pos(a, row) + 1 : 0;
+    row_lo[t] = on ? g.first_pos(a, row) : 0;
+    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + h) * D + 8 * j;
+    uint4 w[kSteps];
+    float top = 0.f;
+    bool finite = true;
+    for (int s = 0; s < kSteps; ++s) {
+      w[s] = make_uint4(0u, 0u, 0u, 0u);
+      if (on) w[s] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 32 * s);
+      const uint32_t u[4] = {w[s].x, w[s].y, w[s].z, w[s].w};
+      for (int e = 0; e < 4; ++e) {
+        const float x = fabsf(__uint_as_float(u[e] << 16)), y = fabsf(__uint_as_float(u[e] & 0xffff0000u));
+        finite = finite && x < __builtin_inff() && y < __builtin_inff();
+        top = fmaxf(top, fmaxf(x, y));
+      }
+    }
+    top = max_rows32(max_rows16(finite ? top : __builtin_inff()));
+    const bool usable = top < __builtin_inff();
+    const int up = usable && top > 0.f ? min(13 - ilogbf(top), 120) : 0;
+    const float unit = ldexpf(1.f, up);
+    for (int s = 0; s < kSteps; ++s) {
+      const uint32_t u[4] = {w[s].x, w[s].y, w[s].z, w[s].w};
+      for (int e = 0; e < 4; ++e) {
+        const float x[2] = {__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xffff0000u)};
+        for (int y = 0; y < 2; ++y) {
+          const int c = 2 * e + y;  // slots as value_pair has the nibbles: 0, 4, 1, 5, 2, 6, 3, 7
+          qf[t][s][2 * (c & 3) + (c >> 2)] = static_cast<_Float16>(usable ? x[y] * unit : 0.f);
+        }
+      }
+    }
+    alpha[t] = usable ? fmaxf(ldexpf(a.qscale, -up), 0x1p-126f) : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    ref[t] = kNone;
+    sum[t] = 0.f;
+    for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  if (any) {
+    announce(cur, 0);
+    __syncthreads();
+    unpack(cur, 0, s_tokens[0]);
+    request(cur);
+    look_up();
+    announce(cur, 1);
+    __syncthreads();
+  }
+  int slot = 0;
+  for (int tb = g.t0, round = 0; tb < g.t1; tb += kTokens, ++round) {
+    const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
+    request(next);  // past the end: row 0, hidden
+    look_up();
+    unpack(cur, slot1, s_tokens[(round + 1) & 1]);
+    if (!idle && tb < wave_hi && tb + kTokens > wave_lo) {
+      const half8_t *tokens = s_tokens[round & 1];
+      int ek, ev;
+      exponents(slot, ek, ev);
+      const uint32_t valid[2] = {s_valid[slot][0], s_valid[slot][1]};
+      const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
+      const float key_unit = ldexpf(1.f, ek), value_exp = static_cast<float>(ev), value_inv = ldexpf(1.f, -ev);
+      float4_t s[kRowTiles][4];
+      for (int x = 0; x < 4; ++x) {
+        for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
+        for (int st = 0; st < kSteps; ++st) {
+          const half8_t k = tokens[(x * kSteps + st) * 64 + lane];
+          for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
+        }
+      }
+      half8_t pf[kRowTiles][2];
+      for (int t = 0; t < kRowTiles; ++t) {
+        if (!inner) {
+          for (int x = 0; x < 4; ++x)
+            for (int i = 0; i < 4; ++i) {
+              const int m = 16 * x + 4 * j + i;
+              const bool seen = ((valid[x >> 1] >> (m & 31)) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
+              s[t][x][i] = seen ? s[t][x][i] : kNone;
+            }
+        }
+        float top = kNone;
+        for (int x = 0; x < 4; ++x)
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
+        const float scale = fmaxf(alpha[t] * key_unit, 0x1p-126f);
+        const float by = alpha[t] != alpha[t] ? alpha[t] : scale;
+        const float bound = top * by + value_exp;
+        if (__any(bound > ref[t] + (kTop + kSlack))) {
+          const float most = max_rows32(max_rows16(bound));
+          const float to = fmaxf(ref[t], most - kTop);
+          const float f = to == kNone ? 1.f : exp2_raw(ref[t] - to);
+          ref[t] = to;
+          sum[t] *= f;
+          for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+        }
+        const float from = value_exp - (ref[t] == kNone ? 0.f : ref[t]);
+        float part_sum = 0.f;
+        for (int x = 0; x < 4; ++x)
+          for (int i = 0; i < 4; ++i) {
+            const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by, from));
+            part_sum += p;
+            pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p);
+          }
+        sum[t] += part_sum * value_inv;
+      }
+      for (int h = 0; h < 2; ++h)
+        for (int o = 0; o < kTiles; ++o) {
+          const half8_t v = tokens[kKeys + (h * kTiles + o) * 64 + lane];
+          for (int t = 0; t < kRowTiles; ++t) acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[t][h], acc[t][o], 0, 0, 0);
+        }
+    }
+    announce(next, slot2);
+    __syncthreads();
+    cur = next;
+    slot = slot1;
+  }
+
+  for (int t = 0; t < kRowTiles; ++t) {
+    sum[t] = add_rows32(add_rows16(sum[t]));
+    if (sum[t] != sum[t]) ref[t] = fmaxf(ref[t], 0.f);  // NaN logits move no reference, but attend
+  }
+  finish_rows<D, kRowTiles, kWaves, true>(a, g, {reinterpret_cast<float *>(s_tokens), nullptr, nullptr, s_inv, &s_last}, wave, lane, acc, ref,
+                                          sum);
+}
+
+}  // namespace
+
+hipError_t launch_q4_tile(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
+  const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
+  if (a.head_dim == 128) q4_tile_kernel<128><<<groups, 64 * kWaves, 0, stream>>>(a);
+  else q4_tile_kernel<64><<<groups, 64 * kWaves, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace novakv

@@ -14,7 +14,12 @@ Tolerance of an output value, from the roundings on its way (u = 2^-24):
     a probability then is off by a factor e^{2 dz} with its normalization, an output by 2 dz V;
   - fp32 sums over n tokens: below n u of the magnitudes summed, in practice
     sqrt(n) u; taken as 2^-18 V, which covers n = 64 in the worst case and n = 4096 as it is;
-  - probabilities below 2^-31 of the largest leave fp16: n * 2^-30 V.
+  - probabilities below 2^-31 of the largest leave fp16: n * 2^-30 V;
+  - bf16 queries with more than 32 rows per KV head: keys and values are rounded to fp16 over a power of
+    two at or above the largest magnitude of a coordinate's parts, K and V at most, so below twice them: a step of
+    2^-11 below 1. A value: half a step for its offset and for itself, 2^-11 * 2 V. A key's
+    coordinates: independent errors, six deviations of step / sqrt(12) * |q| * scale are
+    1.74 * 2^-10 * K |q| * scale; its offset alike in all, 2^-11 K |sum q| * scale.
 """
 
 import math
@@ -70,12 +75,14 @@ def make_cache(nk, rng, seqs, H, D, block, extra_blocks=3, key_size=1.0, v_size=
     return cache, (kc, vc, ksq, vsq, where)
 
 
-def bound(o, coded, mags, norms, vmax, n, bf16):
+def bound(o, coded, mags, norms, key_mags, key_sums, vmax, n, bf16, tiled):
     """The tolerance above, of outputs [m][G][D]."""
-    V, M, N = vmax[:, None, None], mags[..., None], norms[..., None]
+    V, M, N, K, Q = vmax[:, None, None], *(x[..., None] for x in (mags, norms, key_mags, key_sums))
     dz = 2.0 ** (-13 if bf16 else -20) * N + 2.0 ** -22 * M
+    if tiled:
+        dz = dz + 1.74 * 2.0 ** -10 * K + 2.0 ** -11 * Q
     return (np.abs(o) * 2.0 ** (-8 if bf16 else -24) + ((coded + 8 * V / 15) * 2.0 ** -11 if bf16 else 0) +
-            (2 * dz + 2.0 ** -18 + n * 2.0 ** -30) * V)
+            (2 * dz + 2.0 ** -18 + n * 2.0 ** -30 + (2.0 ** -10 if tiled else 0)) * V)
 
 
 def reference_and_bounds(host, q, seqs, q_lens, window, sinks, scale, bf16):
@@ -92,11 +99,11 @@ def reference_and_bounds(host, q, seqs, q_lens, window, sinks, scale, bf16):
         for h in range(H):
             hs = slice(h * G, (h + 1) * G)
             k, ks, v, vs = (x[phys, h, row] for x in (kc, ksq, vc, vsq))
-            o, coded, mags, norms, vmax = q4.attend(q[b, :m, hs], q4.unpack_codes(k), q4.from_bf16_bits(ks), q4.unpack_codes(v),
+            o, *parts = q4.attend(q[b, :m, hs], q4.unpack_codes(k), q4.from_bf16_bits(ks), q4.unpack_codes(v),
                                              q4.from_bf16_bits(vs), S - m + np.arange(m), window,
                                              None if sinks is None else sinks[hs], scale)
             out[b, :m, hs] = o
-            tol[b, :m, hs] = bound(o, coded, mags, norms, vmax, S, bf16)
+            tol[b, :m, hs] = bound(o, *parts, S, bf16, bf16 and n * G > 32)
     return out, tol
 
 
@@ -229,9 +236,9 @@ def test_blocks_that_hold_nothing(nk):
                 k, ks, v, vs = (x[where[b][0], h, where[b][1]][keep] for x in (kc, ksq, vc, vsq))
                 for i in range(n):
                     m = int((at <= seqs[b] - n + i).sum())
-                    o, coded, mags, norms, vmax = q4.attend(q[b, i:i + 1, 4 * h:4 * h + 4].double().cpu().numpy(), q4.unpack_codes(k),
+                    o, *parts = q4.attend(q[b, i:i + 1, 4 * h:4 * h + 4].double().cpu().numpy(), q4.unpack_codes(k),
                                                      q4.from_bf16_bits(ks), q4.unpack_codes(v), q4.from_bf16_bits(vs), np.array([m - 1]))
-                    tol = bound(o, coded, mags, norms, vmax, 200, True)
+                    tol = bound(o, *parts, 200, True, n * 4 > 32)
                     assert (np.abs(got[b, i:i + 1, 4 * h:4 * h + 4] - o) <= tol).all(), (b, h, i)
 
 
