@@ -30,13 +30,16 @@ __device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdg
 
 typedef int int4_t __attribute__((ext_vector_type(4)));
 
-// Codes k and k + 4 of a word as (c - 8) * 2^-9, two fp16 numbers in a word.
+// Codes k and k + 4 of a word as fp16 denormals in a word: c * 2^-24, times 16 for odd k.
+template <int K>
+__device__ __forceinline__ lut::half2_t code_pair(const uint32_t w) {
+  return __builtin_bit_cast(lut::half2_t, (K < 2 ? w : w >> 8) & (K % 2 ? 0x00f000f0u : 0x000f000fu));
+}
+// The same as (c - 8) * 2^-9.
 template <int K>
 __device__ __forceinline__ uint32_t value_pair(const uint32_t w) {
-  const uint32_t x = (K < 2 ? w : w >> 8) & (K % 2 ? 0x00f000f0u : 0x000f000fu);
   const _Float16 up = K % 2 ? 0x1p11f : 0x1p15f, centre = -0x1p-6f;
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(lut::half2_t, x), lut::half2_t{up, up},
-                                                                lut::half2_t{centre, centre}));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair<K>(w), lut::half2_t{up, up}, lut::half2_t{centre, centre}));
 }
 
 // Coordinate of a lane's output value: tile t, accumulator register i, lane row j.
@@ -94,7 +97,7 @@ __device__ __forceinline__ bool find_tile(const Q4AttnArgs &a, const int rows, c
   int wg = lut::xcd_contiguous(blockIdx.x, gridDim.x);
   g.split = wg % a.n_split;
   wg /= a.n_split;
-  g.tile = wg % a.row_tiles;
+  g.tile = a.row_tiles - 1 - wg % a.row_tiles;  // the last queries, which attend most, first
   g.unit = wg / a.row_tiles;
   g.b = g.unit / a.num_kv_heads;
   g.kv = g.unit - g.b * a.num_kv_heads;

@@ -9,9 +9,11 @@
 // q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
 // of keys and values).
 //
-// Keys and values are divided by a power of two at or above the largest
-// magnitude of the 64 tokens (each side its own), which the exponent takes back:
-// fp16 then rounds them by at most 2^-12 of it, below what bf16 queries and
+// Keys and values are divided by 2^9 times a power of two at or above the
+// largest magnitude of the 64 tokens (each side its own), which the exponent and
+// the output take back: a scale's and an offset's 8 bits then fit fp16, and one
+// packed multiply-add unpacks two codes (fp16 denormals as they lie, c * 2^-24)
+// with one rounding, at most 2^-12 of that power, below what bf16 queries and
 // outputs show (2^-9 of theirs).
 #include <type_traits>
 
@@ -100,11 +102,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     __builtin_amdgcn_wave_barrier();
     r.sq = sq[row];
   };
-  // scale and offset (from code 8 on) of the lane's token, 0 for hidden tokens
+  // scale and offset of the lane's token, 0 for hidden tokens
   auto scale_of = [&](const Round &r, float &scale, float &offset) {
     scale = r.ok ? __uint_as_float(r.sq << 16) : 0.f;
-    offset = r.ok ? __builtin_fmaf(8.f, scale, __uint_as_float(r.sq & 0xffff0000u)) : 0.f;
-    return 8.f * fabsf(scale) + fabsf(offset);  // the largest magnitude a coordinate can have; not finite: NaN or infinity
+    offset = r.ok ? __uint_as_float(r.sq & 0xffff0000u) : 0.f;
+    // the largest magnitude of the row (of code 0 or 15); NaN or infinity where one is
+    const float last = __builtin_fmaf(15.f, scale, offset);
+    return last - last == 0.f ? fmaxf(fabsf(offset), fabsf(last)) : last;
   };
   auto announce = [&](const Round &r, const int slot) {
     float scale, offset, mag = scale_of(r, scale, offset);
@@ -133,15 +137,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     const uint32_t any_odd = static_cast<uint32_t>(odds) | static_cast<uint32_t>(odds >> 32);
     const bool token_odd = (any_odd >> (lane & 31)) & 1u;
     const float unit = ldexpf(1.f, -(lane < 32 ? ek : ev));
-    scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 512.f);
-    offset = token_odd ? 0.f : offset * unit;
+    scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p15f);  // 15 s <= 2 / unit: below 2^13
+    offset = token_odd ? 0.f : offset * (unit * 0x1p-9f);
     const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
     s_pack[wave][lane] = __builtin_bit_cast(uint32_t, both);
     __builtin_amdgcn_wave_barrier();
-    auto place = [](const uint32_t codes, const uint32_t scales, const uint32_t offsets) {
-      return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(lut::half2_t, codes), __builtin_bit_cast(lut::half2_t, scales),
+    // codes k and k + 4 of a word (of two tokens' halves), with their scales and offsets
+    auto place = [](auto k, const uint32_t w, const uint32_t scales, const uint32_t offsets) {
+      const _Float16 down = k() % 2 ? 0x1p-4f : 1.f;
+      return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair<k()>(w), __builtin_bit_cast(lut::half2_t, scales) * lut::half2_t{down, down},
                                                                     __builtin_bit_cast(lut::half2_t, offsets)));
     };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0> c0{};
+    constexpr integral_constant<int, 1> c1{};
+    constexpr integral_constant<int, 2> c2{};
+    constexpr integral_constant<int, 3> c3{};
     {  // key 16 part + n of the 32: fragment (token tile, step) holds eight coordinates of it a lane
       const uint32_t p = s_pack[wave][16 * part + n];
       const uint32_t s2 = __builtin_amdgcn_perm(p, p, 0x01000100u), o2 = __builtin_amdgcn_perm(p, p, 0x03020302u);
@@ -149,8 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
         const int word = kKeyWords * j + i;
         const uint32_t w = r.kw[i];
         to[(wave * kSteps + word / 4) * 64 + 16 * (word % 4) + n] = __builtin_bit_cast(
-            half8_t, make_uint4(place(value_pair<0>(w), s2, o2), place(value_pair<1>(w), s2, o2),
-                                place(value_pair<2>(w), s2, o2), place(value_pair<3>(w), s2, o2)));
+            half8_t, make_uint4(place(c0, w, s2, o2), place(c1, w, s2, o2), place(c2, w, s2, o2), place(c3, w, s2, o2)));
       }
     }
     // values: fragment (32 tokens, output tile) holds eight tokens of a coordinate a lane
@@ -165,21 +175,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     for (int e = 0; e < 4; ++e) pair[e] = __builtin_amdgcn_perm(r.vw[2 * e + 1], r.vw[2 * e], pick);
     auto put = [&](auto k, const int o) {
       to[kKeys + (group * kTiles + o) * 64 + lane] = __builtin_bit_cast(
-          half8_t, make_uint4(place(value_pair<k()>(pair[0]), s2[0], o2[0]), place(value_pair<k()>(pair[1]), s2[1], o2[1]),
-                              place(value_pair<k()>(pair[2]), s2[2], o2[2]), place(value_pair<k()>(pair[3]), s2[3], o2[3])));
+          half8_t, make_uint4(place(k, pair[0], s2[0], o2[0]), place(k, pair[1], s2[1], o2[1]), place(k, pair[2], s2[2], o2[2]),
+                              place(k, pair[3], s2[3], o2[3])));
     };
-    using std::integral_constant;
     if constexpr (D == 128) {
-      put(integral_constant<int, 0>{}, 4 * part);
-      put(integral_constant<int, 1>{}, 4 * part + 1);
-      put(integral_constant<int, 2>{}, 4 * part + 2);
-      put(integral_constant<int, 3>{}, 4 * part + 3);
+      put(c0, 4 * part);
+      put(c1, 4 * part + 1);
+      put(c2, 4 * part + 2);
+      put(c3, 4 * part + 3);
     } else if (part == 0) {
-      put(integral_constant<int, 0>{}, 0);
-      put(integral_constant<int, 1>{}, 1);
+      put(c0, 0);
+      put(c1, 1);
     } else {
-      put(integral_constant<int, 2>{}, 2);
-      put(integral_constant<int, 3>{}, 3);
+      put(c2, 2);
+      put(c3, 3);
     }
   };
 
@@ -257,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
       exponents(slot, ek, ev);
       const uint32_t valid[2] = {s_valid[slot][0], s_valid[slot][1]};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
-      const float key_unit = ldexpf(1.f, ek), value_exp = static_cast<float>(ev), value_inv = ldexpf(1.f, -ev);
+      const float key_unit = ldexpf(512.f, ek), value_exp = static_cast<float>(ev), value_inv = ldexpf(1.f, -ev);
       float4_t s[kRowTiles][4];
       for (int x = 0; x < 4; ++x) {
         for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -315,6 +324,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
   for (int t = 0; t < kRowTiles; ++t) {
     sum[t] = add_rows32(add_rows16(sum[t]));
     if (sum[t] != sum[t]) ref[t] = fmaxf(ref[t], 0.f);  // NaN logits move no reference, but attend
+    for (int o = 0; o < kTiles; ++o) acc[t][o] *= 512.f;
   }
   finish_rows<D, kRowTiles, kWaves, true>(a, g, {reinterpret_cast<float *>(s_tokens), nullptr, nullptr, s_inv, &s_last}, wave, lane, acc, ref,
                                           sum);
