@@ -49,28 +49,26 @@ __device__ __forceinline__ uint32_t bf16_any(const float x) {
   return x != x ? 0x7fc0u : bf16_rne(x);
 }
 
-// Four consecutive elements.
+// Four consecutive elements as they lie (VEC: aligned to their 8 or 16 bytes),
+// converted where they are used, so that a load issued early is not waited for.
 template <bool BF16>
-__device__ __forceinline__ void load4(const void *p, const long long i, const bool vec, float *x) {
+using Raw4 = std::conditional_t<BF16, uint2, float4>;
+template <bool BF16, bool VEC>
+__device__ __forceinline__ Raw4<BF16> load4(const void *p) {
+  if constexpr (VEC) return *static_cast<const Raw4<BF16> *>(p);
   if constexpr (BF16) {
-    const uint16_t *h = static_cast<const uint16_t *>(p) + i;
-    if (vec) {
-      const uint2 w = *reinterpret_cast<const uint2 *>(h);
-      x[0] = __uint_as_float(w.x << 16), x[1] = __uint_as_float(w.x & 0xffff0000u);
-      x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
-    } else {
-      for (int j = 0; j < 4; ++j) x[j] = bf16_bits_to_float(h[j]);
-    }
+    const uint16_t *h = static_cast<const uint16_t *>(p);
+    return make_uint2(h[0] | (static_cast<uint32_t>(h[1]) << 16), h[2] | (static_cast<uint32_t>(h[3]) << 16));
   } else {
-    const float *f = static_cast<const float *>(p) + i;
-    if (vec) {
-      const float4 w = *reinterpret_cast<const float4 *>(f);
-      x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
-    } else {
-      for (int j = 0; j < 4; ++j) x[j] = f[j];
-    }
+    const float *f = static_cast<const float *>(p);
+    return make_float4(f[0], f[1], f[2], f[3]);
   }
 }
+__device__ __forceinline__ void to_floats(const uint2 w, float *x) {
+  x[0] = __uint_as_float(w.x << 16), x[1] = __uint_as_float(w.x & 0xffff0000u);
+  x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
+}
+__device__ __forceinline__ void to_floats(const float4 w, float *x) { x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w; }
 template <bool BF16>
 __device__ __forceinline__ void store4(void *p, const long long i, const float *x) {
   if constexpr (BF16) {
@@ -89,7 +87,10 @@ __device__ __forceinline__ void norm_rotate(T *y, const float *w, const bool nor
     T ss = 0;
     for (int j = 0; j < 8; ++j) ss += y[j] * y[j];
     ss = reduce_row<D / 8>(ss, [](T a, T b) { return a + b; });
-    const T r = static_cast<T>(1) / sqrt(ss / D + static_cast<T>(eps));
+    const T v = ss * static_cast<T>(1. / D) + static_cast<T>(eps);
+    T r;
+    if constexpr (std::is_same_v<T, float>) r = v > 0x1p-100f ? __builtin_amdgcn_rsqf(v) : 1.f / sqrtf(v);  // within 2 u
+    else r = 1 / sqrt(v);
     for (int j = 0; j < 8; ++j) y[j] *= r * static_cast<T>(w[j]);
   }
   if (turns) {
@@ -103,12 +104,152 @@ __device__ __forceinline__ void norm_rotate(T *y, const float *w, const bool nor
   }
 }
 
-template <int D, bool BF16, bool IL, bool Q4>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, const bool vec) {
-  constexpr int kLanes = D / 8, kSlots = kThreads / kLanes;
+// A row's 4-bit codes and its scale and offset in a word, everything that decides
+// them in fp64, so that they do not depend on how a sum is ordered.
+template <int D, bool IL>
+__device__ __forceinline__ void quantize_wide(const float *x, const float *w, const bool norm, const float eps, const float *cs,
+                                              const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+  double y[8];
+  bool odd = false;
+  for (int j = 0; j < 8; ++j) y[j] = x[j];
+  norm_rotate<D, IL, double>(y, w, norm, eps, cs, sn, turns);
+  double lo = y[0], hi = y[0];
+  for (int j = 0; j < 8; ++j) {
+    odd |= !(fabs(y[j]) < __builtin_inf());
+    lo = fmin(lo, y[j]);
+    hi = fmax(hi, y[j]);
+  }
+  lo = reduce_row<D / 8>(lo, [](double p, double q) { return fmin(p, q); });
+  hi = reduce_row<D / 8>(hi, [](double p, double q) { return fmax(p, q); });
+  const float any_odd = reduce_row<D / 8>(odd ? 1.f : 0.f, [](float p, float q) { return fmaxf(p, q); });
+  uint32_t sc = bf16_rne(static_cast<float>((hi - lo) / 15)), of = bf16_rne(static_cast<float>(lo));
+  const bool nan = any_odd != 0.f || (sc & 0x7f80u) == 0x7f80u || (of & 0x7f80u) == 0x7f80u;
+  if (nan) sc = of = 0x7fc0u;
+  const float offset = bf16_bits_to_float(of);
+  const double step = bf16_bits_to_float(sc), inv = 1 / step;
+  for (int j = 0; j < 8; ++j) {
+    // the quotient rounded half to even: from an approximate quotient, then
+    // by the remainder, which is exact
+    const double u = y[j] - offset;
+    double c = rint(u * inv);
+    const double rem = __builtin_fma(-c, step, u);
+    const bool c_odd = (static_cast<int>(fmin(fmax(c, -1.), 16.)) & 1) != 0;
+    if (rem > 0.5 * step || (rem == 0.5 * step && c_odd)) c += 1;
+    if (rem < -0.5 * step || (rem == -0.5 * step && c_odd)) c -= 1;
+    code[j] = nan || step == 0 ? 0u : static_cast<uint32_t>(fmin(fmax(c, 0.), 15.));
+  }
+  sq = sc | (of << 16);
+}
+
+// Whether a value known to within `off` might round to another bf16 number:
+// fp32 bits next to the middle of two. (Zero, denormals and what overflows: yes.)
+__device__ __forceinline__ bool near_bf16_border(const float v, const float off) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const float middle = __builtin_bit_cast(float, (u & 0xffff0000u) | 0x8000u);
+  const uint32_t e = u & 0x7f800000u;
+  return !(fabsf(v - middle) > off) || e == 0 || e >= 0x7f000000u;
+}
+
+// The same codes from fp32 arithmetic, where its rounding cannot have decided one:
+// returns whether the row is sure. The error of y = norm and rotation, u = 2^-24 and
+// m the row's largest |y|: 13 u of the sum of squares (all positive: 8 + 4 additions),
+// half of it in the reciprocal root, with eps, the root's 2 u and two products below
+// 13 u of a coordinate; the rotation's two products and sum below 15 u (|a| + |b|) <=
+// 30 u m. Below 32 u m = 2^-19 m all told; values are exact.
+template <int D, bool IL>
+__device__ __forceinline__ bool quantize_fast(const float *x, const float *w, const bool norm, const float eps, const float *cs,
+                                              const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+  float y[8];
+  for (int j = 0; j < 8; ++j) y[j] = x[j];
+  norm_rotate<D, IL, float>(y, w, norm, eps, cs, sn, turns);
+  float lo = y[0], hi = y[0];
+  for (int j = 1; j < 8; ++j) {
+    lo = fminf(lo, y[j]);
+    hi = fmaxf(hi, y[j]);
+  }
+  float total = 0.f;  // NaN where a coordinate is not finite
+  for (int j = 0; j < 8; ++j) total += y[j] * 0.f;
+  lo = reduce_row<D / 8>(lo, [](float p, float q) { return fminf(p, q); });
+  hi = reduce_row<D / 8>(hi, [](float p, float q) { return fmaxf(p, q); });
+  const float m = fmaxf(fabsf(lo), fabsf(hi));
+  const float off = norm || turns ? m * 0x1p-19f : 0.f;
+  const float range = hi - lo, scale32 = range * (1.f / 15.f);
+  // the roundings of the range, of 1/15 and of their product: below 4 u
+  bool sure = total == 0.f && !near_bf16_border(scale32, 2.f / 15.f * off + scale32 * 0x1p-22f);
+  sure = sure && (off == 0.f ? (__builtin_bit_cast(uint32_t, lo) & 0x7f800000u) < 0x7f000000u : !near_bf16_border(lo, off));
+  const uint32_t sc = bf16_rne(scale32), of = bf16_rne(lo);
+  const float step = bf16_bits_to_float(sc), offset = bf16_bits_to_float(of);
+  const float inv = __builtin_amdgcn_rcpf(step);
+  // a remainder so near half a step that y's error, or the subtraction's, may have decided
+  const float near = off + 0x1p-20f * step;
+  for (int j = 0; j < 8; ++j) {
+    const float u = y[j] - offset;
+    const float c = rintf(u * inv);
+    const float rem = __builtin_fmaf(-c, step, u);
+    const float beyond = fabsf(rem) - 0.5f * step;
+    if (fabsf(beyond) <= near) {
+      // exact where the subtraction was (and y is): then a tie goes to the even code
+      const float bb = u - y[j], lost = (y[j] - (u - bb)) - (offset + bb);
+      const bool exact = off == 0.f && lost == 0.f;
+      float d = c;
+      if (beyond > 0.f || (beyond == 0.f && (static_cast<int>(c) & 1))) d += rem > 0.f ? 1.f : -1.f;
+      sure = sure && (exact || c < -1.f || c > 16.f);
+      code[j] = static_cast<uint32_t>(fminf(fmaxf(d, 0.f), 15.f));
+    } else {
+      sure = sure && beyond < 0.f;  // the quotient's own rounding is far below `near`
+      code[j] = static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
+    }
+  }
+  sq = sc | (of << 16);
+  return sure;
+}
+
+// A row's codes: in fp32, and again in fp64 where any of the wave's rows needs it
+// (the other rows' results are the same). 32 x 4096 tokens: 788 us, 1568 us all in fp64.
+template <int D, bool IL>
+__device__ __forceinline__ void quantize(const float *x, const float *w, const bool norm, const float eps, const float *cs,
+                                         const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+  const bool sure = quantize_fast<D, IL>(x, w, norm, eps, cs, sn, turns, code, sq);
+  // every lane of a row takes the same way: its codes and its scale belong together
+  if (reduce_row<D / 8>(sure ? 0.f : 1.f, [](float p, float q) { return fmaxf(p, q); }) != 0.f)
+    quantize_wide<D, IL>(x, w, norm, eps, cs, sn, turns, code, sq);
+}
+
+// VEC: the rows' base and strides are multiples of 16 bytes. AHEAD: rows of a
+// lane requested at once. FAST: quantize in fp32 where that decides the codes.
+template <int D, bool BF16, bool IL, bool Q4, bool VEC, int AHEAD, bool FAST>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
+  constexpr int kLanes = D / 8, kSlots = kThreads / kLanes, kElem = BF16 ? 2 : 4;
   const int tok = blockIdx.x;
   const int b = tok / a.n_new, i = tok - b * a.n_new;
   if (a.new_lens && i >= a.new_lens[b]) return;
+  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
+  const int heads = a.nq + a.nk + a.nv;
+  const bool turns = lane < a.rotary_dim / 8;
+  const int c0 = !IL && turns ? 4 * lane : 8 * lane;
+  const int c1 = !IL && turns ? c0 + a.rotary_dim / 2 : c0 + 4;
+  // the token's rows on each side (addresses in scalar registers)
+  auto rows_of = [&](const HeadRows &r) {
+    return static_cast<const char *>(r.data) + (b * r.batch_stride + i * r.token_stride) * kElem;
+  };
+  const char *const q_rows = rows_of(a.q), *const k_rows = rows_of(a.k), *const v_rows = rows_of(a.v);
+  struct Row {
+    int side, head;  // 0: query, 1: key, 2: value; -1: none
+    Raw4<BF16> x[2];
+  };
+  const int first = (blockIdx.y * kSlots * AHEAD) + slot;
+  Row rows[AHEAD];
+#pragma unroll
+  for (int y = 0; y < AHEAD; ++y) {
+    const int h = first + y * kSlots;
+    Row &r = rows[y];
+    r.side = h < a.nq ? 0 : h < a.nq + a.nk ? 1 : h < heads ? 2 : -1;
+    r.head = r.side == 0 ? h : r.side == 1 ? h - a.nq : h - a.nq - a.nk;
+    if (r.side < 0) continue;
+    const char *p = (r.side == 0 ? q_rows : r.side == 1 ? k_rows : v_rows) + r.head * (D * kElem);
+    r.x[0] = load4<BF16, VEC>(p + c0 * kElem);
+    r.x[1] = load4<BF16, VEC>(p + c1 * kElem);
+  }
   const long long pos = a.start_pos ? static_cast<long long>(a.start_pos[b]) + i : i;
   if (a.rotary_dim && (pos < 0 || pos >= a.num_positions)) return;
   size_t row0 = 0;  // the cache row of KV head 0
@@ -121,80 +262,56 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a, co
     if (phys < 0 || phys >= a.num_blocks) return;
     row0 = static_cast<size_t>(phys) * a.nk * a.layout.block_size + (static_cast<int>(pos) - blk * a.layout.block_size);
   }
-
-  const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
-  const bool turns = lane < a.rotary_dim / 8;
-  const int c0 = !IL && turns ? 4 * lane : 8 * lane;
-  const int c1 = !IL && turns ? c0 + a.rotary_dim / 2 : c0 + 4;
   float cs[4], sn[4];
   if (turns) {
     const float *t = a.cos_sin + pos * a.rotary_dim + 4 * lane;
-    load4<false>(t, 0, true, cs);
-    load4<false>(t, a.rotary_dim / 2, true, sn);
+    to_floats(load4<false, true>(t), cs);
+    to_floats(load4<false, true>(t + a.rotary_dim / 2), sn);
   }
 
-  const int heads = a.nq + a.nk + a.nv;
-  for (int h = blockIdx.y * kSlots + slot; h < heads; h += gridDim.y * kSlots) {
-    const int side = h < a.nq ? 0 : h < a.nq + a.nk ? 1 : 2;
-    const HeadRows &src = side == 0 ? a.q : side == 1 ? a.k : a.v;
-    const int hh = side == 0 ? h : side == 1 ? h - a.nq : h - a.nq - a.nk;
-    const int n_heads = side == 0 ? a.nq : side == 1 ? a.nk : a.nv;
-    const long long at = b * src.batch_stride + i * src.token_stride + static_cast<long long>(hh) * D;
+#pragma unroll
+  for (int y = 0; y < AHEAD; ++y) {
+    const int side = rows[y].side, hh = rows[y].head;
+    if (side < 0) continue;
     float x[8], w[8];
-    load4<BF16>(src.data, at + c0, vec, x);
-    load4<BF16>(src.data, at + c1, vec, x + 4);
+    to_floats(rows[y].x[0], x);
+    to_floats(rows[y].x[1], x + 4);
     const float *weight = side == 0 ? a.q_norm : side == 1 ? a.k_norm : nullptr;
     if (weight) {
       weight += hh * (side == 0 ? a.q_norm_stride : a.k_norm_stride);
-      load4<false>(weight, c0, true, w);
-      load4<false>(weight, c1, true, w + 4);
+      to_floats(load4<false, true>(weight + c0), w);
+      to_floats(load4<false, true>(weight + c1), w + 4);
     }
     void *out = side == 0 ? a.q_out : side == 1 ? a.k_out : a.v_out;
-    const long long to = (static_cast<long long>(tok) * n_heads + hh) * D;
+    const long long to = (static_cast<long long>(tok) * (side == 0 ? a.nq : side == 1 ? a.nk : a.nv) + hh) * D;
     if (!Q4 || side == 0) {
       norm_rotate<D, IL, float>(x, w, weight != nullptr, a.eps, cs, sn, turns && side < 2);
       store4<BF16>(out, to + c0, x);
       store4<BF16>(out, to + c1, x + 4);
       continue;
     }
-    // 4 bits: everything that decides a code in fp64, so that the codes do not
-    // depend on how a sum is ordered
-    double y[8];
-    bool odd = false;
-    for (int j = 0; j < 8; ++j) y[j] = x[j];
-    norm_rotate<D, IL, double>(y, w, weight != nullptr, a.eps, cs, sn, turns && side < 2);
-    double lo = y[0], hi = y[0];
-    for (int j = 0; j < 8; ++j) {
-      odd |= !(fabs(y[j]) < __builtin_inf());
-      lo = fmin(lo, y[j]);
-      hi = fmax(hi, y[j]);
-    }
-    lo = reduce_row<kLanes>(lo, [](double p, double q) { return fmin(p, q); });
-    hi = reduce_row<kLanes>(hi, [](double p, double q) { return fmax(p, q); });
-    const float any_odd = reduce_row<kLanes>(odd ? 1.f : 0.f, [](float p, float q) { return fmaxf(p, q); });
-    uint32_t sc = bf16_rne(static_cast<float>((hi - lo) / 15)), of = bf16_rne(static_cast<float>(lo));
-    const bool nan = any_odd != 0.f || (sc & 0x7f80u) == 0x7f80u || (of & 0x7f80u) == 0x7f80u;
-    if (nan) sc = of = 0x7fc0u;
-    const float scale = bf16_bits_to_float(sc), offset = bf16_bits_to_float(of);
-    const double step = scale, inv = 1 / step;
-    uint32_t code[8];
-    for (int j = 0; j < 8; ++j) {
-      // the quotient rounded half to even: from an approximate quotient, then
-      // by the remainder, which is exact
-      const double u = y[j] - offset;
-      double c = rint(u * inv);
-      const double rem = __builtin_fma(-c, step, u);
-      const bool c_odd = (static_cast<int>(fmin(fmax(c, -1.), 16.)) & 1) != 0;
-      if (rem > 0.5 * step || (rem == 0.5 * step && c_odd)) c += 1;
-      if (rem < -0.5 * step || (rem == -0.5 * step && c_odd)) c -= 1;
-      code[j] = nan || step == 0 ? 0u : static_cast<uint32_t>(fmin(fmax(c, 0.), 15.));
-    }
+    uint32_t code[8], sq;
+    if constexpr (FAST) quantize<D, IL>(x, w, weight != nullptr, a.eps, cs, sn, turns && side == 1, code, sq);
+    else quantize_wide<D, IL>(x, w, weight != nullptr, a.eps, cs, sn, turns && side == 1, code, sq);
     const size_t row = row0 + static_cast<size_t>(hh) * a.layout.block_size;
     uint8_t *dst = (side == 1 ? a.k_codes : a.v_codes) + row * (D / 2);
-    *reinterpret_cast<uint16_t *>(dst + c0 / 2) = code[0] | (code[1] << 4) | (code[2] << 8) | (code[3] << 12);
-    *reinterpret_cast<uint16_t *>(dst + c1 / 2) = code[4] | (code[5] << 4) | (code[6] << 8) | (code[7] << 12);
-    if (lane == 0) *reinterpret_cast<uint32_t *>((side == 1 ? a.k_sq : a.v_sq) + 2 * row) = sc | (of << 16);
+    uint32_t packed = 0;
+    for (int j = 0; j < 8; ++j) packed |= code[j] << (4 * j);
+    // Stores of four bytes: a lane's chunks follow each other, or (halves) two
+    // neighbours exchange one, the even lane storing both lower chunks.
+    if (IL || !turns) {
+      *reinterpret_cast<uint32_t *>(dst + c0 / 2) = packed;
+    } else if ((lane | 1) < a.rotary_dim / 8) {
+      const uint32_t other = __builtin_amdgcn_update_dpp(0, static_cast<int>(packed), 0xB1, 0xf, 0xf, false);  // lane ^ 1
+      if (lane & 1) *reinterpret_cast<uint32_t *>(dst + (c1 - 4) / 2) = (other >> 16) | (packed & 0xffff0000u);
+      else *reinterpret_cast<uint32_t *>(dst + c0 / 2) = (packed & 0xffffu) | (other << 16);
+    } else {  // the last of an odd number of rotated chunks
+      *reinterpret_cast<uint16_t *>(dst + c0 / 2) = packed;
+      *reinterpret_cast<uint16_t *>(dst + c1 / 2) = packed >> 16;
+    }
+    if (lane == 0) *reinterpret_cast<uint32_t *>((side == 1 ? a.k_sq : a.v_sq) + 2 * row) = sq;
     if (out) {
+      const float scale = bf16_bits_to_float(sq & 0xffffu), offset = bf16_bits_to_float(sq >> 16);
       for (int j = 0; j < 8; ++j) x[j] = scale * static_cast<float>(code[j]) + offset;
       store4<BF16>(out, to + c0, x);
       store4<BF16>(out, to + c1, x + 4);
@@ -215,18 +332,31 @@ hipError_t launch_rotate(const RotateArgs &a, hipStream_t stream) {
   const int elem = a.bf16 ? 2 : 4;
   const bool vec = vector_rows(a.q, elem) && vector_rows(a.k, elem) && vector_rows(a.v, elem);
   const int slots = kThreads / (a.head_dim / 8), heads = a.nq + a.nk + a.nv;
-  const dim3 grid(static_cast<unsigned>(a.batch) * a.n_new, (heads + slots - 1) / slots);
-  auto go = [&](auto kernel) {
-    kernel<<<grid, kThreads, 0, stream>>>(a, vec);
-    return hipGetLastError();
+  const unsigned tokens = static_cast<unsigned>(a.batch) * a.n_new;
+  // Many tokens: a lane requests three rows at once (32 x 4096 tokens rotated in
+  // 589 us, one row at a time 693 us; with few, more workgroups share them: 1839
+  // tokens 11.9 us against 12.8 us), and quantizes in fp32 with a second look in fp64
+  // (805 us against 1568 us; of 64 tokens some wave always takes both ways: 5.5 us
+  // against 4.9 us in fp64 alone).
+  auto go = [&](auto d, auto bf16, auto il, auto q4, auto vec) {
+    const auto launch = [&](auto ahead, auto fast) {
+      const dim3 grid(tokens, (heads + slots * ahead() - 1) / (slots * ahead()));
+      rotate_kernel<d(), bf16(), il(), q4(), vec(), ahead(), fast()><<<grid, kThreads, 0, stream>>>(a);
+      return hipGetLastError();
+    };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 3> three{};
+    if (tokens >= 8192) return launch(three, std::bool_constant<q4()>{});
+    if constexpr (q4())
+      if (tokens >= 512) return launch(one, std::true_type{});
+    return launch(one, std::false_type{});
   };
-  auto by_cache = [&](auto d, auto bf16, auto il) {
-    return a.q4 ? go(rotate_kernel<d(), bf16(), il(), true>) : go(rotate_kernel<d(), bf16(), il(), false>);
-  };
-  auto by_pairs = [&](auto d, auto bf16) {
-    return a.interleaved ? by_cache(d, bf16, std::true_type{}) : by_cache(d, bf16, std::false_type{});
-  };
-  auto by_type = [&](auto d) { return a.bf16 ? by_pairs(d, std::true_type{}) : by_pairs(d, std::false_type{}); };
+  using std::false_type;
+  using std::true_type;
+  auto by_rows = [&](auto d, auto bf16, auto il, auto q4) { return vec ? go(d, bf16, il, q4, true_type{}) : go(d, bf16, il, q4, false_type{}); };
+  auto by_cache = [&](auto d, auto bf16, auto il) { return a.q4 ? by_rows(d, bf16, il, true_type{}) : by_rows(d, bf16, il, false_type{}); };
+  auto by_pairs = [&](auto d, auto bf16) { return a.interleaved ? by_cache(d, bf16, true_type{}) : by_cache(d, bf16, false_type{}); };
+  auto by_type = [&](auto d) { return a.bf16 ? by_pairs(d, true_type{}) : by_pairs(d, false_type{}); };
   return a.head_dim == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
 }
 

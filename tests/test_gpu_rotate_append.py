@@ -203,7 +203,38 @@ def test_append(nk, shape, block, dtype):
             assert (got_c == (0xA5, 0x5A)[side]).all() and (got_sq == q4.to_bf16_bits((2.0, 3.0)[side])).all()
 
 
-def test_append_borders(nk):
+@pytest.mark.parametrize("dtype", (BF, F32))
+@pytest.mark.parametrize("shape", [(2, 300, 4, 2, 128, 128, False, "shared"), (1, 8200, 2, 1, 64, 64, True, "heads"),
+                                   (3, 2800, 3, 1, 128, 48, False, None), (600, 1, 2, 2, 64, 24, False, "shared")])
+def test_many_tokens(nk, shape, dtype):
+    """Launches of many tokens quantize in fp32, and again in fp64 where that may not decide:
+    the codes are those of fp64 all the same."""
+    B, n, Hq, H, D, rotary, il, norm = shape
+    say(f"many tokens {shape} {dtype}")
+    rng = np.random.default_rng(7)
+    rot = rotary_of(nk, rng, Hq, H, D, rotary, il, norm, P=n + 5)
+    q, k, v = heads_of(rng, B, n, Hq, H, D, dtype, True)
+    start = [int(rng.integers(0, 5)) for _ in range(B)]
+    lay = nk.CacheLayout(16, -(-(n + 5) // 16), None)
+    cache = nk.Q4Cache.zeros(lay, B, H, D)
+    q_out = nk.q4_append(rot, cache, q, k, v, i32(start))
+    rotated = nk.rotate_qkv(rot, q, k, v, i32(start))
+    assert torch.equal(q_out, rotated[0]) and torch.equal(rotated[2], v)
+    every = np.ones((B, n), dtype=bool)
+    ref_k = oracle_heads(rot, k, rot.k_norm, start)
+    assert_close(q_out, oracle_heads(rot, q, rot.q_norm, start), dtype, every)
+    assert_close(rotated[1], ref_k, dtype, every)
+    pos = np.asarray(start)[:, None] + np.arange(n)
+    page = np.arange(B)[:, None] * lay.blocks_per_seq + pos // 16
+    for y, codes, sq in ((ref_k, cache.k_codes, cache.k_sq), (v.double().cpu().numpy(), cache.v_codes, cache.v_sq)):
+        rc, rsq, gap = q4.quantize_rows(y)
+        assert (sq.view(torch.int16).cpu().numpy().view(np.uint16)[page, :, pos % 16] == rsq).all()
+        bad = q4.unpack_codes(codes.cpu().numpy()[page, :, pos % 16]) != rc
+        assert not (bad & (gap > 1e-9)).any()
+
+
+@pytest.mark.parametrize("copies", (1, 40, 600))
+def test_append_borders(nk, copies):
     """Rows of quotients that are ties, constant rows, tiny and huge ones, NaN and infinities."""
     D = 64
     rows = [np.arange(D) % 31 / 2 - 3.0,                                   # every half: ties to even
@@ -213,6 +244,7 @@ def test_append_borders(nk):
             np.where(np.arange(D) == 63, 1e30, 1.0), np.linspace(100, 100.01, D),
             np.where(np.arange(D) == 9, np.nan, 1.0), np.where(np.arange(D) == 63, np.inf, 1.0),
             np.where(np.arange(D) == 0, -np.inf, 1.0), np.where(np.arange(D) == 31, -3.4e38, 1.0)]
+    rows = rows * copies
     x = np.array(rows, dtype=np.float32)[None, :, None]
     for dtype in (F32, BF):
         t = torch.as_tensor(x).to(dtype).cuda()
