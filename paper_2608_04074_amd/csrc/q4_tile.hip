@@ -259,56 +259,64 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
     request(next);  // past the end: row 0, hidden
     look_up();
+    const half8_t *tokens = s_tokens[round & 1];
+    float4_t s[kRowTiles][4];
+    for (int x = 0; x < 4; ++x) {
+      for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
+      for (int st = 0; st < kSteps; ++st) {
+        const half8_t k = tokens[(x * kSteps + st) * 64 + lane];
+        for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
+      }
+    }
     unpack(cur, slot1, s_tokens[(round + 1) & 1]);
     if (!idle && tb < wave_hi && tb + kTokens > wave_lo) {
-      const half8_t *tokens = s_tokens[round & 1];
       int ek, ev;
       exponents(slot, ek, ev);
       const uint32_t valid[2] = {s_valid[slot][0], s_valid[slot][1]};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
       const float key_unit = ldexpf(512.f, ek), value_exp = static_cast<float>(ev), value_inv = ldexpf(1.f, -ev);
-      float4_t s[kRowTiles][4];
-      for (int x = 0; x < 4; ++x) {
-        for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
-        for (int st = 0; st < kSteps; ++st) {
-          const half8_t k = tokens[(x * kSteps + st) * 64 + lane];
-          for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
-        }
-      }
-      half8_t pf[kRowTiles][2];
-      for (int t = 0; t < kRowTiles; ++t) {
-        if (!inner) {
+      if (!inner) {
+        for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
             for (int i = 0; i < 4; ++i) {
               const int m = 16 * x + 4 * j + i;
               const bool seen = ((valid[x >> 1] >> (m & 31)) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
               s[t][x][i] = seen ? s[t][x][i] : kNone;
             }
-        }
+      }
+      float by[kRowTiles], bound[kRowTiles];
+      bool over = false;
+      for (int t = 0; t < kRowTiles; ++t) {
         float top = kNone;
         for (int x = 0; x < 4; ++x)
           for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
-        const float scale = fmaxf(alpha[t] * key_unit, 0x1p-126f);
-        const float by = alpha[t] != alpha[t] ? alpha[t] : scale;
-        const float bound = top * by + value_exp;
-        if (__any(bound > ref[t] + (kTop + kSlack))) {
-          const float most = max_rows32(max_rows16(bound));
+        by[t] = alpha[t] != alpha[t] ? alpha[t] : fmaxf(alpha[t] * key_unit, 0x1p-126f);
+        bound[t] = top * by[t] + value_exp;
+        over |= bound[t] > ref[t] + (kTop + kSlack);
+      }
+      if (__any(over)) {
+        for (int t = 0; t < kRowTiles; ++t) {
+          const float most = max_rows32(max_rows16(bound[t]));
           const float to = fmaxf(ref[t], most - kTop);
           const float f = to == kNone ? 1.f : exp2_raw(ref[t] - to);
           ref[t] = to;
           sum[t] *= f;
           for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
         }
+      }
+      half8_t pf[kRowTiles][2];
+      auto probabilities = [&](const int t) {
         const float from = value_exp - (ref[t] == kNone ? 0.f : ref[t]);
         float part_sum = 0.f;
         for (int x = 0; x < 4; ++x)
           for (int i = 0; i < 4; ++i) {
-            const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by, from));
+            const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by[t], from));
             part_sum += p;
             pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p);
           }
         sum[t] += part_sum * value_inv;
-      }
+      };
+      for (int t = 0; t < kRowTiles; ++t) probabilities(t);
       for (int h = 0; h < 2; ++h)
         for (int o = 0; o < kTiles; ++o) {
           const half8_t v = tokens[kKeys + (h * kTiles + o) * 64 + lane];
