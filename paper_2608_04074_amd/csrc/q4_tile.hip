@@ -28,17 +28,24 @@ using namespace q4;
 constexpr int kWaves = 4, kRowTiles = 2, kTokens = 64;
 constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability after a rescale, and how far it may grow
 
-// A power of two's exponent at or above a magnitude.
-__device__ __forceinline__ int exponent_of(const float mag) { return mag > 0x1p-100f ? min(ilogbf(mag) + 1, 127) : -99; }
+// The same value in every lane, in a scalar register.
+__device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
+// Exponent of a power of two above a magnitude (above a quarter of it beyond 2^126), from its bits.
+__device__ __forceinline__ int exponent_of(const float mag) {
+  const int e = uniform(__builtin_bit_cast(int, mag)) >> 23;  // mag >= 0
+  return min(max(e - 126, -99), 126);
+}
+__device__ __forceinline__ float power_of_two(const int e) { return __builtin_bit_cast(float, (e + 127) << 23); }
 
-template <int D>
+// ALIGNED: blocks of a multiple of 16 rows.
+template <int D, bool ALIGNED>
 __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArgs a) {
   constexpr int kSteps = D / 32, kTiles = D / 16, kKeyWords = D / 32;
   constexpr int kKeys = 4 * kSteps * 64, kBuffer = kKeys + 2 * kTiles * 64;  // fragments of 16 bytes: keys, then values
   using Lds = FinishLds<D, kRowTiles, kWaves, true>;
   static_assert(2 * kBuffer * 16 >= Lds::kMerge * 4, "the splits' weights take the tokens' place");
   __shared__ half8_t s_tokens[2][kBuffer];
-  __shared__ uint32_t s_rows[kWaves][32];
+  __shared__ uint32_t s_rows[ALIGNED ? 1 : kWaves][32];
   __shared__ __align__(16) uint32_t s_pack[kWaves][64];
   __shared__ float s_mag[3][2][2];     // [round mod 3][32 tokens][keys, values]
   __shared__ uint32_t s_valid[3][2];
@@ -83,12 +90,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     uint32_t kw[kKeyWords], vw[8], sq;
     bool ok;
   };
-  auto request = [&](Round &r) {
-    r.ok = static_cast<uint32_t>(phys) < static_cast<uint32_t>(a.num_blocks) && phys_tok < g.t1 && phys_tok >= g.lo;
-    const uint32_t row = r.ok ? static_cast<uint32_t>(phys) * block_rows + head_row + phys_row : 0u;  // hidden: row 0 is read
-    s_rows[wave][lane & 31] = row;
-    __builtin_amdgcn_wave_barrier();
-    const uint8_t *k = a.k_codes + static_cast<size_t>(s_rows[wave][16 * part + n]) * (D / 2) + 4 * kKeyWords * j;
+  const uint32_t k_lane = n * (D / 2) + 4 * kKeyWords * j, v_lane = 4 * j * (D / 2) + 4 * (n & (D / 8 - 1));
+  auto read_key = [&](Round &r, const uint8_t *k) {
     if constexpr (D == 128) {
       const uint4 w = *reinterpret_cast<const uint4 *>(k);
       r.kw[0] = w.x, r.kw[1] = w.y, r.kw[2] = w.z, r.kw[3] = w.w;
@@ -96,10 +99,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
       const uint2 w = *reinterpret_cast<const uint2 *>(k);
       r.kw[0] = w.x, r.kw[1] = w.y;
     }
-    for (int e = 0; e < 8; ++e)
-      r.vw[e] = *reinterpret_cast<const uint32_t *>(
-          a.v_codes + static_cast<size_t>(s_rows[wave][16 * (e >> 2) + 4 * j + (e & 3)]) * (D / 2) + 4 * (n & (D / 8 - 1)));
-    __builtin_amdgcn_wave_barrier();
+  };
+  auto request = [&](Round &r) {
+    const bool held = static_cast<uint32_t>(phys) < static_cast<uint32_t>(a.num_blocks);
+    r.ok = held && phys_tok < g.t1 && phys_tok >= g.lo;
+    uint32_t row = static_cast<uint32_t>(phys) * block_rows + head_row + phys_row;
+    if constexpr (ALIGNED) {  // 16 tokens' rows follow each other; in the place of a block that holds nothing, the pool's first
+      if (!held) row = lane & 15;
+      const size_t first[2] = {static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(row, 0))) * (D / 2),
+                               static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(row, 16))) * (D / 2)};
+      read_key(r, a.k_codes + first[part] + k_lane);
+      for (int e = 0; e < 8; ++e)
+        r.vw[e] = *reinterpret_cast<const uint32_t *>(a.v_codes + first[e >> 2] + (v_lane + (e & 3) * (D / 2)));
+    } else {
+      if (!r.ok) row = 0;
+      s_rows[wave][lane & 31] = row;
+      __builtin_amdgcn_wave_barrier();
+      read_key(r, a.k_codes + static_cast<size_t>(s_rows[wave][16 * part + n]) * (D / 2) + 4 * kKeyWords * j);
+      for (int e = 0; e < 8; ++e)
+        r.vw[e] = *reinterpret_cast<const uint32_t *>(
+            a.v_codes + static_cast<size_t>(s_rows[wave][16 * (e >> 2) + 4 * j + (e & 3)]) * (D / 2) + 4 * (n & (D / 8 - 1)));
+      __builtin_amdgcn_wave_barrier();
+    }
     r.sq = sq[row];
   };
   // scale and offset of the lane's token, 0 for hidden tokens
@@ -126,9 +147,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     ek = exponent_of(fmaxf(s_mag[slot][0][0], s_mag[slot][1][0]));
     ev = exponent_of(fmaxf(s_mag[slot][0][1], s_mag[slot][1][1]));
   };
-  auto unpack = [&](const Round &r, const int slot, half8_t *to) {
-    int ek, ev;
-    exponents(slot, ek, ev);
+  auto unpack = [&](const Round &r, const int ek, const int ev, half8_t *to) {
     float scale, offset;
     const bool odd = !(scale_of(r, scale, offset) < __builtin_inff());
     // A value that is not finite would reach the rows it is hidden from (0 * NaN): its
@@ -136,7 +155,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     const uint64_t odds = __ballot(odd);
     const uint32_t any_odd = static_cast<uint32_t>(odds) | static_cast<uint32_t>(odds >> 32);
     const bool token_odd = (any_odd >> (lane & 31)) & 1u;
-    const float unit = ldexpf(1.f, -(lane < 32 ? ek : ev));
+    const float unit = lane < 32 ? power_of_two(-ek) : power_of_two(-ev);
     scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p15f);  // 15 s <= 2 / unit: below 2^13
     offset = token_odd ? 0.f : offset * (unit * 0x1p-9f);
     const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
@@ -193,7 +212,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
   };
 
   const bool any = g.t0 < g.t1;
-  Round cur, next;
+  Round cur;
   if (any) {
     look_up();
     request(cur);
@@ -245,20 +264,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
 
+  int ek = 0, ev = 0, slot = 1;  // of the round at hand; the slot of the one behind it
   if (any) {
     announce(cur, 0);
     __syncthreads();
-    unpack(cur, 0, s_tokens[0]);
+    exponents(0, ek, ev);
+    unpack(cur, ek, ev, s_tokens[0]);
     request(cur);
     look_up();
     announce(cur, 1);
     __syncthreads();
   }
-  int slot = 0;
   for (int tb = g.t0, round = 0; tb < g.t1; tb += kTokens, ++round) {
-    const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
-    request(next);  // past the end: row 0, hidden
-    look_up();
+    const int slot0 = slot == 0 ? 2 : slot - 1, slot2 = slot == 2 ? 0 : slot + 1;
     const half8_t *tokens = s_tokens[round & 1];
     float4_t s[kRowTiles][4];
     for (int x = 0; x < 4; ++x) {
@@ -268,13 +286,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
         for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
       }
     }
-    unpack(cur, slot1, s_tokens[(round + 1) & 1]);
+    int next_ek, next_ev;
+    exponents(slot, next_ek, next_ev);
+    unpack(cur, next_ek, next_ev, s_tokens[(round + 1) & 1]);
+    request(cur);  // past the end: hidden
+    look_up();
     if (!idle && tb < wave_hi && tb + kTokens > wave_lo) {
-      int ek, ev;
-      exponents(slot, ek, ev);
-      const uint32_t valid[2] = {s_valid[slot][0], s_valid[slot][1]};
+      const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][0])), static_cast<uint32_t>(uniform(s_valid[slot0][1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
-      const float key_unit = ldexpf(512.f, ek), value_exp = static_cast<float>(ev), value_inv = ldexpf(1.f, -ev);
+      const float key_unit = power_of_two(ek) * 512.f, value_exp = static_cast<float>(ev), value_inv = power_of_two(-ev);
       if (!inner) {
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
@@ -307,12 +327,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
       half8_t pf[kRowTiles][2];
       auto probabilities = [&](const int t) {
         const float from = value_exp - (ref[t] == kNone ? 0.f : ref[t]);
-        float part_sum = 0.f;
+        float part_sum = 0.f;  // of the probabilities as fp16 has them
         for (int x = 0; x < 4; ++x)
-          for (int i = 0; i < 4; ++i) {
-            const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by[t], from));
-            part_sum += p;
-            pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p);
+          for (int i = 0; i < 4; i += 2) {
+            const lut::half2_t p = {static_cast<_Float16>(exp2_raw(__builtin_fmaf(s[t][x][i], by[t], from))),
+                                    static_cast<_Float16>(exp2_raw(__builtin_fmaf(s[t][x][i + 1], by[t], from)))};
+            part_sum = __builtin_amdgcn_fdot2(p, lut::half2_t{1, 1}, part_sum, false);
+            pf[t][x >> 1][4 * (x & 1) + i] = p[0], pf[t][x >> 1][4 * (x & 1) + i + 1] = p[1];
           }
         sum[t] += part_sum * value_inv;
       };
@@ -323,10 +344,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
           for (int t = 0; t < kRowTiles; ++t) acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[t][h], acc[t][o], 0, 0, 0);
         }
     }
-    announce(next, slot2);
+    announce(cur, slot2);
     __syncthreads();
-    cur = next;
-    slot = slot1;
+    ek = next_ek, ev = next_ev;
+    slot = slot2;
   }
 
   for (int t = 0; t < kRowTiles; ++t) {
@@ -342,9 +363,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
 
 hipError_t launch_q4_tile(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
   const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
-  if (a.head_dim == 128) q4_tile_kernel<128><<<groups, 64 * kWaves, 0, stream>>>(a);
-  else q4_tile_kernel<64><<<groups, 64 * kWaves, 0, stream>>>(a);
-  return hipGetLastError();
+  auto go = [&](auto d, auto aligned) {
+    q4_tile_kernel<d(), aligned()><<<groups, 64 * kWaves, 0, stream>>>(a);
+    return hipGetLastError();
+  };
+  auto by_size = [&](auto aligned) {
+    return a.head_dim == 128 ? go(std::integral_constant<int, 128>{}, aligned) : go(std::integral_constant<int, 64>{}, aligned);
+  };
+  return a.layout.block_size % 16 == 0 ? by_size(std::true_type{}) : by_size(std::false_type{});
 }
 
 }  // namespace novakv
