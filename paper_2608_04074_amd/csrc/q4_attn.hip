@@ -362,32 +362,36 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
   // over both (8 KV heads of 128, bf16, us): one sequence of 128K tokens 36.2 in
   // 32 splits of 12 waves, 38.6 in 64 of 4 waves, 46.2 in 32 of 4; of 2000 tokens
   // 15.2 in 3 of 12, 10.4 in 16 of 4; 32 x 8192 55.6 whole by 12 waves, 57.2 in 3 of
-  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12.
+  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12; 64 queries over 32K tokens 128 in 16
+  // splits, 186 in 32, 168 in 8; 8 x 64 over 2000 tokens 70 whole, 81 in 2.
   const double size = head_dim == 128 ? 1.0 : 0.75;
   const double row_ns = static_cast<double>(std::min<long long>(rows, p.tile_rows));
   // token[k - 1]: ns of a CU for a token where k workgroups share it
-  auto consider = [&](const int waves, const int setup, const std::initializer_list<double> token, const double merge) {
+  auto consider = [&](const int waves, const int setup, const std::initializer_list<double> token, const int split,
+                      const double merge) {
     const int step = tiled ? (q_bf16 ? 64 : kRound) : kRound * waves, per_cu = static_cast<int>(token.size());
     for (int n = 1; n <= most_splits(p.tile_rows, tiles, span); ++n) {
       const long long chunk = ((span + n - 1) / n + step - 1) / step * step;
       const long long groups = tiles * n, rounds = (groups + 256 * per_cu - 1) / (256 * per_cu);
       const int share = static_cast<int>(std::min<long long>(per_cu, (groups + 255) / 256));
       const double each = chunk * size * token.begin()[share - 1] * share;
-      const double cost = rounds * (setup + each) + (n > 1 ? 3500 + merge * row_ns * n : 0);
+      const double cost = rounds * (setup + each) + (n > 1 ? split + merge * row_ns * n : 0);
       if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n;
     }
   };
-  if (tiled) {
-    consider(4, 8000, {40}, 10);
+  if (tiled && q_bf16) {
+    consider(4, 10000, {29, 23}, 25000, 19);
+  } else if (tiled) {
+    consider(4, 10000, {62}, 25000, 19);
   } else if (p.tile_rows == 32) {
-    consider(4, 10000, {13}, 10);
-    consider(8, 10000, {8.5}, 10);
+    consider(4, 10000, {13}, 3500, 10);
+    consider(8, 10000, {8.5}, 3500, 10);
   } else if (q_bf16) {
-    consider(4, 6500, {9, 6.2, 5.7}, 10);
-    consider(12, 7000, {5.8}, 5);
+    consider(4, 6500, {9, 6.2, 5.7}, 3500, 10);
+    consider(12, 7000, {5.8}, 3500, 5);
   } else {
-    consider(4, 6500, {9.9, 8}, 10);
-    consider(8, 7000, {7.5}, 5);
+    consider(4, 6500, {9.9, 8}, 3500, 10);
+    consider(8, 7000, {7.5}, 3500, 5);
   }
   // the counters of all shapes lie at the workspace's start; its size covers
   // every window and type
