@@ -375,14 +375,15 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
       const long long groups = tiles * n, rounds = (groups + 256 * per_cu - 1) / (256 * per_cu);
       const int share = static_cast<int>(std::min<long long>(per_cu, (groups + 255) / 256));
       const double each = chunk * size * token.begin()[share - 1] * share;
-      const double cost = rounds * (setup + each) + (n > 1 ? split + merge * row_ns * n : 0);
+      const double words = groups * row_ns * (head_dim + 2);  // of the partials, 1.2 TB/s
+      const double cost = rounds * (setup + each) + (n > 1 ? split + merge * row_ns * n + words / 300 : 0);
       if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n;
     }
   };
   if (tiled && q_bf16) {
-    consider(4, 10000, {29, 23}, 25000, 19);
+    consider(4, 10000, {29, 23}, 10000, 19);
   } else if (tiled) {
-    consider(4, 10000, {62}, 25000, 19);
+    consider(4, 10000, {62}, 10000, 19);
   } else if (p.tile_rows == 32) {
     consider(4, 10000, {13}, 3500, 10);
     consider(8, 10000, {8.5}, 3500, 10);
