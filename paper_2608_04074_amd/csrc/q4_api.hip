@@ -166,8 +166,8 @@ nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nov
     if (!q || !seq_lens || !out) return fail(NOVA_KV_ERR_INVALID_ARG, "q, seq_lens or out is NULL");
     if (!aligned(q, 16) || !aligned(out, 16)) return fail(NOVA_KV_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
     const long long rows = static_cast<long long>(n_q) * (num_q_heads / cache->num_kv_heads);
-    // rows of a unit and workgroups of a launch (256 threads each) are counted in 32 bits
-    if (rows > (1 << 24) || static_cast<long long>(batch) * cache->num_kv_heads * ((rows + 15) / 16) > (1 << 23))
+    // rows of a unit and threads of a launch (768 a tile) are counted in 32 bits
+    if (rows > (1 << 24) || static_cast<long long>(batch) * cache->num_kv_heads * ((rows + 15) / 16) > (1 << 22))
       return fail(NOVA_KV_ERR_UNSUPPORTED, "too many query rows in a call");
     const novakv::Q4AttnPlan plan = novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim,
                                                          q_dtype == NOVA_KV_BF16, max_seq_len, window);

@@ -59,11 +59,26 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   const int tw = wave % WT, rw = wave / WT;
 
   Tile g;
-  if (!find_tile(a, kRows, kRound * WT, g)) return;
+  place_tile(a, kRows, g);
+  // The queries are requested first: nothing of them waits for the sequence's
+  // length. (Rows past the sequence's own are padding, whatever they hold.)
+  const int row0 = g.row0 + rw * 16 * NT;
+  uint4 qraw[NT][kKeyWords][WIDE ? 2 : 1];
+  for (int t = 0; t < NT; ++t) {
+    const int row = row0 + 16 * t + n, i = row / a.gqa, h = row - i * a.gqa;
+    const size_t at = ((static_cast<size_t>(g.b) * a.n_q + i) * a.num_q_heads + g.kv * a.gqa + h) * D + 8 * kKeyWords * j;
+    for (int s = 0; s < kKeyWords; ++s)
+      for (int y = 0; y < (WIDE ? 2 : 1); ++y) {
+        qraw[t][s][y] = make_uint4(0u, 0u, 0u, 0u);
+        if (i < a.n_q)
+          qraw[t][s][y] = WIDE ? reinterpret_cast<const uint4 *>(static_cast<const float *>(a.q) + at + 8 * s)[y]
+                               : *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 8 * s);
+      }
+  }
+  if (!find_span(a, kRows, kRound * WT, g)) return;
   const int b = g.b, kv = g.kv, rows_valid = g.rows_valid, lo = g.lo, t0 = g.t0, t1 = g.t1;
 
   // this wave's rows
-  const int row0 = g.row0 + rw * 16 * NT;
   const int row1 = min(row0 + 16 * NT, rows_valid);
   const bool idle = row0 >= rows_valid;
   const int inner_lo = idle ? 0 : g.first_pos(a, row1 - 1), inner_hi = idle ? 0 : g.last_pos(a, row0) + 1;
@@ -155,28 +170,21 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + 16 * t + n;
     const bool on = row < rows_valid;
-    const int i = row / a.gqa, h = row - i * a.gqa;
     row_hi[t] = on ? g.last_pos(a, row) + 1 : 0;
     row_lo[t] = on ? g.first_pos(a, row) : 0;
     float x[kKeyWords][8];
     float top = 0.f;
     bool finite = true;
-    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + h) * D + 8 * kKeyWords * j;
     for (int s = 0; s < kKeyWords; ++s) {
-      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-      if (on) {
-        if constexpr (!WIDE) {
-          const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at + 8 * s);
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-          for (int e = 0; e < 4; ++e) {
+      for (int y = 0; y < (WIDE ? 2 : 1); ++y) {
+        const uint32_t u[4] = {qraw[t][s][y].x, qraw[t][s][y].y, qraw[t][s][y].z, qraw[t][s][y].w};
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (WIDE) {
+            x[s][4 * y + e] = __uint_as_float(u[e]);
+          } else {
             x[s][2 * e] = __uint_as_float(u[e] << 16);
             x[s][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
           }
-        } else {
-          const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at + 8 * s);
-          const float4 u = f[0], v = f[1];
-          x[s][0] = u.x, x[s][1] = u.y, x[s][2] = u.z, x[s][3] = u.w;
-          x[s][4] = v.x, x[s][5] = v.y, x[s][6] = v.z, x[s][7] = v.w;
         }
       }
       for (int e = 0; e < 8; ++e) {

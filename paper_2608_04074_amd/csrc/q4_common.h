@@ -91,9 +91,9 @@ struct Tile {
   }
 };
 
-// False: the tile has no rows. `step`: tokens that a split is a multiple of.
-// Consecutive tiles, which read the same rows and pages, run on one XCD.
-__device__ __forceinline__ bool find_tile(const Q4AttnArgs &a, const int rows, const int step, Tile &g) {
+// The workgroup's place. Consecutive tiles, which read the same rows and pages,
+// run on one XCD.
+__device__ __forceinline__ void place_tile(const Q4AttnArgs &a, const int rows, Tile &g) {
   int wg = lut::xcd_contiguous(blockIdx.x, gridDim.x);
   g.split = wg % a.n_split;
   wg /= a.n_split;
@@ -101,10 +101,14 @@ __device__ __forceinline__ bool find_tile(const Q4AttnArgs &a, const int rows, c
   g.unit = wg / a.row_tiles;
   g.b = g.unit / a.num_kv_heads;
   g.kv = g.unit - g.b * a.num_kv_heads;
+  g.row0 = g.tile * rows;
+}
+// Its rows and tokens; false: the tile has no rows. `step`: tokens that a split is
+// a multiple of.
+__device__ __forceinline__ bool find_span(const Q4AttnArgs &a, const int rows, const int step, Tile &g) {
   g.S = min(max(a.seq_lens[g.b], 0), a.max_seq_len);
   g.nb = a.q_lens ? min(max(a.q_lens[g.b], 0), a.n_q) : a.n_q;
   g.rows_valid = g.nb * a.gqa;
-  g.row0 = g.tile * rows;
   if (g.row0 >= g.rows_valid) return false;
   g.row1 = min(g.row0 + rows, g.rows_valid);
   g.lo = g.first_pos(a, g.row0);

@@ -56,7 +56,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const int group = wave >> 1, part = wave & 1;  // the wave unpacks 16 keys and half of the coordinates of 32 values
   Tile g;
-  if (!find_tile(a, Lds::kRows, kTokens, g)) return;
+  place_tile(a, Lds::kRows, g);
+  if (!find_span(a, Lds::kRows, kTokens, g)) return;
   const int b = g.b, kv = g.kv;
   const int row0 = g.row0 + 16 * kRowTiles * wave, row1 = min(row0 + 16 * kRowTiles, g.rows_valid);
   const bool idle = row0 >= g.rows_valid;
