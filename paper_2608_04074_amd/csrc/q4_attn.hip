@@ -27,7 +27,8 @@ namespace {
 
 using namespace q4;
 
-constexpr int kRound = 32;    // tokens a wave takes at a time
+constexpr int kRound = 32;  // tokens a wave takes at a time
+
 // D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows a wave. W: waves of a
 // workgroup. TILED: each wave has rows of its own and all tokens, else the waves
 // share the rows and divide the tokens. ALIGNED: blocks of a multiple of 16 rows.
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
 
     const bool inner = valid == 0xffffffffu && tb >= inner_lo && tb + kRound <= inner_hi;
     float top_vs = 0x1p-100f;
-    for (int e = 0; e < 8; ++e) top_vs = fmaxf(top_vs, vs[e]);
+    for (int e = 0; e < 8; ++e) top_vs = fmaxf(top_vs, fabsf(vs[e]));
     const float log_vs = __builtin_amdgcn_logf(top_vs);
     int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
     for (int h = 0; h < 2; ++h)

@@ -336,3 +336,53 @@ def test_repeatable(nk):
     ref = nk.q4_attn(cache, q, seq, 20000)
     for _ in range(20):
         assert torch.equal(nk.q4_attn(cache, q, seq, 20000), ref)
+
+
+def test_two_graphs_share_a_workspace(nk):
+    """Graphs of calls of different shapes (whole rows, tiles of rows) on one workspace, replayed in turn with eager
+    calls between them."""
+    rng = np.random.default_rng(12)
+    cache, _ = make_cache(nk, rng, [3000, 2500], 2, 64, 16)
+    seq = torch.tensor([3000, 2500], dtype=torch.int32, device="cuda")
+    qs = [torch.as_tensor(rng.standard_normal((2, n, 16, 64))).to(dt).cuda() for n, dt in ((1, BF), (3, F32), (20, BF), (9, F32))]
+    ws = torch.zeros(max(nk.q4_attn_workspace_bytes(cache, 2, q.shape[1], 16, 3000) for q in qs), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty_like(q) for q in qs]
+    graphs = []
+    for q, out in zip(qs, outs):
+        nk.q4_attn(cache, q, seq, 3000, out=out, workspace=ws)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            nk.q4_attn(cache, q, seq, 3000, out=out, workspace=ws)
+        graphs.append(g)
+    for r in range(3):
+        for q in qs:
+            q.copy_(torch.as_tensor(rng.standard_normal(tuple(q.shape))).to(q.dtype))
+        for i in rng.permutation(4):
+            outs[i].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], nk.q4_attn(cache, qs[i], seq, 3000)), f"round {r}, graph {i}"
+            nk.q4_attn(cache, qs[0], seq, 3000, workspace=ws)
+
+
+def test_refusals(nk):
+    rng = np.random.default_rng(13)
+    cache, _ = make_cache(nk, rng, [100], 2, 64, 16)
+    q = torch.zeros((1, 3, 8, 64), dtype=BF, device="cuda")
+    seq = torch.tensor([100], dtype=torch.int32, device="cuda")
+    cases = [
+        (ValueError, dict(q=q[0])), (ValueError, dict(q=q[..., :32])), (TypeError, dict(q=q.half())), (ValueError, dict(q=q.transpose(1, 2))),
+        (TypeError, dict(seq_lens=seq.long())), (ValueError, dict(seq_lens=seq.cpu())), (ValueError, dict(seq_lens=seq.expand(2).contiguous())),
+        (ValueError, dict(q=q.expand(2, -1, -1, -1).contiguous(), seq_lens=seq.expand(2).contiguous())),   # the table holds one sequence
+        (TypeError, dict(out=q.float())), (ValueError, dict(out=q[:, :2].contiguous())), (ValueError, dict(sinks=torch.zeros(7, device="cuda"))),
+        (ValueError, dict(q_lens=seq.expand(2).contiguous())), (nk.NovaKVError, dict(max_seq_len=10 ** 6)), (nk.NovaKVError, dict(window=-1)),
+        (nk.NovaKVError, dict(softmax_scale=-1.0)), (TypeError, dict(workspace=torch.zeros(4, device="cuda"))),
+        (nk.NovaKVError, dict(q=torch.zeros(q.numel() + 4, dtype=BF, device="cuda")[4:].view(q.shape))),   # 8-byte aligned
+        (nk.NovaKVError, dict(q=torch.zeros((1, 3, 7, 64), dtype=BF, device="cuda"))),                     # 7 query heads, 2 KV heads
+    ]
+    for error, change in cases:
+        args = dict(q=q, seq_lens=seq, max_seq_len=100)
+        args.update(change)
+        with pytest.raises(error):
+            nk.q4_attn(cache, **args)
+    assert nk.q4_attn(cache, q[:, :0], seq, 100).shape == (1, 0, 8, 64)

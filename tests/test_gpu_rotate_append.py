@@ -340,3 +340,34 @@ def test_append_then_attend(nk):
         keep(held, np.ones(B, dtype=np.int64))
         expect(qr, [1] * B, out)
     assert start.tolist() == lens.tolist()
+
+
+def test_refusals(nk):
+    rng = np.random.default_rng(8)
+    q, k, v = heads_of(rng, 2, 3, 8, 2, 64, BF, True)
+    rot = rotary_of(nk, rng, 8, 2, 64, 64, False, "shared")
+    cache = nk.Q4Cache.zeros(nk.CacheLayout.contiguous(16), 2, 2, 64)
+    start = i32([0, 1])
+    dense = q.contiguous()
+    cases = [
+        (TypeError, dict(k=k.float())), (TypeError, dict(q=q.half())), (ValueError, dict(k=k[:, :, :1])), (ValueError, dict(v=v.transpose(1, 2))),
+        (ValueError, dict(q=q[..., :32])), (ValueError, dict(q=dense.transpose(2, 3).contiguous().transpose(2, 3))),
+        (TypeError, dict(start_pos=start.long())), (ValueError, dict(start_pos=i32([0]))), (ValueError, dict(new_lens=i32([0]))),
+        (ValueError, dict(q_out=q)), (TypeError, dict(q_out=dense.float())), (ValueError, dict(q_out=dense[:, :1].contiguous())),
+        (ValueError, dict(start_pos=start.cpu())), (nk.NovaKVError, dict(q=dense[:, :, :].clone(), start_pos=None)),
+    ]
+    for error, change in cases:
+        for append in (False, True):
+            args = dict(q=q, k=k, v=v, start_pos=start)
+            args.update(change)
+            with pytest.raises(error):
+                nk.q4_append(rot, cache, **args) if append else nk.rotate_qkv(rot, **args)
+    with pytest.raises(nk.NovaKVError):
+        nk.rotate_qkv(rot, dense, None, None, start, q_out=torch.zeros(dense.numel() + 1, dtype=BF, device="cuda")[1:].view(dense.shape))
+    buf = torch.zeros(2 * dense.numel(), dtype=BF, device="cuda")
+    with pytest.raises(nk.NovaKVError, match="overlaps"):
+        nk.rotate_qkv(rot, buf[:dense.numel()].view(dense.shape), None, None, start, q_out=buf[64:64 + dense.numel()].view(dense.shape))
+    with pytest.raises(nk.NovaKVError):       # another head_dim than the cache's
+        nk.q4_append(nk.Rotary(8, 2, 128), cache, None, torch.zeros((2, 1, 2, 128), device="cuda"), torch.zeros((2, 1, 2, 128), device="cuda"), start)
+    with pytest.raises(ValueError):
+        nk.rotate_qkv(rot, None, None, None, start)

@@ -4,6 +4,9 @@ Every call here is rejected by the host-side checks (or is a no-op) before any
 HIP call, so nothing touches a device."""
 
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -154,3 +157,16 @@ def test_binding_refusals():
             call()
     assert nk.q4_code_shape(8, 128, nk.CacheLayout(16, 4), 2) == (8, 8, 16, 64)
     assert nk.q4_sq_shape(8, nk.CacheLayout(16, 4), 2, 11) == (11, 8, 16, 2)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ is not installed")
+def test_checks_under_sanitizers(tmp_path):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = tmp_path / "q4_checks"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-I", os.path.join(root, "include"),
+                    os.path.join(root, "paper_2608_04074_amd", "csrc", "host_checks.cpp"),
+                    os.path.join(root, "tests", "asan", "q4_checks_driver.cpp"), "-o", str(exe)], check=True)
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0:verify_asan_link_order=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=300)
+    assert r.returncode == 0, r.stderr[-4000:]
