@@ -20,13 +20,13 @@ constexpr int kThreads = 256;
 // Value of another lane of the 16-lane row (DPP).
 template <int CTRL>
 __device__ __forceinline__ float dpp(const float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
 template <int CTRL>
 __device__ __forceinline__ double dpp(const double x) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xf, 0xf, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xf, 0xf, false);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp(static_cast<int>(u), CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp(static_cast<int>(u >> 32), CTRL, 0xf, 0xf, true);
   return __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
 }
 
@@ -44,9 +44,6 @@ __device__ __forceinline__ T reduce_row(T x, F f) {
 __device__ __forceinline__ uint32_t bf16_rne(const float x) {  // finite x (or overflow to infinity)
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-}
-__device__ __forceinline__ uint32_t bf16_any(const float x) {
-  return x != x ? 0x7fc0u : bf16_rne(x);
 }
 
 // Four consecutive elements as they lie (VEC: aligned to their 8 or 16 bytes),
@@ -70,12 +67,13 @@ __device__ __forceinline__ void to_floats(const uint2 w, float *x) {
 }
 __device__ __forceinline__ void to_floats(const float4 w, float *x) { x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w; }
 template <bool BF16>
-__device__ __forceinline__ void store4(void *p, const long long i, const float *x) {
+__device__ __forceinline__ void store4(char *p, const float *x) {
   if constexpr (BF16) {
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + i) =
-        make_uint2(bf16_any(x[0]) | (bf16_any(x[1]) << 16), bf16_any(x[2]) | (bf16_any(x[3]) << 16));
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4 *>(p) =
+        bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])};
   } else {
-    *reinterpret_cast<float4 *>(static_cast<float *>(p) + i) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
   }
 }
 
@@ -104,11 +102,11 @@ __device__ __forceinline__ void norm_rotate(T *y, const float *w, const bool nor
   }
 }
 
-// A row's 4-bit codes and its scale and offset in a word, everything that decides
+// A row's 4-bit codes (clamped by the caller) and its scale and offset in a word, everything that decides
 // them in fp64, so that they do not depend on how a sum is ordered.
 template <int D, bool IL>
 __device__ __forceinline__ void quantize_wide(const float *x, const float *w, const bool norm, const float eps, const float *cs,
-                                              const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+                                              const float *sn, const bool turns, float *code, uint32_t &sq) {
   double y[8];
   bool odd = false;
   for (int j = 0; j < 8; ++j) y[j] = x[j];
@@ -136,7 +134,7 @@ __device__ __forceinline__ void quantize_wide(const float *x, const float *w, co
     const bool c_odd = (static_cast<int>(fmin(fmax(c, -1.), 16.)) & 1) != 0;
     if (rem > 0.5 * step || (rem == 0.5 * step && c_odd)) c += 1;
     if (rem < -0.5 * step || (rem == -0.5 * step && c_odd)) c -= 1;
-    code[j] = nan || step == 0 ? 0u : static_cast<uint32_t>(fmin(fmax(c, 0.), 15.));
+    code[j] = nan || step == 0 ? 0.f : static_cast<float>(fmin(fmax(c, 0.), 15.));
   }
   sq = sc | (of << 16);
 }
@@ -158,49 +156,47 @@ __device__ __forceinline__ bool near_bf16_border(const float v, const float off)
 // 30 u m. Below 32 u m = 2^-19 m all told; values are exact.
 template <int D, bool IL>
 __device__ __forceinline__ bool quantize_fast(const float *x, const float *w, const bool norm, const float eps, const float *cs,
-                                              const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+                                              const float *sn, const bool turns, float *code, uint32_t &sq) {
   float y[8];
   for (int j = 0; j < 8; ++j) y[j] = x[j];
   norm_rotate<D, IL, float>(y, w, norm, eps, cs, sn, turns);
-  float lo = y[0], hi = y[0];
+  float lo = y[0], hi = y[0], all = y[0];  // all: not finite where a coordinate is not (or the sum overflows)
   for (int j = 1; j < 8; ++j) {
     lo = fminf(lo, y[j]);
     hi = fmaxf(hi, y[j]);
+    all += y[j];
   }
-  float total = 0.f;  // NaN where a coordinate is not finite
-  for (int j = 0; j < 8; ++j) total += y[j] * 0.f;
   lo = reduce_row<D / 8>(lo, [](float p, float q) { return fminf(p, q); });
   hi = reduce_row<D / 8>(hi, [](float p, float q) { return fmaxf(p, q); });
   const float m = fmaxf(fabsf(lo), fabsf(hi));
   const float off = norm || turns ? m * 0x1p-19f : 0.f;
   const float range = hi - lo, scale32 = range * (1.f / 15.f);
   // the roundings of the range, of 1/15 and of their product: below 4 u
-  bool sure = total == 0.f && !near_bf16_border(scale32, 2.f / 15.f * off + scale32 * 0x1p-22f);
+  bool sure = all - all == 0.f && !near_bf16_border(scale32, 2.f / 15.f * off + scale32 * 0x1p-22f);
   sure = sure && (off == 0.f ? (__builtin_bit_cast(uint32_t, lo) & 0x7f800000u) < 0x7f000000u : !near_bf16_border(lo, off));
   const uint32_t sc = bf16_rne(scale32), of = bf16_rne(lo);
   const float step = bf16_bits_to_float(sc), offset = bf16_bits_to_float(of);
   const float inv = __builtin_amdgcn_rcpf(step);
-  // a remainder so near half a step that y's error, or the subtraction's, may have decided
-  const float near = off + 0x1p-20f * step;
+  sq = sc | (of << 16);
+  float u[8], worst = 0.f;
   for (int j = 0; j < 8; ++j) {
-    const float u = y[j] - offset;
-    const float c = rintf(u * inv);
-    const float rem = __builtin_fmaf(-c, step, u);
-    const float beyond = fabsf(rem) - 0.5f * step;
-    if (fabsf(beyond) <= near) {
+    u[j] = y[j] - offset;
+    code[j] = rintf(u[j] * inv);
+    worst = fmaxf(worst, fabsf(__builtin_fmaf(-code[j], step, u[j])));
+  }
+  // a remainder so near half a step that y's error, or the subtraction's (of at
+  // most 16 steps), may have decided
+  const float near = off + 0x1p-20f * step;
+  if (!(worst < 0.5f * step - near)) {
+    for (int j = 0; j < 8; ++j) {
+      const float c = code[j], rem = __builtin_fmaf(-c, step, u[j]), beyond = fabsf(rem) - 0.5f * step;
+      if (beyond < -near || c < -1.f || c > 16.f) continue;
       // exact where the subtraction was (and y is): then a tie goes to the even code
-      const float bb = u - y[j], lost = (y[j] - (u - bb)) - (offset + bb);
-      const bool exact = off == 0.f && lost == 0.f;
-      float d = c;
-      if (beyond > 0.f || (beyond == 0.f && (static_cast<int>(c) & 1))) d += rem > 0.f ? 1.f : -1.f;
-      sure = sure && (exact || c < -1.f || c > 16.f);
-      code[j] = static_cast<uint32_t>(fminf(fmaxf(d, 0.f), 15.f));
-    } else {
-      sure = sure && beyond < 0.f;  // the quotient's own rounding is far below `near`
-      code[j] = static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
+      const float bb = u[j] - y[j], lost = (y[j] - (u[j] - bb)) - (offset + bb);
+      sure = sure && off == 0.f && lost == 0.f && beyond <= near;
+      if (beyond > 0.f || (beyond == 0.f && (static_cast<int>(c) & 1))) code[j] += rem > 0.f ? 1.f : -1.f;
     }
   }
-  sq = sc | (of << 16);
   return sure;
 }
 
@@ -208,7 +204,7 @@ __device__ __forceinline__ bool quantize_fast(const float *x, const float *w, co
 // (the other rows' results are the same). 32 x 4096 tokens: 788 us, 1568 us all in fp64.
 template <int D, bool IL>
 __device__ __forceinline__ void quantize(const float *x, const float *w, const bool norm, const float eps, const float *cs,
-                                         const float *sn, const bool turns, uint32_t *code, uint32_t &sq) {
+                                         const float *sn, const bool turns, float *code, uint32_t &sq) {
   const bool sure = quantize_fast<D, IL>(x, w, norm, eps, cs, sn, turns, code, sq);
   // every lane of a row takes the same way: its codes and its scale belong together
   if (reduce_row<D / 8>(sure ? 0.f : 1.f, [](float p, float q) { return fmaxf(p, q); }) != 0.f)
@@ -233,6 +229,10 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     return static_cast<const char *>(r.data) + (b * r.batch_stride + i * r.token_stride) * kElem;
   };
   const char *const q_rows = rows_of(a.q), *const k_rows = rows_of(a.k), *const v_rows = rows_of(a.v);
+  auto outs_of = [&](void *out, const int n_heads) {
+    return out ? static_cast<char *>(out) + static_cast<long long>(tok) * n_heads * (D * kElem) : nullptr;
+  };
+  char *const q_out = outs_of(a.q_out, a.nq), *const k_out = outs_of(a.k_out, a.nk), *const v_out = outs_of(a.v_out, a.nv);
   struct Row {
     int side, head;  // 0: query, 1: key, 2: value; -1: none
     Raw4<BF16> x[2];
@@ -282,21 +282,25 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
       to_floats(load4<false, true>(weight + c0), w);
       to_floats(load4<false, true>(weight + c1), w + 4);
     }
-    void *out = side == 0 ? a.q_out : side == 1 ? a.k_out : a.v_out;
-    const long long to = (static_cast<long long>(tok) * (side == 0 ? a.nq : side == 1 ? a.nk : a.nv) + hh) * D;
+    char *out = side == 0 ? q_out : side == 1 ? k_out : v_out;
+    const int to0 = (hh * D + c0) * kElem, to1 = (hh * D + c1) * kElem;
     if (!Q4 || side == 0) {
       norm_rotate<D, IL, float>(x, w, weight != nullptr, a.eps, cs, sn, turns && side < 2);
-      store4<BF16>(out, to + c0, x);
-      store4<BF16>(out, to + c1, x + 4);
+      store4<BF16>(out + to0, x);
+      store4<BF16>(out + to1, x + 4);
       continue;
     }
-    uint32_t code[8], sq;
+    float code[8];
+    uint32_t sq;
     if constexpr (FAST) quantize<D, IL>(x, w, weight != nullptr, a.eps, cs, sn, turns && side == 1, code, sq);
     else quantize_wide<D, IL>(x, w, weight != nullptr, a.eps, cs, sn, turns && side == 1, code, sq);
     const size_t row = row0 + static_cast<size_t>(hh) * a.layout.block_size;
     uint8_t *dst = (side == 1 ? a.k_codes : a.v_codes) + row * (D / 2);
-    uint32_t packed = 0;
-    for (int j = 0; j < 8; ++j) packed |= code[j] << (4 * j);
+    for (int j = 0; j < 8; ++j) code[j] = __builtin_amdgcn_fmed3f(code[j], 0.f, 15.f);
+    auto four = [](const float *c) {  // 16 bits, exact in fp32
+      return static_cast<uint32_t>(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3], 16.f, c[2]), 16.f, c[1]), 16.f, c[0]));
+    };
+    const uint32_t packed = four(code) | (four(code + 4) << 16);
     // Stores of four bytes: a lane's chunks follow each other, or (halves) two
     // neighbours exchange one, the even lane storing both lower chunks.
     if (IL || !turns) {
@@ -312,9 +316,9 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     if (lane == 0) *reinterpret_cast<uint32_t *>((side == 1 ? a.k_sq : a.v_sq) + 2 * row) = sq;
     if (out) {
       const float scale = bf16_bits_to_float(sq & 0xffffu), offset = bf16_bits_to_float(sq >> 16);
-      for (int j = 0; j < 8; ++j) x[j] = scale * static_cast<float>(code[j]) + offset;
-      store4<BF16>(out, to + c0, x);
-      store4<BF16>(out, to + c1, x + 4);
+      for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(scale, code[j], offset);
+      store4<BF16>(out + to0, x);
+      store4<BF16>(out + to1, x + 4);
     }
   }
 }
