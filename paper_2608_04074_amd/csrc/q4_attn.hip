@@ -42,14 +42,16 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   constexpr float kTopQ = WIDE ? 127.f * 128 * 128 : 127.f * 128;  // the largest fixed-point number
   constexpr int kProbParts = WIDE ? 3 : 1;  // and of a probability
   // log2 of the largest scaled probability after a rescale, and how far it may
-  // grow before the next one: 2^14 fits fp16, 2^11 units of 1 are 11 bits
+  // grow before the next one: 2^14 fits fp16, 2^11 units of 1 are 11 bits. Scaled
+  // by the value's scale or, where that is less, 2^-8 of its offset's magnitude (of
+  // code 8), at least 2^-70: sums of probabilities and of offsets stay in range too.
   constexpr float kTop = WIDE ? 10.f : 6.f, kSlack = WIDE ? 1.f : 8.f;
   constexpr int kRowGroups = kWaves / WT; // waves on rows of their own
   constexpr int kRows = 16 * NT * kRowGroups;
   using Lds = FinishLds<D, NT, W, TILED>;
 
   __shared__ __align__(16) uint32_t s_rows[ALIGNED ? 1 : kWaves][kRound];
-  __shared__ __align__(16) float s_scale[kWaves][2 * kRound], s_offset[kWaves][2 * kRound];
+  __shared__ __align__(16) float s_scale[kWaves][2 * kRound], s_offset[kWaves][2 * kRound], s_log[kWaves][2 * kRound];
   __shared__ float s_ref[kWaves][16 * NT], s_sum[kWaves][16 * NT];
   __shared__ __align__(16) float s_merge[Lds::kMerge];
   __shared__ float s_inv[kRows];
@@ -230,6 +232,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
       if (lane >= 32) offset = __builtin_fmaf(8.f, scale, offset);  // values count from code 8
       s_scale[wave][lane] = cur.ok ? scale : 0.f;
       s_offset[wave][lane] = cur.ok ? offset : 0.f;
+      s_log[wave][lane] = __builtin_amdgcn_logf(fmaxf(fmaxf(fabsf(scale), fabsf(offset) * 0x1p-8f), 0x1p-70f));
     }
     __builtin_amdgcn_wave_barrier();
     // of the lane's 8 tokens, 4j + i and 16 + 4j + i, as its scores have them
@@ -246,9 +249,6 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     __builtin_amdgcn_wave_barrier();
 
     const bool inner = valid == 0xffffffffu && tb >= inner_lo && tb + kRound <= inner_hi;
-    float top_vs = 0x1p-100f;
-    for (int e = 0; e < 8; ++e) top_vs = fmaxf(top_vs, fabsf(vs[e]));
-    const float log_vs = __builtin_amdgcn_logf(top_vs);
     int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
     for (int h = 0; h < 2; ++h)
       for (int s = 0; s < kKeyWords; ++s) {
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
           d[h][x] = int4_t{0, 0, 0, 0};
           for (int s = 0; s < kSteps; ++s) d[h][x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[h][x], 0, 0, 0);
         }
-      float z[8], top = kNone, scale[8], offset[8];
+      float z[8], bound = kNone, scale[8], offset[8];
       for (int e = 0; e < 8; ++e) {
         const int4_t(&dig)[kDigits] = d[e >> 2];
         float dot = static_cast<float>((dig[1][e & 3] << 7) + dig[0][e & 3]);
@@ -281,8 +281,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
           offset[e] = seen ? offset[e] : 0.f;
         }
       }
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, z[e]);
-      const float bound = top * alpha[t] + log_vs;
+      for (int e = 0; e < 8; ++e)
+        bound = fmaxf(bound, __builtin_fmaf(z[e], alpha[t], s_log[wave][32 + 16 * (e >> 2) + 4 * j + (e & 3)]));
       if (__any(bound > ref[t] + (kTop + kSlack))) {
         const float most = max_rows32(max_rows16(bound));
         const float next = fmaxf(ref[t], most - kTop);

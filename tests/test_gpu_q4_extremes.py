@@ -1,0 +1,86 @@
+"""4-bit cache: values, keys and heads whose magnitudes lie far apart.
+
+Tolerances of attention are those of test_gpu_q4_attn.py, from what a row attends
+alone."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import q4
+from test_gpu_q4_attn import BF, F32, make_cache, nk, reference_and_bounds, say  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def put_values(cache, host, b, tokens, scale, offset):
+    """Scale and offset of the values of a sequence's tokens, in every KV head."""
+    vsq, where = host[3], host[4]
+    phys, row = (x[tokens] for x in where[b])
+    vsq[phys, :, row] = q4.to_bf16_bits(np.array([scale, offset]))
+    cache.v_sq.copy_(torch.as_tensor(vsq.view(np.int16)).cuda().view(torch.bfloat16))
+
+
+def assert_within(nk, cache, host, q, seqs, window=0):
+    n, D = q.shape[1], q.shape[3]
+    out = nk.q4_attn(cache, q, torch.tensor(seqs, dtype=torch.int32, device="cuda"), max(seqs), window=window)
+    ref, tol = reference_and_bounds(host, q.double().cpu().numpy(), seqs, [n] * len(seqs), window, None, 1 / math.sqrt(D),
+                                    q.dtype == BF)
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert (np.abs(got - ref) <= tol).all(), f"{(np.abs(got - ref) - tol).max():.3e} over the bound"
+
+
+@pytest.mark.parametrize("dtype", (BF, F32))
+@pytest.mark.parametrize("n", (1, 5, 40))
+@pytest.mark.parametrize("value", (0.0, -1000.0, 1e25, 1e-25))
+def test_constant_values(nk, value, n, dtype):  # noqa: F811
+    """Every value row is one constant (scale 0), while later logits grow."""
+    say(f"constant values {value} n={n} {dtype}")
+    rng = np.random.default_rng(11)
+    seqs = [3000, 65]
+    cache, host = make_cache(nk, rng, seqs, 2, 64, 16)
+    for b, S in enumerate(seqs):
+        put_values(cache, host, b, np.arange(S), 0.0, value)
+    q = torch.as_tensor(3 * rng.standard_normal((2, n, 8, 64))).to(dtype).cuda()
+    assert_within(nk, cache, host, q, seqs)
+
+
+@pytest.mark.parametrize("dtype,n,Hq", ((BF, 1, 8), (BF, 4, 8), (BF, 16, 4), (F32, 4, 8), (F32, 40, 8)))
+@pytest.mark.parametrize("size", (1e4, 1e12, 1e30))
+def test_hidden_tokens_with_large_values(nk, size, dtype, n, Hq):  # noqa: F811
+    """Tokens that some of a call's rows do not attend, with values far above the others'.
+    (In front of the window, and behind the first queries.)"""
+    say(f"hidden large values {size} n={n} heads={Hq} {dtype}")
+    rng = np.random.default_rng(12)
+    seqs = [100, 47]
+    cache, host = make_cache(nk, rng, seqs, 2, 128, 16)
+    for b, S in enumerate(seqs):
+        put_values(cache, host, b, np.array([S - 20 - n, S - 1] if n > 1 else [S - 21]), size, -3 * size)
+    q = torch.as_tensor(rng.standard_normal((2, n, Hq, 128))).to(dtype).cuda()
+    assert_within(nk, cache, host, q, seqs, window=20)
+
+
+@pytest.mark.parametrize("dtype", (BF, F32))
+def test_large_values_of_little_weight(nk, dtype):  # noqa: F811
+    """A token whose value is 2^40 times the others' and whose probability is nothing."""
+    rng = np.random.default_rng(13)
+    S, D = 64, 64
+    cache, host = make_cache(nk, rng, [S], 1, D, 0)
+    kc, vc, ksq, vsq, _ = host
+    ksq[0, 0, :S] = q4.to_bf16_bits(np.array([0.0, 0.0]))
+    ksq[0, 0, 40] = q4.to_bf16_bits(np.array([0.0, -8.0]))  # its logit: -8 sum(q) / 8, -256
+    cache.k_sq.copy_(torch.as_tensor(ksq.view(np.int16)).cuda().view(torch.bfloat16))
+    put_values(cache, host, 0, np.array([40]), 2.0 ** 40, -2.0 ** 42)
+    q = torch.full((1, 1, 4, D), 4.0, dtype=dtype, device="cuda")
+    out = nk.q4_attn(cache, q, torch.tensor([S], dtype=torch.int32, device="cuda"), S).double().cpu().numpy()
+    keep = np.arange(S) != 40
+    v = q4.unpack_codes(vc[0, 0, :S]) * q4.from_bf16_bits(vsq[0, 0, :S, :1]) + q4.from_bf16_bits(vsq[0, 0, :S, 1:])
+    ref = v[keep].mean(0)
+    # its weight is e^-256 / 63, of an output 2^42 e^-256: nothing; the others are alike, exactly 1 / 63.
+    # Roundings: the output's; a probability's to fp16 (bf16 queries), the sum's 63 of fp32.
+    tol = np.abs(ref) * 2.0 ** (-8 if dtype == BF else -24) + np.abs(v[keep]).max() * (2.0 ** -11 if dtype == BF else 0) + \
+        np.abs(v[keep]).max() * 2.0 ** -18
+    assert (np.abs(out[0, 0] - ref) <= tol).all()
