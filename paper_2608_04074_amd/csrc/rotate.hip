@@ -77,15 +77,16 @@ __device__ __forceinline__ void store4(char *p, const float *x) {
   }
 }
 
-// Norm and rotation of a lane's 8 coordinates, in T.
+// Norm and rotation of a lane's 8 coordinates, in T; the mean square with eps (1 without a norm).
 template <int D, bool IL, typename T>
-__device__ __forceinline__ void norm_rotate(T *y, const float *w, const bool norm, const float eps, const float *cs,
-                                            const float *sn, const bool turns) {
+__device__ __forceinline__ T norm_rotate(T *y, const float *w, const bool norm, const float eps, const float *cs,
+                                         const float *sn, const bool turns) {
+  T v = 1;
   if (norm) {
     T ss = 0;
     for (int j = 0; j < 8; ++j) ss += y[j] * y[j];
     ss = reduce_row<D / 8>(ss, [](T a, T b) { return a + b; });
-    const T v = ss * static_cast<T>(1. / D) + static_cast<T>(eps);
+    v = ss * static_cast<T>(1. / D) + static_cast<T>(eps);
     T r;
     if constexpr (std::is_same_v<T, float>) r = v > 0x1p-100f ? __builtin_amdgcn_rsqf(v) : 1.f / sqrtf(v);  // within 2 u
     else r = 1 / sqrt(v);
@@ -100,6 +101,7 @@ __device__ __forceinline__ void norm_rotate(T *y, const float *w, const bool nor
       b = b * c + a0 * s;
     }
   }
+  return v;
 }
 
 // A row's 4-bit codes (clamped by the caller) and its scale and offset in a word, everything that decides
@@ -159,7 +161,7 @@ __device__ __forceinline__ bool quantize_fast(const float *x, const float *w, co
                                               const float *sn, const bool turns, float *code, uint32_t &sq) {
   float y[8];
   for (int j = 0; j < 8; ++j) y[j] = x[j];
-  norm_rotate<D, IL, float>(y, w, norm, eps, cs, sn, turns);
+  const float square = norm_rotate<D, IL, float>(y, w, norm, eps, cs, sn, turns);
   float lo = y[0], hi = y[0], all = y[0];  // all: not finite where a coordinate is not (or the sum overflows)
   for (int j = 1; j < 8; ++j) {
     lo = fminf(lo, y[j]);
@@ -173,6 +175,8 @@ __device__ __forceinline__ bool quantize_fast(const float *x, const float *w, co
   const float range = hi - lo, scale32 = range * (1.f / 15.f);
   // the roundings of the range, of 1/15 and of their product: below 4 u
   bool sure = all - all == 0.f && !near_bf16_border(scale32, 2.f / 15.f * off + scale32 * 0x1p-22f);
+  // squares, or the root's product with a weight, that left the normal numbers have lost more
+  sure = sure && (!norm || (square > 0x1p-100f && m > 0x1p-60f));
   sure = sure && (off == 0.f ? (__builtin_bit_cast(uint32_t, lo) & 0x7f800000u) < 0x7f000000u : !near_bf16_border(lo, off));
   const uint32_t sc = bf16_rne(scale32), of = bf16_rne(lo);
   const float step = bf16_bits_to_float(sc), offset = bf16_bits_to_float(of);

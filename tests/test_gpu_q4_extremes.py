@@ -84,3 +84,24 @@ def test_large_values_of_little_weight(nk, dtype):  # noqa: F811
     tol = np.abs(ref) * 2.0 ** (-8 if dtype == BF else -24) + np.abs(v[keep]).max() * (2.0 ** -11 if dtype == BF else 0) + \
         np.abs(v[keep]).max() * 2.0 ** -18
     assert (np.abs(out[0, 0] - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", (BF, F32))
+@pytest.mark.parametrize("key_size,weight", ((1e-21, 1.0), (1e-23, 1e4), (2.0 ** 30, 2.0 ** -100), (3e19, 1.0)))
+def test_norms_past_fp32(nk, key_size, weight, dtype):  # noqa: F811
+    """Keys whose squares, or weights whose products, leave the normal fp32 numbers: the codes
+    are those of fp64 all the same, of few tokens and of many."""
+    say(f"norms past fp32: keys {key_size} weight {weight} {dtype}")
+    rng = np.random.default_rng(15)
+    H, D = 2, 128
+    w = torch.full((D,), weight, device="cuda") * torch.as_tensor(rng.uniform(0.5, 1, D)).float().cuda()
+    rot = nk.Rotary(H, H, D, k_norm=w, eps=0.0)
+    for n in (3, 600):
+        cache = nk.Q4Cache.zeros(nk.CacheLayout.contiguous(n), 1, H, D)
+        k = torch.as_tensor(key_size * rng.standard_normal((1, n, H, D))).to(dtype).cuda()
+        nk.q4_append(rot, cache, None, k, k, torch.zeros(1, dtype=torch.int32, device="cuda"))
+        y = q4.norm_rotate(k.double().cpu().numpy(), w.double().cpu().numpy())
+        codes, sq, gap = q4.quantize_rows(y[0].transpose(1, 0, 2))
+        assert (cache.k_sq.view(torch.int16).cpu().numpy().view(np.uint16)[0] == sq).all()
+        got = q4.unpack_codes(cache.k_codes.cpu().numpy()[0])
+        assert ((got == codes) | (gap < 1e-9)).all()
