@@ -9,12 +9,14 @@
 // q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
 // of keys and values).
 //
-// Keys and values are divided by 2^9 times a power of two at or above the
+// Keys and values are divided by 2^7 times a power of two at or above the
 // largest magnitude of the 64 tokens (each side its own), which the exponent and
 // the output take back: a scale's and an offset's 8 bits then fit fp16, and one
 // packed multiply-add unpacks two codes (fp16 denormals as they lie, c * 2^-24)
-// with one rounding, at most 2^-12 of that power, below what bf16 queries and
-// outputs show (2^-9 of theirs).
+// with one rounding: half a step of fp16, 2^-12 of the power of two above the number,
+// or of the smallest normal one, 2^-18 of the largest magnitude, below. bf16 queries
+// and outputs show 2^-9 of theirs, so tokens up to 2^9 below the largest lose nothing.
+// (2^7 is the least that keeps 15 scales, at most four times the power, in fp16.)
 #include <type_traits>
 
 #include "q4_common.h"
@@ -30,12 +32,13 @@ constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability af
 
 // The same value in every lane, in a scalar register.
 __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
-// Exponent of a power of two above a magnitude (above a quarter of it beyond 2^126), from its bits.
+// Exponent of a power of two above a magnitude (at least 2^-90, so that sums of
+// probabilities over it stay in range; half of it beyond 2^127), from its bits.
 __device__ __forceinline__ int exponent_of(const float mag) {
   const int e = uniform(__builtin_bit_cast(int, mag)) >> 23;  // mag >= 0
-  return min(max(e - 126, -99), 126);
+  return min(max(e - 126, -90), 127);
 }
-__device__ __forceinline__ float power_of_two(const int e) { return __builtin_bit_cast(float, (e + 127) << 23); }
+__device__ __forceinline__ float power_of_two(const int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
 // ALIGNED: blocks of a multiple of 16 rows.
 template <int D, bool ALIGNED>
@@ -157,8 +160,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     const uint32_t any_odd = static_cast<uint32_t>(odds) | static_cast<uint32_t>(odds >> 32);
     const bool token_odd = (any_odd >> (lane & 31)) & 1u;
     const float unit = lane < 32 ? power_of_two(-ek) : power_of_two(-ev);
-    scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p15f);  // 15 s <= 2 / unit: below 2^13
-    offset = token_odd ? 0.f : offset * (unit * 0x1p-9f);
+    scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p17f);  // s <= 4 / 15 / unit: below 2^15.1
+    offset = token_odd ? 0.f : offset * (unit * 0x1p-7f);
     const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
     s_pack[wave][lane] = __builtin_bit_cast(uint32_t, both);
     __builtin_amdgcn_wave_barrier();
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     if (!idle && tb < wave_hi && tb + kTokens > wave_lo) {
       const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][0])), static_cast<uint32_t>(uniform(s_valid[slot0][1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
-      const float key_unit = power_of_two(ek) * 512.f, value_exp = static_cast<float>(ev), value_inv = power_of_two(-ev);
+      const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev), value_inv = power_of_two(-ev);
       if (!inner) {
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
         float top = kNone;
         for (int x = 0; x < 4; ++x)
           for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
-        by[t] = alpha[t] != alpha[t] ? alpha[t] : fmaxf(alpha[t] * key_unit, 0x1p-126f);
+        by[t] = alpha[t] != alpha[t] ? alpha[t] : fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f);
         bound[t] = top * by[t] + value_exp;
         over |= bound[t] > ref[t] + (kTop + kSlack);
       }
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
   for (int t = 0; t < kRowTiles; ++t) {
     sum[t] = add_rows32(add_rows16(sum[t]));
     if (sum[t] != sum[t]) ref[t] = fmaxf(ref[t], 0.f);  // NaN logits move no reference, but attend
-    for (int o = 0; o < kTiles; ++o) acc[t][o] *= 512.f;
+    for (int o = 0; o < kTiles; ++o) acc[t][o] *= 128.f;
   }
   finish_rows<D, kRowTiles, kWaves, true>(a, g, {reinterpret_cast<float *>(s_tokens), nullptr, nullptr, s_inv, &s_last}, wave, lane, acc, ref,
                                           sum);

@@ -86,6 +86,45 @@ def test_large_values_of_little_weight(nk, dtype):  # noqa: F811
     assert (np.abs(out[0, 0] - ref) <= tol).all()
 
 
+@pytest.mark.parametrize("n", (40, 70))
+@pytest.mark.parametrize("D", (64, 128))
+def test_tokens_far_below_their_neighbours(nk, n, D):  # noqa: F811
+    """Many bf16 queries over tokens of which every fourth is 2^8 times the others, with logits
+    that hide it: keys and values are rounded to 2^-12 of theirs, or 2^-18 of the largest around."""
+    say(f"far below n={n} D={D}")
+    rng = np.random.default_rng(14)
+    S, G = 200, 4
+    cache, host = make_cache(nk, rng, [S], 1, D, 16)
+    kc, vc, ksq, vsq, ((phys, row),) = host
+    large = np.arange(S) % 4 == 3
+    size = np.where(large, 2.0 ** 8, 1.0)
+    ksq[phys, 0, row] = q4.to_bf16_bits(np.stack([np.where(large, 0.0, 0.01), np.where(large, -64.0, 0.25)], -1))
+    vsq[phys, 0, row] = q4.to_bf16_bits(np.stack([0.25 * size, -1.5 * size], -1))
+    dev = lambda x: torch.as_tensor(x.view(np.int16)).cuda().view(torch.bfloat16)  # noqa: E731
+    cache.k_sq.copy_(dev(ksq))
+    cache.v_sq.copy_(dev(vsq))
+    q = torch.as_tensor(0.25 + 0.25 * rng.random((1, n, G, D))).to(BF).cuda()  # logits of large tokens: below -64 * 0.25 sqrt(D)
+    got = nk.q4_attn(cache, q, torch.tensor([S], dtype=torch.int32, device="cuda"), S).double().cpu().numpy()
+    qd = q.double().cpu().numpy()
+    # every row attends a token that is not large, whose weight e^-128 leaves of the large ones below 2^8 e^-128
+    k = q4.from_bf16_bits(ksq[phys, 0, row])
+    v = q4.from_bf16_bits(vsq[phys, 0, row])
+    kd = k[:, 1:] + k[:, :1] * q4.unpack_codes(kc[phys, 0, row])
+    vd = v[:, 1:] + v[:, :1] * q4.unpack_codes(vc[phys, 0, row])
+    small = ~large
+    for i in range(n):
+        at = np.flatnonzero(small & (np.arange(S) <= S - n + i))
+        z = qd[0, i] @ kd[at].T / np.sqrt(D)
+        p = np.exp(z - z.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        ref, V = p @ vd[at], np.abs(vd[at]).max()
+        # a key's coordinate is off by 2^-18 * 64, a logit by that times sum(q) / sqrt(D), a probability by twice that;
+        # a value by 2^-18 * 2.25 * 2^8; the output's rounding, a probability's, a sum's as elsewhere
+        dz = 2.0 ** -12 * qd[0, i].sum(-1, keepdims=True) / np.sqrt(D)
+        tol = np.abs(ref) * 2.0 ** -8 + 2 * dz * V + 2.25 * 2.0 ** -10 + V * (2.0 ** -11 + 2.0 ** -18)
+        assert (np.abs(got[0, i] - ref) <= tol).all(), (i, (np.abs(got[0, i] - ref) - tol).max())
+
+
 @pytest.mark.parametrize("dtype", (BF, F32))
 @pytest.mark.parametrize("key_size,weight", ((1e-21, 1.0), (1e-23, 1e4), (2.0 ** 30, 2.0 ** -100), (3e19, 1.0)))
 def test_norms_past_fp32(nk, key_size, weight, dtype):  # noqa: F811
