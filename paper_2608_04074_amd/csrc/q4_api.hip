@@ -23,6 +23,12 @@ nova_kv_status guarded(F f) {
   }
 }
 
+// The rows of a unit and the threads of a launch (768 a tile) are counted in 32 bits.
+bool too_many_rows(int32_t batch, int32_t n_q, int32_t num_q_heads, int32_t num_kv_heads) {
+  const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
+  return batch > 65535 || rows > (1 << 24) || ((rows + 15) / 16) * num_kv_heads > (1 << 22) / batch;
+}
+
 novakv::HeadRows to_rows(const nova_kv_rows *r) {
   return r ? novakv::HeadRows{r->data, r->batch_stride, r->token_stride} : novakv::HeadRows{nullptr, 0, 0};
 }
@@ -135,8 +141,9 @@ nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache
 
 size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t batch, int32_t n_q, int32_t num_q_heads,
                                        int32_t max_seq_len) {
-  if (!cache || batch <= 0 || n_q <= 0 || num_q_heads <= 0 || max_seq_len <= 0 || cache->num_kv_heads <= 0 ||
-      cache->head_dim <= 0 || num_q_heads % cache->num_kv_heads != 0)
+  if (!cache || batch <= 0 || n_q <= 0 || num_q_heads <= 0 || max_seq_len <= 0 || max_seq_len > (1 << 30) ||
+      cache->num_kv_heads <= 0 || (cache->head_dim != 64 && cache->head_dim != 128) || num_q_heads % cache->num_kv_heads != 0 ||
+      too_many_rows(batch, n_q, num_q_heads, cache->num_kv_heads))
     return 0;
   return novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim, 1, max_seq_len, 0).total;
 }
@@ -165,9 +172,7 @@ nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nov
     if (batch == 0 || n_q == 0) return ok();
     if (!q || !seq_lens || !out) return fail(NOVA_KV_ERR_INVALID_ARG, "q, seq_lens or out is NULL");
     if (!aligned(q, 16) || !aligned(out, 16)) return fail(NOVA_KV_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
-    const long long rows = static_cast<long long>(n_q) * (num_q_heads / cache->num_kv_heads);
-    // rows of a unit and threads of a launch (768 a tile) are counted in 32 bits
-    if (rows > (1 << 24) || static_cast<long long>(batch) * cache->num_kv_heads * ((rows + 15) / 16) > (1 << 22))
+    if (too_many_rows(batch, n_q, num_q_heads, cache->num_kv_heads))
       return fail(NOVA_KV_ERR_UNSUPPORTED, "too many query rows in a call");
     const novakv::Q4AttnPlan plan = novakv::plan_q4_attn(batch, n_q, num_q_heads, cache->num_kv_heads, cache->head_dim,
                                                          q_dtype == NOVA_KV_BF16, max_seq_len, window);

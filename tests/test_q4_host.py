@@ -170,3 +170,11 @@ def test_checks_under_sanitizers(tmp_path):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0:verify_asan_link_order=0", UBSAN_OPTIONS="print_stacktrace=1")
     r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=300)
     assert r.returncode == 0, r.stderr[-4000:]
+
+
+def test_workspace_query_of_refused_calls():
+    """The workspace query returns 0 for calls of too many rows, of lengths past any capacity and of other heads."""
+    size = lambda *a, **kw: nat.lib().nova_kv_q4_attn_workspace_bytes(ref(cache(**kw)), *a)  # noqa: E731
+    assert size(1, 1, 32, 1 << 30) > 0
+    assert size(1, 1, 32, (1 << 30) + 1) == size(1, 2 ** 31 - 1, 32, 4096) == 0
+    assert size(65536, 1, 32, 4096) == size(65535, 65535, 32, 4096) == size(1, 1, 32, 4096, head_dim=96) == 0
