@@ -7,7 +7,9 @@
 // are used. Unpacked, a score needs no more than its multiply-add into the
 // exponent, and a probability no scale: 7.5 vector instructions each, where
 // q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
-// of keys and values).
+// of keys and values). Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV
+// heads of 128): 553 us, 870 TFLOP/s. Vector (360 us) and matrix instructions (192 us) bound
+// it, which add on a SIMD; without the LDS the same took 1211 us.
 //
 // Keys and values are divided by 2^7 times a power of two at or above the
 // largest magnitude of the 64 tokens (each side its own), which the exponent and
