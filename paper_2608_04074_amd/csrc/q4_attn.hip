@@ -348,72 +348,73 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   finish_rows<D, NT, W, TILED>(a, g, {s_merge, s_ref, s_sum, s_inv, &s_last}, wave, lane, acc, ref, sum);
 }
 
-}  // namespace
-
-namespace {
-
 int most_splits(const int tile_rows, const long long tiles, const long long span) {
-  const long long limit = tile_rows == 128 ? kMaxSplitsTiled : kMaxSplits;
+  const long long limit = tile_rows >= 128 ? kMaxSplitsTiled : kMaxSplits;
   return static_cast<int>(std::max<long long>(1, std::min({limit, (span + 127) / 128, kMaxCounters / tiles})));
 }
 
 }  // namespace
 
 // Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the
-// workgroup's waves dividing the tokens; more rows take 128 a workgroup, 32 a
-// wave.
+// workgroup's waves dividing the tokens; more rows take 32 a wave, 128 or 256 a
+// workgroup.
 Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads,
                         const int head_dim, const int q_bf16, const int max_seq_len, const int window) {
   Q4AttnPlan p{};
-  const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
-  p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
-  p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
-  const long long tiles = static_cast<long long>(batch) * num_kv_heads * p.row_tiles;
-  const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
-  const bool tiled = p.tile_rows == 128;
+  const int gqa = num_q_heads / num_kv_heads;
+  const long long rows = static_cast<long long>(n_q) * gqa;
+  auto tiles_of = [&](const int tile_rows) { return (rows + tile_rows - 1) / tile_rows * batch * num_kv_heads; };
   // A launch takes rounds of the workgroups that the CUs hold, each its setup
   // and tail beside its tokens; splits add the merge, by rows. Fitted to sweeps
   // over both (8 KV heads of 128, bf16, us): one sequence of 128K tokens 36.2 in
   // 32 splits of 12 waves, 38.6 in 64 of 4 waves, 46.2 in 32 of 4; of 2000 tokens
   // 15.2 in 3 of 12, 10.4 in 16 of 4; 32 x 8192 55.6 whole by 12 waves, 57.2 in 3 of
-  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12; 64 queries over 32K tokens 128 in 16
-  // splits, 186 in 32, 168 in 8; 8 x 64 over 2000 tokens 70 whole, 81 in 2.
+  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12; 64 queries over 32K tokens 123 in 16
+  // splits of 128 rows, 154 of 256; 8 x 64 over 2000 tokens 79 in tiles of 128, 98 of
+  // 256; 2 x 2048 over 8192 tokens 559 in tiles of 128, 503 of 256.
   const double size = head_dim == 128 ? 1.0 : 0.75;
-  const double row_ns = static_cast<double>(std::min<long long>(rows, p.tile_rows));
   // token[k - 1]: ns of a CU for a token where k workgroups share it
-  auto consider = [&](const int waves, const int setup, const std::initializer_list<double> token, const int split,
-                      const double merge) {
-    const int step = tiled ? (q_bf16 ? 64 : kRound) : kRound * waves, per_cu = static_cast<int>(token.size());
-    for (int n = 1; n <= most_splits(p.tile_rows, tiles, span); ++n) {
+  auto consider = [&](const int tile_rows, const int waves, const int step, const int setup,
+                      const std::initializer_list<double> token, const int split, const double merge) {
+    const long long tiles = tiles_of(tile_rows), queries = std::min(n_q, tile_rows / gqa + 1);  // of a tile
+    const long long span = window > 0 ? std::min<long long>(max_seq_len, window + queries) : max_seq_len;
+    const double row_ns = static_cast<double>(std::min<long long>(rows, tile_rows));
+    const int per_cu = static_cast<int>(token.size());
+    for (int n = 1; n <= most_splits(tile_rows, tiles, span); ++n) {
       const long long chunk = ((span + n - 1) / n + step - 1) / step * step;
       const long long groups = tiles * n, rounds = (groups + 256 * per_cu - 1) / (256 * per_cu);
       const int share = static_cast<int>(std::min<long long>(per_cu, (groups + 255) / 256));
       const double each = chunk * size * token.begin()[share - 1] * share;
       const double words = groups * row_ns * (head_dim + 2);  // of the partials, 1.2 TB/s
       const double cost = rounds * (setup + each) + (n > 1 ? split + merge * row_ns * n + words / 300 : 0);
-      if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n;
+      if (p.waves == 0 || cost < p.cost) p.cost = cost, p.waves = waves, p.n_split = n, p.tile_rows = tile_rows;
     }
   };
-  if (tiled && q_bf16) {
-    consider(4, 10000, {29, 23}, 10000, 19);
-  } else if (tiled) {
-    consider(4, 10000, {62}, 10000, 19);
-  } else if (p.tile_rows == 32) {
-    consider(4, 10000, {13}, 3500, 10);
-    consider(8, 10000, {8.5}, 3500, 10);
+  const int most_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 256;
+  if (rows > 32 && q_bf16) {
+    consider(128, 4, 64, 10000, {29, 23}, 10000, 19);
+    if (rows <= 128) consider(256, 8, 128, 10000, {27}, 10000, 19);  // half of the waves have no rows, and unpack only
+    else consider(256, 8, 128, 12000, {42}, 10000, 19);
+  } else if (rows > 32) {
+    consider(128, 4, kRound, 10000, {62}, 10000, 19);
+  } else if (rows > 16) {
+    consider(32, 4, 4 * kRound, 10000, {13}, 3500, 10);
+    consider(32, 8, 8 * kRound, 10000, {8.5}, 3500, 10);
   } else if (q_bf16) {
-    consider(4, 6500, {9, 6.2, 5.7}, 3500, 10);
-    consider(12, 7000, {5.8}, 3500, 5);
+    consider(16, 4, 4 * kRound, 6500, {9, 6.2, 5.7}, 3500, 10);
+    consider(16, 12, 12 * kRound, 7000, {5.8}, 3500, 5);
   } else {
-    consider(4, 6500, {9.9, 8}, 3500, 10);
-    consider(8, 7000, {7.5}, 3500, 5);
+    consider(16, 4, 4 * kRound, 6500, {9.9, 8}, 3500, 10);
+    consider(16, 8, 8 * kRound, 7000, {7.5}, 3500, 5);
   }
-  // the counters of all shapes lie at the workspace's start; its size covers
-  // every window and type
-  const int most = most_splits(p.tile_rows, tiles, max_seq_len);
+  p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
+  // The counters of all shapes lie at the workspace's start; its size covers
+  // every window, type and tile (tiles of 256 rows need no less than ones of 128).
+  const long long tiles = tiles_of(most_rows);
+  const int most = most_splits(most_rows, tiles, max_seq_len);
   p.off_part = kMaxCounters * sizeof(int);
   if (most > 1) {
-    const size_t part = static_cast<size_t>(tiles) * most * p.tile_rows * (head_dim + 2) * sizeof(float);
+    const size_t part = static_cast<size_t>(tiles) * most * most_rows * (head_dim + 2) * sizeof(float);
     p.total = p.off_part + ((part + 255) & ~static_cast<size_t>(255));
   }
   return p;
@@ -429,7 +430,7 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream
       q4_attn_kernel<d(), wide(), nt(), w(), tiled(), false><<<tiles * a.n_split, 64 * w(), 0, stream>>>(a);
     return hipGetLastError();
   };
-  if (a.q_bf16 && plan.tile_rows == 128) return launch_q4_tile(a, plan, stream);
+  if (a.q_bf16 && plan.tile_rows >= 128) return launch_q4_tile(a, plan, stream);
   using std::false_type;
   using std::integral_constant;
   using std::true_type;

@@ -1,15 +1,19 @@
 // Attention of many query rows over a cache held in 4 bits (nova_kv_q4_attn with
 // bf16 queries and more than 32 rows per KV head: chunks of prompts).
 //
-// A workgroup of four waves takes 128 rows, 32 a wave, and 64 tokens at a time. The
-// waves unpack the tokens' rows once, between them, to fp16 keys and values in
-// LDS, in the order in which the matrix cores take them, the next 64 while these
-// are used. Unpacked, a score needs no more than its multiply-add into the
-// exponent, and a probability no scale: 7.5 vector instructions each, where
-// q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
-// of keys and values). Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV
-// heads of 128): 553 us, 870 TFLOP/s. Vector (360 us) and matrix instructions (192 us) bound
-// it, which add on a SIMD; without the LDS the same took 1211 us.
+// A workgroup of eight (four) waves takes 256 (128) rows, 32 a wave, and 128 (64)
+// tokens at a time. The waves unpack the tokens' rows once, between them, to fp16
+// keys and values in LDS, in the order in which the matrix cores take them, the
+// next ones while these are used. Unpacked, a score needs no more than its
+// multiply-add into the exponent, and a probability no scale: 7 vector instructions
+// each, an exponential among them (9 with four waves, which unpack for half the rows),
+// where q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
+// of keys and values).
+//
+// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 498 us, 966
+// TFLOP/s. Vector (about 290 us) and matrix instructions (192 us) bound it, which add
+// on a SIMD. Four waves take 554 us, and the same without the LDS 1211; with few tiles
+// the smaller ones win, by parallelism and by a merge of splits over more workgroups.
 //
 // Keys and values are divided by 2^7 times a power of two at or above the
 // largest magnitude of the 64 tokens (each side its own), which the exponent and
@@ -29,7 +33,7 @@ namespace {
 
 using namespace q4;
 
-constexpr int kWaves = 4, kRowTiles = 2, kTokens = 64;
+constexpr int kRowTiles = 2;
 constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability after a rescale, and how far it may grow
 
 // The same value in every lane, in a scalar register.
@@ -42,24 +46,26 @@ __device__ __forceinline__ int exponent_of(const float mag) {
 }
 __device__ __forceinline__ float power_of_two(const int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
-// ALIGNED: blocks of a multiple of 16 rows.
-template <int D, bool ALIGNED>
-__global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArgs a) {
+// W: waves of a workgroup, a multiple of four. ALIGNED: blocks of a multiple of 16 rows.
+template <int D, int W, bool ALIGNED>
+__global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) {
+  constexpr int kWaves = W, kParts = W / 4, kTokens = 64 * kParts;  // tokens of a round, in parts of 64
   constexpr int kSteps = D / 32, kTiles = D / 16, kKeyWords = D / 32;
   constexpr int kKeys = 4 * kSteps * 64, kBuffer = kKeys + 2 * kTiles * 64;  // fragments of 16 bytes: keys, then values
   using Lds = FinishLds<D, kRowTiles, kWaves, true>;
-  static_assert(2 * kBuffer * 16 >= Lds::kMerge * 4, "the splits' weights take the tokens' place");
-  __shared__ half8_t s_tokens[2][kBuffer];
+  static_assert(2 * kParts * kBuffer * 16 >= Lds::kMerge * 4, "the splits' weights take the tokens' place");
+  __shared__ half8_t s_tokens[2][kParts * kBuffer];
   __shared__ uint32_t s_rows[ALIGNED ? 1 : kWaves][32];
   __shared__ __align__(16) uint32_t s_pack[kWaves][64];
-  __shared__ float s_mag[3][2][2];     // [round mod 3][32 tokens][keys, values]
-  __shared__ uint32_t s_valid[3][2];
+  __shared__ float s_mag[3][2 * kParts][2];     // [round mod 3][32 tokens][keys, values]
+  __shared__ uint32_t s_valid[3][2 * kParts];
   __shared__ float s_inv[Lds::kRows];
   __shared__ int s_last;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
-  const int group = wave >> 1, part = wave & 1;  // the wave unpacks 16 keys and half of the coordinates of 32 values
+  // the wave unpacks, of a round's part, 16 keys and half of the coordinates of 32 values
+  const int group = wave >> 1, part = wave & 1, own = wave >> 2;
   Tile g;
   place_tile(a, Lds::kRows, g);
   if (!find_span(a, Lds::kRows, kTokens, g)) return;
@@ -149,11 +155,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     if (part == 0 && (lane & 31) == 0) s_mag[slot][group][lane >> 5] = mag;
     if (part == 0 && lane == 0) s_valid[slot][group] = valid;
   };
-  auto exponents = [&](const int slot, int &ek, int &ev) {
-    ek = exponent_of(fmaxf(s_mag[slot][0][0], s_mag[slot][1][0]));
-    ev = exponent_of(fmaxf(s_mag[slot][0][1], s_mag[slot][1][1]));
+  auto exponents = [&](const int slot, const int y, int &ek, int &ev) {
+    ek = exponent_of(fmaxf(s_mag[slot][2 * y][0], s_mag[slot][2 * y + 1][0]));
+    ev = exponent_of(fmaxf(s_mag[slot][2 * y][1], s_mag[slot][2 * y + 1][1]));
   };
   auto unpack = [&](const Round &r, const int ek, const int ev, half8_t *to) {
+    to += own * kBuffer;
     float scale, offset;
     const bool odd = !(scale_of(r, scale, offset) < __builtin_inff());
     // A value that is not finite would reach the rows it is hidden from (0 * NaN): its
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
       for (int i = 0; i < kKeyWords; ++i) {
         const int word = kKeyWords * j + i;
         const uint32_t w = r.kw[i];
-        to[(wave * kSteps + word / 4) * 64 + 16 * (word % 4) + n] = __builtin_bit_cast(
+        to[((wave & 3) * kSteps + word / 4) * 64 + 16 * (word % 4) + n] = __builtin_bit_cast(
             half8_t, make_uint4(place(c0, w, s2, o2), place(c1, w, s2, o2), place(c2, w, s2, o2), place(c3, w, s2, o2)));
       }
     }
@@ -199,7 +206,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     __builtin_amdgcn_wave_barrier();
     for (int e = 0; e < 4; ++e) pair[e] = __builtin_amdgcn_perm(r.vw[2 * e + 1], r.vw[2 * e], pick);
     auto put = [&](auto k, const int o) {
-      to[kKeys + (group * kTiles + o) * 64 + lane] = __builtin_bit_cast(
+      to[kKeys + ((group & 1) * kTiles + o) * 64 + lane] = __builtin_bit_cast(
           half8_t, make_uint4(place(k, pair[0], s2[0], o2[0]), place(k, pair[1], s2[1], o2[1]), place(k, pair[2], s2[2], o2[2]),
                               place(k, pair[3], s2[3], o2[3])));
     };
@@ -270,11 +277,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  int ek = 0, ev = 0, slot = 1;  // of the round at hand; the slot of the one behind it
+  int slot = 1;  // of the round behind the one at hand
   if (any) {
+    int ek, ev;
     announce(cur, 0);
     __syncthreads();
-    exponents(0, ek, ev);
+    exponents(0, own, ek, ev);
     unpack(cur, ek, ev, s_tokens[0]);
     request(cur);
     look_up();
@@ -283,30 +291,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
   }
   for (int tb = g.t0, round = 0; tb < g.t1; tb += kTokens, ++round) {
     const int slot0 = slot == 0 ? 2 : slot - 1, slot2 = slot == 2 ? 0 : slot + 1;
-    const half8_t *tokens = s_tokens[round & 1];
-    float4_t s[kRowTiles][4];
-    for (int x = 0; x < 4; ++x) {
-      for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
-      for (int st = 0; st < kSteps; ++st) {
-        const half8_t k = tokens[(x * kSteps + st) * 64 + lane];
-        for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
+    auto scores = [&](const half8_t *tokens, float4_t (&s)[kRowTiles][4]) {
+      for (int x = 0; x < 4; ++x) {
+        for (int t = 0; t < kRowTiles; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
+        for (int st = 0; st < kSteps; ++st) {
+          const half8_t k = tokens[(x * kSteps + st) * 64 + lane];
+          for (int t = 0; t < kRowTiles; ++t) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][st], s[t][x], 0, 0, 0);
+        }
       }
-    }
-    int next_ek, next_ev;
-    exponents(slot, next_ek, next_ev);
-    unpack(cur, next_ek, next_ev, s_tokens[(round + 1) & 1]);
-    request(cur);  // past the end: hidden
-    look_up();
-    if (!idle && tb < wave_hi && tb + kTokens > wave_lo) {
-      const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][0])), static_cast<uint32_t>(uniform(s_valid[slot0][1]))};
-      const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb >= inner_lo && tb + kTokens <= inner_hi;
+    };
+    auto attend = [&](const half8_t *tokens, float4_t (&s)[kRowTiles][4], const int y) {
+      const int tb0 = tb + 64 * y;
+      if (idle || tb0 >= wave_hi || tb0 + 64 <= wave_lo) return;
+      int ek, ev;
+      exponents(slot0, y, ek, ev);
+      const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][2 * y])), static_cast<uint32_t>(uniform(s_valid[slot0][2 * y + 1]))};
+      const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb0 >= inner_lo && tb0 + 64 <= inner_hi;
       const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev), value_inv = power_of_two(-ev);
-      if (!inner) {
+      if (!inner) {  // without branches in it the scores stay where they are, and inner rounds copy nothing
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
             for (int i = 0; i < 4; ++i) {
               const int m = 16 * x + 4 * j + i;
-              const bool seen = ((valid[x >> 1] >> (m & 31)) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
+              const bool seen = ((valid[x >> 1] >> (m & 31)) & 1u) & (tb0 + m >= row_lo[t]) & (tb0 + m < row_hi[t]);
               s[t][x][i] = seen ? s[t][x][i] : kNone;
             }
       }
@@ -349,10 +356,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
           const half8_t v = tokens[kKeys + (h * kTiles + o) * 64 + lane];
           for (int t = 0; t < kRowTiles; ++t) acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[t][h], acc[t][o], 0, 0, 0);
         }
+    };
+    const half8_t *tokens = s_tokens[round & 1];
+    float4_t s[kRowTiles][4];
+    scores(tokens, s);
+    int next_ek, next_ev;  // of the wave's tokens of the next round
+    exponents(slot, own, next_ek, next_ev);
+    unpack(cur, next_ek, next_ev, s_tokens[(round + 1) & 1]);
+    request(cur);  // past the end: hidden
+    look_up();
+    attend(tokens, s, 0);
+    for (int y = 1; y < kParts; ++y) {
+      scores(tokens + y * kBuffer, s);
+      attend(tokens + y * kBuffer, s, y);
     }
     announce(cur, slot2);
     __syncthreads();
-    ek = next_ek, ev = next_ev;
     slot = slot2;
   }
 
@@ -369,12 +388,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void q4_tile_kernel(const Q4AttnArg
 
 hipError_t launch_q4_tile(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream) {
   const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
-  auto go = [&](auto d, auto aligned) {
-    q4_tile_kernel<d(), aligned()><<<groups, 64 * kWaves, 0, stream>>>(a);
+  auto go = [&](auto d, auto w, auto aligned) {
+    q4_tile_kernel<d(), w(), aligned()><<<groups, 64 * w(), 0, stream>>>(a);
     return hipGetLastError();
   };
+  using std::integral_constant;
+  auto by_waves = [&](auto d, auto aligned) {
+    return plan.waves == 8 ? go(d, integral_constant<int, 8>{}, aligned) : go(d, integral_constant<int, 4>{}, aligned);
+  };
   auto by_size = [&](auto aligned) {
-    return a.head_dim == 128 ? go(std::integral_constant<int, 128>{}, aligned) : go(std::integral_constant<int, 64>{}, aligned);
+    return a.head_dim == 128 ? by_waves(integral_constant<int, 128>{}, aligned) : by_waves(integral_constant<int, 64>{}, aligned);
   };
   return a.layout.block_size % 16 == 0 ? by_size(std::true_type{}) : by_size(std::false_type{});
 }
