@@ -277,10 +277,10 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
         scale[e] = vs[e];
         offset[e] = vo8[e];
       }
-      if (!inner) {
+      if (!inner) {  // without branches in it, inner rounds copy nothing
         for (int e = 0; e < 8; ++e) {
           const int m = 16 * (e >> 2) + 4 * j + (e & 3);
-          const bool seen = ((valid >> m) & 1u) && tb + m >= row_lo[t] && tb + m < row_hi[t];
+          const bool seen = ((valid >> m) & 1u) & (tb + m >= row_lo[t]) & (tb + m < row_hi[t]);
           z[e] = seen ? z[e] : kNone;
           scale[e] = seen ? scale[e] : 0.f;  // whatever a hidden token's scale and offset are
           offset[e] = seen ? offset[e] : 0.f;
