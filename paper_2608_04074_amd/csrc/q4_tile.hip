@@ -11,7 +11,7 @@
 // of keys and values).
 //
 // Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 498 us, 966
-// TFLOP/s. Vector (about 290 us) and matrix instructions (192 us) bound it, which add
+// TFLOP/s. Vector (about 310 us) and matrix instructions (192 us) bound it, which add
 // on a SIMD. Four waves take 554 us, and the same without the LDS 1211; with few tiles
 // the smaller ones win, by parallelism and by a merge of splits over more workgroups.
 //
