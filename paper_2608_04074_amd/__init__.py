@@ -1,5 +1,7 @@
 """NOVA-KV hot path for MI355X (gfx950): 2-bit VQ KV-cache encode and decode attention.
 
+Beside it: norm and rotation of heads, and a cache held in 4 bits with its attention (q4.py).
+
 The compute lives in ``libnovakv.so`` (hand-written HIP, C ABI in
 ``include/nova_kv.h``); this package is its Python binding.
 """

@@ -357,7 +357,8 @@ int most_splits(const int tile_rows, const long long tiles, const long long span
 
 // Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the
 // workgroup's waves dividing the tokens; more rows take 32 a wave, 128 or 256 a
-// workgroup.
+// workgroup (fp32: 16 and 128, which leaves registers for two waves a SIMD: 2 x 2048
+// over 8192 tokens 1462 us, 1756 with 32 a wave; 8 x 16 over 4096 60 us, 93).
 Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads,
                         const int head_dim, const int q_bf16, const int max_seq_len, const int window) {
   Q4AttnPlan p{};
@@ -396,7 +397,7 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
     if (rows <= 128) consider(256, 8, 128, 10000, {27}, 10000, 19);  // half of the waves have no rows, and unpack only
     else consider(256, 8, 128, 12000, {42}, 10000, 19);
   } else if (rows > 32) {
-    consider(128, 4, kRound, 10000, {62}, 10000, 19);
+    consider(128, 8, kRound, 10000, {51}, 10000, 19);
   } else if (rows > 16) {
     consider(32, 4, 4 * kRound, 10000, {13}, 3500, 10);
     consider(32, 8, 8 * kRound, 10000, {8.5}, 3500, 10);
@@ -441,7 +442,7 @@ hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream
   constexpr integral_constant<int, 12> w12{};
   auto by_rows = [&](auto d, auto wide) {
     if constexpr (wide())
-      if (plan.tile_rows == 128) return go(d, wide, two, w4, true_type{});
+      if (plan.tile_rows == 128) return go(d, wide, one, w8, true_type{});
     if (plan.tile_rows == 32) return plan.waves == 4 ? go(d, wide, two, w4, false_type{}) : go(d, wide, two, w8, false_type{});
     if (plan.waves == 4) return go(d, wide, one, w4, false_type{});
     if constexpr (wide()) return go(d, wide, one, w8, false_type{});
