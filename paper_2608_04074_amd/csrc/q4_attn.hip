@@ -17,8 +17,8 @@
 // value, and cut those bits off the sum: 1e-5 of an output, towards one side.)
 //
 // With 4 query heads a KV head, bf16 (8 KV heads of 128): 64 sequences of 32K tokens
-// take 411 us, 5.55 TB/s of HBM, which bounds them; one of 128K 39 us (35 from the
-// caches), the reads' 24 us, their ramp and 9 us of merge; one of 2000 tokens 9.9 us,
+// take 405 us, 5.6 TB/s of HBM, which bounds them; one of 128K 38 us (34 from the
+// caches), the reads' 24 us, their ramp and 9 us of merge; one of 2000 tokens 9.7 us,
 // latency. fp32: 5 sequences of up to 5003 tokens, 10 rows a KV head, 19 us, latency and vector issue.
 #include <algorithm>
 #include <initializer_list>
