@@ -20,7 +20,7 @@ using lut::max_rows32;
 // the cut, towards one side, which fp32 outputs would show. So with fp32
 // queries a probability is split into two fixed-point parts of 11 bits and the rest.
 constexpr float kNone = -__builtin_inff();
-// Most splits of a tile's span: their weights lie in LDS (16 or 32 rows, 128 rows).
+// Most splits of a tile's span: their weights lie in LDS (up to 32 rows a tile; 128 or 256).
 constexpr int kMaxSplits = 96, kMaxSplitsTiled = 32;
 // Arrival counters of a workspace: a span is split only where at most this many
 // workgroups run, so no call's partials lie on another shape's counters.
