@@ -5,12 +5,11 @@
 // tokens at a time. The waves unpack the tokens' rows once, between them, to fp16
 // keys and values in LDS, in the order in which the matrix cores take them, the
 // next ones while these are used. Unpacked, a score needs no more than its
-// multiply-add into the exponent, and a probability no scale: 7 vector instructions
-// each, an exponential among them (9 with four waves, which unpack for half the rows),
-// where q4_attn.hip's exact sums over the codes take 14.5 (but no LDS, and no rounding
-// of keys and values).
+// multiply-add into the exponent: 8.5 vector instructions each, an exponential
+// among them (10.5 with four waves, which unpack for half the rows), where q4_attn.hip's
+// exact sums over the codes take 14.5 (but no LDS, and no rounding of keys and values).
 //
-// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 498 us, 966
+// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 504 us, 955
 // TFLOP/s. Vector (about 310 us) and matrix instructions (192 us) bound it, which add
 // on a SIMD. Four waves take 554 us, and the same without the LDS 1211; with few tiles
 // the smaller ones win, by parallelism and by a merge of splits over more workgroups.
@@ -307,7 +306,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
       exponents(slot0, y, ek, ev);
       const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][2 * y])), static_cast<uint32_t>(uniform(s_valid[slot0][2 * y + 1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb0 >= inner_lo && tb0 + 64 <= inner_hi;
-      const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev), value_inv = power_of_two(-ev);
+      const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev), value_unit = power_of_two(ev);
       if (!inner) {  // without branches in it the scores stay where they are, and inner rounds copy nothing
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
@@ -339,16 +338,15 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
       }
       half8_t pf[kRowTiles][2];
       auto probabilities = [&](const int t) {
-        const float from = value_exp - (ref[t] == kNone ? 0.f : ref[t]);
-        float part_sum = 0.f;  // of the probabilities as fp16 has them
+        const float r = ref[t] == kNone ? 0.f : ref[t];
+        // Summed in fp32, in front of the values' power of two and of the rounding to
+        // fp16: a weight does not depend on its value, which may be far below others.
         for (int x = 0; x < 4; ++x)
-          for (int i = 0; i < 4; i += 2) {
-            const lut::half2_t p = {static_cast<_Float16>(exp2_raw(__builtin_fmaf(s[t][x][i], by[t], from))),
-                                    static_cast<_Float16>(exp2_raw(__builtin_fmaf(s[t][x][i + 1], by[t], from)))};
-            part_sum = __builtin_amdgcn_fdot2(p, lut::half2_t{1, 1}, part_sum, false);
-            pf[t][x >> 1][4 * (x & 1) + i] = p[0], pf[t][x >> 1][4 * (x & 1) + i + 1] = p[1];
+          for (int i = 0; i < 4; ++i) {
+            const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by[t], -r));
+            sum[t] += p;
+            pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p * value_unit);
           }
-        sum[t] += part_sum * value_inv;
       };
       for (int t = 0; t < kRowTiles; ++t) probabilities(t);
       for (int h = 0; h < 2; ++h)
