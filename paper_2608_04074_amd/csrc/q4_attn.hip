@@ -291,11 +291,13 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
       if (__any(bound > ref[t] + (kTop + kSlack))) {
         const float most = max_rows32(max_rows16(bound));
         const float next = fmaxf(ref[t], most - kTop);
-        const float f = next == kNone ? 1.f : exp2_raw(ref[t] - next);
+        const float f = next == kNone ? 1.f : half_factor(ref[t] - next);
         ref[t] = next;
-        sum[t] *= f;
-        off_sum[t] *= f;
-        for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+        for (int y = 0; y < 2; ++y) {
+          sum[t] *= f;
+          off_sum[t] *= f;
+          for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+        }
       }
       const float r = ref[t] == kNone ? 0.f : ref[t];
       for (int e = 0; e < 8; ++e) {

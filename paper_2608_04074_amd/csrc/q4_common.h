@@ -28,6 +28,10 @@ constexpr int kMaxCounters = 1024;
 
 __device__ __forceinline__ float exp2_raw(const float x) { return __builtin_amdgcn_exp2f(x); }
 
+// 2^(d / 2), to be multiplied twice: a sum of weights beside small values reaches
+// 2^110, and one factor 2^d below 2^-126 would take it to zero.
+__device__ __forceinline__ float half_factor(const float d) { return exp2_raw(0.5f * d); }
+
 typedef int int4_t __attribute__((ext_vector_type(4)));
 
 // Codes k and k + 4 of a word as fp16 denormals in a word: c * 2^-24, times 16 for odd k.
@@ -180,10 +184,10 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int u = 0; u < kWaves; ++u) {
         if (s_ref[u][r] == kNone) continue;
-        const float f = exp2_raw(s_ref[u][r] - most);
+        const float f = half_factor(s_ref[u][r] - most);
         const float4 y = *reinterpret_cast<const float4 *>(s_merge + (u * 16 * NT + r) * kStride + c);
-        l += f * s_sum[u][r];
-        v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+        l += f * s_sum[u][r] * f;
+        v.x += f * y.x * f, v.y += f * y.y * f, v.z += f * y.z * f, v.w += f * y.w * f;
       }
       if (part) {
         publish4(part + r * D + c, v);
@@ -250,8 +254,8 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
     most = fmaxf(most, lut::row_ror<8>(most));
     for (int x = n; x < a.n_split; x += 16) {
       const float2 ml = weight[r * a.n_split + x];
-      const float f = ml.x == kNone ? 0.f : exp2_raw(ml.x - most);
-      l += f == 0.f ? 0.f : f * ml.y;
+      const float f = ml.x == kNone ? 0.f : half_factor(ml.x - most);
+      l += f == 0.f ? 0.f : f * ml.y * f;
       weight[r * a.n_split + x].x = f;
     }
     l += lut::row_ror<1>(l);
@@ -270,7 +274,7 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
       for (int y = 0; y < kAhead; ++y) {
         const int u = first + y * groups;
         const float f = u < a.n_split ? weight[r * a.n_split + u].x : 0.f;
-        if (f != 0.f) o.x += f * v[y].x, o.y += f * v[y].y, o.z += f * v[y].z, o.w += f * v[y].w;
+        if (f != 0.f) o.x += f * v[y].x * f, o.y += f * v[y].y * f, o.z += f * v[y].z * f, o.w += f * v[y].w * f;
       }
     }
     if (groups > 1) {

@@ -330,10 +330,12 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
         for (int t = 0; t < kRowTiles; ++t) {
           const float most = max_rows32(max_rows16(bound[t]));
           const float to = fmaxf(ref[t], most - kTop);
-          const float f = to == kNone ? 1.f : exp2_raw(ref[t] - to);
+          const float f = to == kNone ? 1.f : half_factor(ref[t] - to);
           ref[t] = to;
-          sum[t] *= f;
-          for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+          for (int y = 0; y < 2; ++y) {
+            sum[t] *= f;
+            for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
+          }
         }
       }
       half8_t pf[kRowTiles][2];
