@@ -254,8 +254,9 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
     most = fmaxf(most, lut::row_ror<8>(most));
     for (int x = n; x < a.n_split; x += 16) {
       const float2 ml = weight[r * a.n_split + x];
-      const float f = ml.x == kNone ? 0.f : half_factor(ml.x - most);
-      l += f == 0.f ? 0.f : f * ml.y * f;
+      // A split of no weight counts all the same: it may hold a NaN. One that attends nothing has weight -1.
+      const float f = ml.x == kNone ? -1.f : half_factor(ml.x - most);
+      if (ml.x != kNone) l += f * ml.y * f;
       weight[r * a.n_split + x].x = f;
     }
     l += lut::row_ror<1>(l);
@@ -273,8 +274,8 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
       if (x != item || first != group) fetch_values(x, first);
       for (int y = 0; y < kAhead; ++y) {
         const int u = first + y * groups;
-        const float f = u < a.n_split ? weight[r * a.n_split + u].x : 0.f;
-        if (f != 0.f) o.x += f * v[y].x * f, o.y += f * v[y].y * f, o.z += f * v[y].z * f, o.w += f * v[y].w * f;
+        const float f = u < a.n_split ? weight[r * a.n_split + u].x : -1.f;
+        if (f != -1.f) o.x += f * v[y].x * f, o.y += f * v[y].y * f, o.z += f * v[y].z * f, o.w += f * v[y].w * f;
       }
     }
     if (groups > 1) {
