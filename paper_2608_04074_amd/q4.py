@@ -229,9 +229,9 @@ def _rotate_call(rotary, q, k, v, start_pos, q_out, k_out, v_out, new_lens, stre
     return _DeviceCall(nat.lib().nova_kv_rotate_qkv, args, (rotary, tensors, rows), device)
 
 
-def _fresh(t, new_lens, stream):
-    """An output for rows like t: zeros where padding rows stay as they are."""
-    make = torch.zeros if new_lens is not None else torch.empty
+def _fresh(t, whole, stream):
+    """An output for rows like t: zeros, but where the call writes the whole of it."""
+    make = torch.empty if whole else torch.zeros
     with torch.cuda.stream(stream):
         return make(t.shape, dtype=t.dtype, device=t.device)
 
@@ -245,9 +245,11 @@ def rotate_qkv(rotary: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tens
     may be None) -> dense (q, k, v) for encode, decode_attn and the step, queries
     and keys normed and rotated at the positions start_pos[b] + i.
 
-    Tokens i >= new_lens[b] are padding: their output rows stay as they were
-    (zeros in outputs that the call makes itself)."""
-    q_out, k_out, v_out = (o if o is not None or t is None else _fresh(t, new_lens, stream)
+    Tokens i >= new_lens[b] and, with a rotation, those at positions outside the table
+    are left out: their output rows stay as they were (zeros in outputs that
+    the call makes itself)."""
+    whole = new_lens is None and rotary.cos_sin is None
+    q_out, k_out, v_out = (o if o is not None or t is None else _fresh(t, whole, stream)
                            for t, o in ((q, q_out), (k, k_out), (v, v_out)))
     _rotate_call(rotary, q, k, v, start_pos, q_out, k_out, v_out, new_lens, stream)()
     return q_out, k_out, v_out
@@ -282,12 +284,14 @@ def q4_append(rotary: Rotary, cache: Q4Cache, q: Optional[torch.Tensor], k: torc
               stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
     """nova_kv_q4_append: k, v [B][n_new][Hkv][D] (as in rotate_qkv) to the positions
     start_pos[b] + i of the 4-bit cache, keys normed and rotated -> the queries q
-    [B][n_new][Hq][D] normed and rotated, dense (None without q).
+    [B][n_new][Hq][D] normed and rotated, dense (None without q).  Rows of tokens that
+    are left out (padding, positions outside the table or the cache, blocks that
+    hold nothing) stay as they were: zeros in an output that the call makes itself.
 
     k_held and v_held, when given, receive the values that the cache now stands
     for, as dense tensors [B][n_new][Hkv][D]."""
     if q is not None and q_out is None:
-        q_out = _fresh(q, new_lens, stream)
+        q_out = _fresh(q, False, stream)
     _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream)()
     return q_out
 
@@ -339,7 +343,7 @@ def q4_attn(cache: Q4Cache, q: torch.Tensor, seq_lens: torch.Tensor, max_seq_len
     before its first use; each call leaves it ready for the next.  When omitted,
     a zeroed one is allocated."""
     if out is None:
-        out = _fresh(q, q_lens, stream)
+        out = _fresh(q, q_lens is None, stream)
     if workspace is None and q.dim() == 4:
         need = q4_attn_workspace_bytes(cache, q.shape[0], q.shape[1], q.shape[2], max_seq_len)
         if need:
