@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/nova_kv.h"
+#include "debug_check.h"
 #include "host_checks.h"
 #include "nova_kv_internal.h"
 

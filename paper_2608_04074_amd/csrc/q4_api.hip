@@ -6,6 +6,7 @@
 #include <exception>
 
 #include "../../include/nova_kv.h"
+#include "debug_check.h"
 #include "host_checks.h"
 #include "q4_internal.h"
 
