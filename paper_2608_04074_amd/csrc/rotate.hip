@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "q4_internal.h"
+#include "rotate_layout.h"
 
 namespace novakv {
 
@@ -230,9 +231,9 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   if (a.new_lens && i >= a.new_lens[b]) return;
   const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
   const int heads = a.nq + a.nk + a.nv;
-  const bool turns = lane < a.rotary_dim / 8;
-  const int c0 = !IL && turns ? 4 * lane : 8 * lane;
-  const int c1 = !IL && turns ? c0 + a.rotary_dim / 2 : c0 + 4;
+  const rotate::LaneChunks chunks = rotate::lane_chunks(lane, a.rotary_dim, IL);
+  const bool turns = chunks.turns;
+  const int c0 = chunks.c0, c1 = chunks.c1;
   // the token's rows on each side (addresses in scalar registers)
   auto rows_of = [&](const HeadRows &r) {
     return static_cast<const char *>(r.data) + (b * r.batch_stride + i * r.token_stride) * kElem;
@@ -310,17 +311,17 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
       return static_cast<uint32_t>(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[3], 16.f, c[2]), 16.f, c[1]), 16.f, c[0]));
     };
     const uint32_t packed = four(code) | (four(code + 4) << 16);
-    // Stores of four bytes: a lane's chunks follow each other, or (halves) two
-    // neighbours exchange one, the even lane storing both lower chunks.
-    if (IL || !turns) {
-      *reinterpret_cast<uint32_t *>(dst + c0 / 2) = packed;
-    } else if ((lane | 1) < a.rotary_dim / 8) {
-      const uint32_t other = __builtin_amdgcn_update_dpp(0, static_cast<int>(packed), 0xB1, 0xf, 0xf, false);  // lane ^ 1
-      if (lane & 1) *reinterpret_cast<uint32_t *>(dst + (c1 - 4) / 2) = (other >> 16) | (packed & 0xffff0000u);
-      else *reinterpret_cast<uint32_t *>(dst + c0 / 2) = (packed & 0xffffu) | (other << 16);
-    } else {  // the last of an odd number of rotated chunks
+    const rotate::CodeStore how = rotate::code_store(chunks, a.rotary_dim, IL);
+    if (how == rotate::CodeStore::kApart) {
       *reinterpret_cast<uint16_t *>(dst + c0 / 2) = packed;
       *reinterpret_cast<uint16_t *>(dst + c1 / 2) = packed >> 16;
+    } else {
+      uint32_t word = packed;
+      if (how == rotate::CodeStore::kExchange) {
+        const uint32_t other = __builtin_amdgcn_update_dpp(0, static_cast<int>(packed), 0xB1, 0xf, 0xf, false);  // lane ^ 1
+        word = lane & 1 ? (other >> 16) | (packed & 0xffff0000u) : (packed & 0xffffu) | (other << 16);
+      }
+      *reinterpret_cast<uint32_t *>(dst + rotate::word_at(chunks, how, lane)) = word;
     }
     if (lane == 0) *reinterpret_cast<uint32_t *>((side == 1 ? a.k_sq : a.v_sq) + 2 * row) = sq;
     if (out) {
