@@ -593,6 +593,12 @@ nova_kv_status nova_kv_check_metadata(const nova_kv_layout *layout, int32_t num_
  * nova_kv_check_metadata (with num_blocks as given here, <= 0: unknown)
  * before launching; a failing check launches nothing.  This synchronizes,
  * so it is for debugging and not for graph capture.
+ *
+ * nova_kv_q4_append and nova_kv_q4_attn check against their cache's own
+ * num_blocks.  A negative block-table entry (a block not held yet, or released in
+ * front of a window) passes.  What else these calls would leave out or cut is
+ * reported, as a likely mistake: entries from num_blocks on, new tokens outside
+ * the capacity (beyond new_lens), lengths outside [0, max_seq_len].
  */
 void nova_kv_set_debug(int32_t on, int32_t num_blocks);
 

@@ -48,7 +48,7 @@ nova_kv_status debug_check(const nova_kv_layout *lay, int32_t batch, const int32
   const nova_kv_status st = check_metadata(&hl, num_blocks > 0 ? num_blocks : debug_num_blocks(), batch,
                                            seq_lens ? lens.data() : nullptr, max_seq_len,
                                            start_pos ? starts.data() : nullptr, n_new,
-                                           new_lens ? counts.data() : nullptr);
+                                           new_lens ? counts.data() : nullptr, num_blocks > 0);
   if (st != NOVA_KV_OK) {
     std::string d = "debug mode: ";
     d += nova_kv_last_error();

@@ -227,7 +227,7 @@ long long capacity_of(const nova_kv_layout *lay) {
 
 nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch,
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
-                              int32_t n_new, const int32_t *new_lens) {
+                              int32_t n_new, const int32_t *new_lens, bool may_be_absent) {
   nova_kv_status st = check_layout(lay);
   if (st != NOVA_KV_OK) return st;
   if (batch < 0 || n_new < 0) return fail(NOVA_KV_ERR_INVALID_ARG, "batch and n_new must be >= 0");
@@ -238,12 +238,14 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
   if (!start_pos && !step_write && n_new > 0)
     return fail(NOVA_KV_ERR_INVALID_ARG, "writes need start_pos (or seq_lens with n_new == 1)");
   const int bs = lay->block_size, bps = lay->blocks_per_seq;
-  // physical block of logical block blk of sequence b, or a failure
+  // physical block of logical block blk of sequence b (-1: absent), or a failure
   auto phys_of = [&](int b, long long blk, long long *phys) -> nova_kv_status {
     if (blk < 0 || blk >= bps)
       return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d: block %lld outside [0, %d)", b, blk, bps);
     const long long logical = static_cast<long long>(b) * bps + blk;
     const long long p = lay->block_table ? lay->block_table[logical] : logical;
+    *phys = -1;
+    if (may_be_absent && p < 0) return NOVA_KV_OK;
     if (p < 0 || (num_blocks > 0 && p >= num_blocks))
       return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d: block %lld maps to physical block %lld outside [0, %d)", b,
                   blk, p, num_blocks > 0 ? num_blocks : 0x7fffffff);
@@ -275,6 +277,7 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
     for (long long t = w0; t < w1; ++t) {
       long long p = 0;
       if ((st = phys_of(b, t / bs, &p)) != NOVA_KV_OK) return st;
+      if (p < 0) continue;
       const long long row = p * bs + t % bs;
       auto it = row_writer.emplace(row, b);
       if (!it.second)
@@ -293,6 +296,7 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
       for (long long blk = 0; blk < nblk; ++blk) {
         long long p = 0;
         if ((st = phys_of(b, blk, &p)) != NOVA_KV_OK) return st;
+        if (p < 0) continue;
         auto it = block_writer.find(p);
         if (it != block_writer.end() && it->second != b)
           return fail(NOVA_KV_ERR_INVALID_ARG,

@@ -54,10 +54,11 @@ nova_kv_status check_q4_cache(const nova_kv_q4_cache *c);
 
 // Host copies of a call's metadata, checked against the layout (see
 // nova_kv_check_metadata): block_table is a host array here.  With new_lens a
-// sequence writes only its first new_lens[b] (at most n_new) positions.
+// sequence writes only its first new_lens[b] (at most n_new) positions; with
+// may_be_absent a negative block-table entry is a block that holds nothing, and passes.
 nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch,
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
-                              int32_t n_new, const int32_t *new_lens = nullptr);
+                              int32_t n_new, const int32_t *new_lens = nullptr, bool may_be_absent = false);
 
 // Debug mode (nova_kv_set_debug; initially on when the environment variable
 // NOVA_KV_DEBUG is a nonzero number): entry points copy their metadata to
