@@ -220,8 +220,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     }
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
-    qsum[t] = static_cast<float>(total);
-    alpha[t] = usable ? fmaxf(a.qscale / to_fixed, 0x1p-126f) : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    qsum[t] = usable ? static_cast<float>(total) : __builtin_nanf("");  // a row that is not finite: NaN logits, of what it attends
+    alpha[t] = fmaxf(a.qscale / to_fixed, 0x1p-126f);
     ref[t] = kNone;
     sum[t] = off_sum[t] = 0.f;
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};

@@ -265,12 +265,13 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
       for (int e = 0; e < 4; ++e) {
         const float x[2] = {__uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xffff0000u)};
         for (int y = 0; y < 2; ++y) {
+          // a row that is not finite: NaN scores, of what it attends
           const int c = 2 * e + y;  // slots as value_pair has the nibbles: 0, 4, 1, 5, 2, 6, 3, 7
-          qf[t][s][2 * (c & 3) + (c >> 2)] = static_cast<_Float16>(usable ? x[y] * unit : 0.f);
+          qf[t][s][2 * (c & 3) + (c >> 2)] = static_cast<_Float16>(usable ? x[y] * unit : __builtin_nanf(""));
         }
       }
     }
-    alpha[t] = usable ? fmaxf(ldexpf(a.qscale, -up), 0x1p-126f) : __builtin_nanf("");  // a row that is not finite: NaN outputs
+    alpha[t] = fmaxf(ldexpf(a.qscale, -up), 0x1p-126f);
     ref[t] = kNone;
     sum[t] = 0.f;
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
         float top = kNone;
         for (int x = 0; x < 4; ++x)
           for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
-        by[t] = alpha[t] != alpha[t] ? alpha[t] : fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f);
+        by[t] = fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f);
         bound[t] = top * by[t] + value_exp;
         over |= bound[t] > ref[t] + (kTop + kSlack);
       }
