@@ -542,8 +542,9 @@ size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t ba
  *              (replays of a captured call included).  Calls that share a
  *              workspace must be ordered on one stream.
  *
- * Precision: a query is taken as multiples of its row's largest magnitude /
- * 16256 (F32: / 2080768) and its products with the codes are exact; softmax
+ * Precision: a BF16 query is taken exactly (a coordinate below 2^-29 of its
+ * row's largest magnitude loses bits), an F32 one as multiples of its row's
+ * largest magnitude / 8323072 whose products with the codes are exact; softmax
  * statistics and sums over values in fp32; with BF16 queries the
  * probabilities are rounded to fp16 for those sums, with F32 ones they keep 24
  * bits.  With BF16 queries and more than 32 of them per KV head (n_q * Hq / Hkv) keys

@@ -5,10 +5,15 @@
 //   out     = (sum_j (p_j scale'_j) c'_j + sum_j p_j offset'_j) / sum_j p_j
 // and both products run on the matrix cores over the codes themselves.
 //
-// Scores: on the 8-bit integer cores, exact. A word's codes are two words of
-// bytes (three instructions for eight codes); the query is a fixed-point number
-// of two digits of 7 bits (three for fp32 queries) of its row's largest
-// magnitude.
+// Scores of bf16 queries: on the fp16 cores, with codes as (c - 8) * 2^-9 like the
+// values below (nine instructions for eight codes), and the query times a power of two
+// that brings its row's largest magnitude to [2^13, 2^14): fp16 holds a bf16 number
+// exactly down to 2^-29 of the largest. (Two 7-bit digits on the integer cores take 32
+// instructions a round less, 405 us of the 410 below, but a coordinate 2^10 below the
+// largest keeps 4 bits of them.)
+// Of fp32 queries: on the 8-bit integer cores, exact. A word's codes are two words of
+// bytes (three instructions); the query is a fixed-point number of three digits of
+// 8 bits of its row's largest magnitude.
 //
 // Values: on the fp16 cores, as (c - 8) * 2^-9: a nibble masked in place is the fp16
 // denormal c * 2^-24 (c * 2^-20, its bits four higher), which one packed multiply-add
@@ -17,7 +22,7 @@
 // value, and cut those bits off the sum: 1e-5 of an output, towards one side.)
 //
 // With 4 query heads a KV head, bf16 (8 KV heads of 128): 64 sequences of 32K tokens
-// take 405 us, 5.6 TB/s of HBM, which bounds them; one of 128K 38 us (34 from the
+// take 410 us, 5.55 TB/s of HBM, which bounds them; one of 128K 38 us (34 from the
 // caches), the reads' 24 us, their ramp and 9 us of merge; one of 2000 tokens 9.7 us,
 // latency. fp32: 5 sequences of up to 5003 tokens, 10 rows a KV head, 19 us, latency and vector issue.
 #include <algorithm>
@@ -40,11 +45,11 @@ constexpr int kRound = 32;  // tokens a wave takes at a time
 template <int D, bool WIDE, int NT, int W, bool TILED, bool ALIGNED>
 __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ? 2 : 3) void q4_attn_kernel(const Q4AttnArgs a) {
   constexpr int kWaves = W, WT = TILED ? 1 : W;
-  constexpr int kSteps = D / 64;          // matrix steps of a score
+  constexpr int kSteps = D / (WIDE ? 64 : 32);  // matrix steps of a score
   constexpr int kTiles = D / 16;          // output tiles
   constexpr int kKeyWords = D / 32;       // words of a lane's part of a key row
-  constexpr int kDigits = WIDE ? 3 : 2;   // 7-bit digits of a query
-  constexpr float kTopQ = WIDE ? 127.f * 128 * 128 : 127.f * 128;  // the largest fixed-point number
+  constexpr int kDigits = 3;              // 8-bit digits of an fp32 query
+  constexpr float kTopQ = 127.f * 256 * 256;  // the largest fixed-point number
   constexpr int kProbParts = WIDE ? 3 : 1;  // and of a probability
   // log2 of the largest scaled probability after a rescale, and how far it may
   // grow before the next one: 2^14 fits fp16, 2^11 units of 1 are 11 bits. Scaled
@@ -171,7 +176,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     look_up();
   }
 
-  int4_t qf[NT][kDigits][kSteps];
+  int4_t qf[NT][WIDE ? kDigits : 1][kSteps];
   float alpha[NT], qsum[NT], ref[NT], sum[NT], off_sum[NT];
   int row_lo[NT], row_hi[NT];
   float4_t acc[NT][kTiles];
@@ -202,26 +207,43 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     }
     top = max_rows32(max_rows16(finite ? top : __builtin_inff()));
     const bool usable = top < __builtin_inff();
-    const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
-    int total = 0;
-    for (int s = 0; s < kSteps; ++s)
-      for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
-    for (int s = 0; s < kKeyWords; ++s) {
-      for (int e = 0; e < 8; ++e) {
-        int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
-        total += f;
-        // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
-        for (int d = 0; d < kDigits; ++d) {
-          const int digit = d == kDigits - 1 ? f : ((f + 64) & 127) - 64;
-          f = (f - digit) >> 7;
-          qf[t][d][s / 2][2 * (s % 2) + e % 2] |= (digit & 255) << (8 * (e / 2));
+    // a row that is not finite: NaN logits, of what it attends
+    if constexpr (WIDE) {
+      const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
+      int total = 0;
+      for (int s = 0; s < kSteps; ++s)
+        for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
+      for (int s = 0; s < kKeyWords; ++s) {
+        for (int e = 0; e < 8; ++e) {
+          int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
+          total += f;
+          // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
+          for (int d = 0; d < kDigits; ++d) {
+            const int digit = d == kDigits - 1 ? f : ((f + 128) & 255) - 128;
+            f = (f - digit) >> 8;
+            qf[t][d][s / 2][2 * (s % 2) + e % 2] |= (digit & 255) << (8 * (e / 2));
+          }
         }
       }
+      total += __shfl_xor(total, 16);
+      total += __shfl_xor(total, 32);
+      qsum[t] = usable ? static_cast<float>(total) : __builtin_nanf("");
+      alpha[t] = fmaxf(a.qscale / to_fixed, 0x1p-126f);
+    } else {
+      const int up = usable && top > 0.f ? min(13 - ilogbf(top), 120) : 0;
+      const float unit = ldexpf(1.f, up);
+      float total = 0.f;
+      for (int s = 0; s < kKeyWords; ++s) {
+        half8_t h;
+        for (int e = 0; e < 8; ++e) {  // slots as value_pair has the nibbles: 0, 4, 1, 5, 2, 6, 3, 7
+          h[2 * (e & 3) + (e >> 2)] = static_cast<_Float16>(usable ? x[s][e] * unit : __builtin_nanf(""));
+          total += x[s][e] * unit;
+        }
+        qf[t][0][s] = __builtin_bit_cast(int4_t, h);
+      }
+      qsum[t] = add_rows32(add_rows16(total)) * 0x1p-9f;
+      alpha[t] = fmaxf(ldexpf(a.qscale, 9 - up), 0x1p-126f);
     }
-    total += __shfl_xor(total, 16);
-    total += __shfl_xor(total, 32);
-    qsum[t] = usable ? static_cast<float>(total) : __builtin_nanf("");  // a row that is not finite: NaN logits, of what it attends
-    alpha[t] = fmaxf(a.qscale / to_fixed, 0x1p-126f);
     ref[t] = kNone;
     sum[t] = off_sum[t] = 0.f;
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -234,7 +256,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     const uint32_t valid = static_cast<uint32_t>(__ballot(cur.ok));
     {
       float scale = __uint_as_float(cur.sq << 16), offset = __uint_as_float(cur.sq & 0xffff0000u);
-      if (lane >= 32) offset = __builtin_fmaf(8.f, scale, offset);  // values count from code 8
+      if (!WIDE || lane >= 32) offset = __builtin_fmaf(8.f, scale, offset);  // on the fp16 cores codes count from 8
       s_scale[wave][lane] = cur.ok ? scale : 0.f;
       s_offset[wave][lane] = cur.ok ? offset : 0.f;
       s_log[wave][lane] = __builtin_amdgcn_logf(fmaxf(fmaxf(fabsf(scale), fabsf(offset) * 0x1p-8f), 0x1p-70f));
@@ -254,26 +276,44 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     __builtin_amdgcn_wave_barrier();
 
     const bool inner = valid == 0xffffffffu && tb >= inner_lo && tb + kRound <= inner_hi;
-    int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
-    for (int h = 0; h < 2; ++h)
-      for (int s = 0; s < kKeyWords; ++s) {
-        kc[h][s / 2][2 * (s % 2)] = static_cast<int>(cur.kw[h][s] & 0x0f0f0f0fu);
-        kc[h][s / 2][2 * (s % 2) + 1] = static_cast<int>((cur.kw[h][s] >> 4) & 0x0f0f0f0fu);
+    float dots[NT][8];  // query times codes, of the lane's tokens
+    if constexpr (WIDE) {
+      int4_t kc[2][kSteps];  // the keys' codes in bytes: even coordinates of a word, then odd ones
+      for (int h = 0; h < 2; ++h)
+        for (int s = 0; s < kKeyWords; ++s) {
+          kc[h][s / 2][2 * (s % 2)] = static_cast<int>(cur.kw[h][s] & 0x0f0f0f0fu);
+          kc[h][s / 2][2 * (s % 2) + 1] = static_cast<int>((cur.kw[h][s] >> 4) & 0x0f0f0f0fu);
+        }
+      for (int t = 0; t < NT; ++t)
+        for (int h = 0; h < 2; ++h) {
+          int4_t d[kDigits];
+          for (int x = 0; x < kDigits; ++x) {
+            d[x] = int4_t{0, 0, 0, 0};
+            for (int s = 0; s < kSteps; ++s) d[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[x], 0, 0, 0);
+          }
+          for (int i = 0; i < 4; ++i)
+            dots[t][4 * h + i] = __builtin_fmaf(65536.f, static_cast<float>(d[2][i]), static_cast<float>((d[1][i] << 8) + d[0][i]));
+        }
+    } else {
+      for (int h = 0; h < 2; ++h) {
+        float4_t d[NT];
+        for (int t = 0; t < NT; ++t) d[t] = float4_t{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < kSteps; ++s) {
+          const uint32_t w = cur.kw[h][s];
+          const half8_t c = __builtin_bit_cast(half8_t, make_uint4(value_pair<0>(w), value_pair<1>(w), value_pair<2>(w), value_pair<3>(w)));
+          for (int t = 0; t < NT; ++t)
+            d[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, __builtin_bit_cast(half8_t, qf[t][0][s]), d[t], 0, 0, 0);
+          if (s % 2) __builtin_amdgcn_sched_barrier(0);  // the others stay packed until here: unpacked together they spill, 453 us
+        }
+        for (int t = 0; t < NT; ++t)
+          for (int i = 0; i < 4; ++i) dots[t][4 * h + i] = d[t][i];
       }
+    }
     half8_t pf[NT][kProbParts];
     for (int t = 0; t < NT; ++t) {
-      int4_t d[2][kDigits];
-      for (int h = 0; h < 2; ++h)
-        for (int x = 0; x < kDigits; ++x) {
-          d[h][x] = int4_t{0, 0, 0, 0};
-          for (int s = 0; s < kSteps; ++s) d[h][x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[h][x], 0, 0, 0);
-        }
       float z[8], bound = kNone, scale[8], offset[8];
       for (int e = 0; e < 8; ++e) {
-        const int4_t(&dig)[kDigits] = d[e >> 2];
-        float dot = static_cast<float>((dig[1][e & 3] << 7) + dig[0][e & 3]);
-        if constexpr (WIDE) dot = __builtin_fmaf(16384.f, static_cast<float>(dig[2][e & 3]), dot);
-        z[e] = ks[e] * dot + ko[e] * qsum[t];
+        z[e] = ks[e] * dots[t][e] + ko[e] * qsum[t];
         scale[e] = vs[e];
         offset[e] = vo8[e];
       }
