@@ -50,6 +50,10 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
   constexpr int kKeyWords = D / 32;       // words of a lane's part of a key row
   constexpr int kDigits = 3;              // 8-bit digits of an fp32 query
   constexpr float kTopQ = 127.f * 256 * 256;  // the largest fixed-point number
+  // A logit in front of its row's factor alpha: keys times this, so that
+  // the products of large ones (up to 2^114) with scaled queries stay in fp32.
+  constexpr int kKeyExp = 6;
+  constexpr float kKeyUnit = 0x1p-6f;
   constexpr int kProbParts = WIDE ? 3 : 1;  // and of a probability
   // log2 of the largest scaled probability after a rescale, and how far it may
   // grow before the next one: 2^14 fits fp16, 2^11 units of 1 are 11 bits. Scaled
@@ -209,13 +213,14 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     const bool usable = top < __builtin_inff();
     // a row that is not finite: NaN logits, of what it attends
     if constexpr (WIDE) {
-      const float to_fixed = usable && top > 0.f ? fminf(kTopQ / top, 0x1p120f) : 1.f;
+      const float lift = top < 0x1p-60f ? 0x1p60f : 1.f;  // kTopQ over a smaller magnitude may be no float
+      const float to_fixed = usable && top > 0.f ? kTopQ / (top * lift) : 1.f;
       int total = 0;
       for (int s = 0; s < kSteps; ++s)
         for (int d = 0; d < kDigits; ++d) qf[t][d][s] = int4_t{0, 0, 0, 0};
       for (int s = 0; s < kKeyWords; ++s) {
         for (int e = 0; e < 8; ++e) {
-          int f = usable ? static_cast<int>(rintf(x[s][e] * to_fixed)) : 0;
+          int f = usable ? static_cast<int>(rintf(x[s][e] * lift * to_fixed)) : 0;
           total += f;
           // byte e / 2 of the word of even (odd) coordinates of code word s; digits from the lowest, balanced
           for (int d = 0; d < kDigits; ++d) {
@@ -227,8 +232,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
       }
       total += __shfl_xor(total, 16);
       total += __shfl_xor(total, 32);
-      qsum[t] = usable ? static_cast<float>(total) : __builtin_nanf("");
-      alpha[t] = fmaxf(a.qscale / to_fixed, 0x1p-126f);
+      qsum[t] = usable ? static_cast<float>(total) * 0x1p-16f : __builtin_nanf("");
+      alpha[t] = ldexpf(a.qscale / to_fixed, 16 + kKeyExp) / lift;
     } else {
       const int up = usable && top > 0.f ? min(13 - ilogbf(top), 120) : 0;
       const float unit = ldexpf(1.f, up);
@@ -242,8 +247,9 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
         qf[t][0][s] = __builtin_bit_cast(int4_t, h);
       }
       qsum[t] = add_rows32(add_rows16(total)) * 0x1p-9f;
-      alpha[t] = fmaxf(ldexpf(a.qscale, 9 - up), 0x1p-126f);
+      alpha[t] = ldexpf(a.qscale, 9 - up + kKeyExp);
     }
+    alpha[t] = fminf(fmaxf(alpha[t], 0x1p-126f), 0x1p127f);  // finite: zero queries have logits of zero
     ref[t] = kNone;
     sum[t] = off_sum[t] = 0.f;
     for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -257,6 +263,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
     {
       float scale = __uint_as_float(cur.sq << 16), offset = __uint_as_float(cur.sq & 0xffff0000u);
       if (!WIDE || lane >= 32) offset = __builtin_fmaf(8.f, scale, offset);  // on the fp16 cores codes count from 8
+      if (lane < 32) scale *= kKeyUnit, offset *= kKeyUnit;
       s_scale[wave][lane] = cur.ok ? scale : 0.f;
       s_offset[wave][lane] = cur.ok ? offset : 0.f;
       s_log[wave][lane] = __builtin_amdgcn_logf(fmaxf(fmaxf(fabsf(scale), fabsf(offset) * 0x1p-8f), 0x1p-70f));
@@ -292,7 +299,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? 1 : NT > 1 ? 1 : WIDE && D == 128 ?
             for (int s = 0; s < kSteps; ++s) d[x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kc[h][s], qf[t][x][s], d[x], 0, 0, 0);
           }
           for (int i = 0; i < 4; ++i)
-            dots[t][4 * h + i] = __builtin_fmaf(65536.f, static_cast<float>(d[2][i]), static_cast<float>((d[1][i] << 8) + d[0][i]));
+            dots[t][4 * h + i] = __builtin_fmaf(0x1p-16f, static_cast<float>((d[1][i] << 8) + d[0][i]), static_cast<float>(d[2][i]));
         }
     } else {
       for (int h = 0; h < 2; ++h) {

@@ -37,12 +37,14 @@ constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability af
 
 // The same value in every lane, in a scalar register.
 __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
-// Exponent of a power of two above a magnitude (at least 2^-90, so that sums of
-// probabilities over it stay in range; half of it beyond 2^127), from its bits.
-__device__ __forceinline__ int exponent_of(const float mag) {
+// Exponent of a power of two above a magnitude (half of it beyond 2^127), from its
+// bits; at least 2^least.
+__device__ __forceinline__ int exponent_of(const float mag, const int least) {
   const int e = uniform(__builtin_bit_cast(int, mag)) >> 23;  // mag >= 0
-  return min(max(e - 126, -90), 127);
+  return min(max(e - 126, least), 127);
 }
+// Of keys, so that 2^17 over it is a float; of values, so that sums of probabilities over it stay in range.
+constexpr int kLeastKey = -110, kLeastValue = -90;
 __device__ __forceinline__ float power_of_two(const int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
 // W: waves of a workgroup, a multiple of four. ALIGNED: blocks of a multiple of 16 rows.
@@ -155,8 +157,8 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     if (part == 0 && lane == 0) s_valid[slot][group] = valid;
   };
   auto exponents = [&](const int slot, const int y, int &ek, int &ev) {
-    ek = exponent_of(fmaxf(s_mag[slot][2 * y][0], s_mag[slot][2 * y + 1][0]));
-    ev = exponent_of(fmaxf(s_mag[slot][2 * y][1], s_mag[slot][2 * y + 1][1]));
+    ek = exponent_of(fmaxf(s_mag[slot][2 * y][0], s_mag[slot][2 * y + 1][0]), kLeastKey);
+    ev = exponent_of(fmaxf(s_mag[slot][2 * y][1], s_mag[slot][2 * y + 1][1]), kLeastValue);
   };
   auto unpack = [&](const Round &r, const int ek, const int ev, half8_t *to) {
     to += own * kBuffer;
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
         float top = kNone;
         for (int x = 0; x < 4; ++x)
           for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
-        by[t] = fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f);
+        by[t] = fminf(fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f), 0x1p127f);
         bound[t] = top * by[t] + value_exp;
         over |= bound[t] > ref[t] + (kTop + kSlack);
       }
