@@ -548,8 +548,8 @@ size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t ba
  * statistics and sums over values in fp32; with BF16 queries the
  * probabilities are rounded to fp16 for those sums, with F32 ones they keep 24
  * bits.  With BF16 queries and more than 32 of them per KV head (n_q * Hq / Hkv) keys
- * and values are rounded to fp16: to 2^-12 of theirs, or to 2^-18 of the largest
- * magnitude among the 64 tokens around, whichever is more.  Results do not
+ * and values are rounded to fp16, by at most 2^-12 of the power of two above their
+ * row's largest magnitude.  Results do not
  * depend on which workgroups finish first.
  * batch == 0 or n_q == 0 is a valid no-op.
  */

@@ -9,18 +9,19 @@
 // among them (10.5 with four waves, which unpack for half the rows), where q4_attn.hip's
 // exact sums over the codes take 14.5 (but no LDS, and no rounding of keys and values).
 //
-// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 504 us, 955
+// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 520 us, 925
 // TFLOP/s. Vector (about 310 us) and matrix instructions (192 us) bound it, which add
 // on a SIMD. Four waves take 554 us, and the same without the LDS 1211; with few tiles
 // the smaller ones win, by parallelism and by a merge of splits over more workgroups.
 //
-// Keys and values are divided by 2^7 times a power of two at or above the
-// largest magnitude of the 64 tokens (each side its own), which the exponent and
-// the output take back: a scale's and an offset's 8 bits then fit fp16, and one
+// Keys and values are divided by 2^7 times a power of two at or above the largest
+// magnitude of the 64 tokens (each side its own), which the exponent and the
+// output take back: a scale's and an offset's 8 bits then fit fp16, and one
 // packed multiply-add unpacks two codes (fp16 denormals as they lie, c * 2^-24)
 // with one rounding: half a step of fp16, 2^-12 of the power of two above the number,
-// or of the smallest normal one, 2^-18 of the largest magnitude, below. bf16 queries
-// and outputs show 2^-9 of theirs, so tokens up to 2^9 below the largest lose nothing.
+// or of the smallest normal one, 2^-18 of the tokens' power, below. Tokens at most 2^5 apart
+// keep 2^-12 of their row's largest so; where 64 tokens are further apart, each has a power of its own, so
+// that no other token, hidden or of no weight, takes bits of it.
 // (2^7 is the least that keeps 15 scales, at most four times the power, in fp16.)
 #include <type_traits>
 
@@ -37,14 +38,20 @@ constexpr float kTop = 6.f, kSlack = 8.f;  // log2 of the largest probability af
 
 // The same value in every lane, in a scalar register.
 __device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
-// Exponent of a power of two above a magnitude (half of it beyond 2^127), from its
-// bits; at least 2^least.
-__device__ __forceinline__ int exponent_of(const float mag, const int least) {
-  const int e = uniform(__builtin_bit_cast(int, mag)) >> 23;  // mag >= 0
-  return min(max(e - 126, least), 127);
-}
+// Exponent of a power of two above a magnitude (half of it beyond 2^127) whose biased exponent is e; at least 2^least.
+__device__ __forceinline__ int power_above(const int e, const int least) { return min(max(e - 126, least), 127); }
 // Of keys, so that 2^17 over it is a float; of values, so that sums of probabilities over it stay in range.
 constexpr int kLeastKey = -110, kLeastValue = -90;
+// Exponents of 64 tokens this far apart at most share one: the least keeps 2^-12 of its largest.
+constexpr int kSpread = 5;
+typedef short short2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ int larger2(const int x, const int y) {  // of both halves
+  return __builtin_bit_cast(int, __builtin_elementwise_max(__builtin_bit_cast(short2_t, x), __builtin_bit_cast(short2_t, y)));
+}
+template <int N>
+__device__ __forceinline__ int larger2_of_row(const int x) {
+  return larger2(x, __builtin_amdgcn_update_dpp(0, x, 0x120 + N, 0xf, 0xf, false));
+}
 __device__ __forceinline__ float power_of_two(const int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
 // W: waves of a workgroup, a multiple of four. ALIGNED: blocks of a multiple of 16 rows.
@@ -58,7 +65,9 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
   __shared__ half8_t s_tokens[2][kParts * kBuffer];
   __shared__ uint32_t s_rows[ALIGNED ? 1 : kWaves][32];
   __shared__ __align__(16) uint32_t s_pack[kWaves][64];
-  __shared__ float s_mag[3][2 * kParts][2];     // [round mod 3][32 tokens][keys, values]
+  // [round mod 3][32 tokens][keys, values]: the largest biased exponent of their magnitudes, and in the high half less the smallest
+  __shared__ int s_exp[3][2 * kParts][2];
+  __shared__ __align__(16) float s_unit[2][2][kTokens];  // [round mod 2][keys, values]: a token's power of two (of keys, over its 64 tokens')
   __shared__ uint32_t s_valid[3][2 * kParts];
   __shared__ float s_inv[Lds::kRows];
   __shared__ int s_last;
@@ -136,40 +145,56 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     }
     r.sq = sq[row];
   };
+  auto biased_of = [](const float mag) { return __builtin_bit_cast(int, mag) >> 23; };  // of mag >= 0
   // scale and offset of the lane's token, 0 for hidden tokens
   auto scale_of = [&](const Round &r, float &scale, float &offset) {
     scale = r.ok ? __uint_as_float(r.sq << 16) : 0.f;
     offset = r.ok ? __uint_as_float(r.sq & 0xffff0000u) : 0.f;
     // the largest magnitude of the row (of code 0 or 15); NaN or infinity where one is
     const float last = __builtin_fmaf(15.f, scale, offset);
-    return last - last == 0.f ? fmaxf(fabsf(offset), fabsf(last)) : last;
+    return last - last == 0.f ? fmaxf(fabsf(offset), fabsf(last)) : fabsf(last);
   };
   auto announce = [&](const Round &r, const int slot) {
-    float scale, offset, mag = scale_of(r, scale, offset);
-    mag = mag < __builtin_inff() ? mag : 0.f;
-    mag = fmaxf(mag, lut::row_ror<8>(mag));
-    mag = fmaxf(mag, lut::row_ror<4>(mag));
-    mag = fmaxf(mag, lut::row_ror<2>(mag));
-    mag = fmaxf(mag, lut::row_ror<1>(mag));
-    mag = max_rows16(mag);  // over the 32 lanes of a side
+    float scale, offset;
+    const float mag = scale_of(r, scale, offset);
+    const int e = biased_of(mag);
+    int both = mag > 0.f && mag < __builtin_inff() ? e | ((255 - e) << 16) : 0;
+    both = larger2_of_row<8>(both);
+    both = larger2_of_row<4>(both);
+    both = larger2_of_row<2>(both);
+    both = larger2_of_row<1>(both);
+    const lut::SwapPair rows = lut::swap_rows16(__builtin_bit_cast(float, both));  // over the 32 lanes of a side
+    both = larger2(__builtin_bit_cast(int, rows.a), __builtin_bit_cast(int, rows.b));
     const uint32_t valid = static_cast<uint32_t>(__ballot(r.ok));
-    if (part == 0 && (lane & 31) == 0) s_mag[slot][group][lane >> 5] = mag;
+    if (part == 0 && (lane & 31) == 0) s_exp[slot][group][lane >> 5] = both;
     if (part == 0 && lane == 0) s_valid[slot][group] = valid;
   };
+  // the exponents of a round's part, and whether its tokens have their own
   auto exponents = [&](const int slot, const int y, int &ek, int &ev) {
-    ek = exponent_of(fmaxf(s_mag[slot][2 * y][0], s_mag[slot][2 * y + 1][0]), kLeastKey);
-    ev = exponent_of(fmaxf(s_mag[slot][2 * y][1], s_mag[slot][2 * y + 1][1]), kLeastValue);
+    auto of = [&](const int side, const int least, int &e) {
+      const int both = uniform(larger2(s_exp[slot][2 * y][side], s_exp[slot][2 * y + 1][side]));
+      e = power_above(both & 0xffff, least);
+      return e - power_above(255 - (both >> 16), least) > kSpread;
+    };
+    const bool k = of(0, kLeastKey, ek), v = of(1, kLeastValue, ev);
+    return k || v;
   };
-  auto unpack = [&](const Round &r, const int ek, const int ev, half8_t *to) {
-    to += own * kBuffer;
+  auto unpack = [&](const Round &r, const int slot, const int buffer) {
+    half8_t *const to = s_tokens[buffer] + own * kBuffer;
+    int ek, ev;
+    const bool spread = exponents(slot, own, ek, ev);
     float scale, offset;
-    const bool odd = !(scale_of(r, scale, offset) < __builtin_inff());
+    const float mag = scale_of(r, scale, offset);
+    const bool odd = !(mag < __builtin_inff());
     // A value that is not finite would reach the rows it is hidden from (0 * NaN): its
     // token's key becomes NaN instead, and the value 0.
     const uint64_t odds = __ballot(odd);
     const uint32_t any_odd = static_cast<uint32_t>(odds) | static_cast<uint32_t>(odds >> 32);
     const bool token_odd = (any_odd >> (lane & 31)) & 1u;
-    const float unit = lane < 32 ? power_of_two(-ek) : power_of_two(-ev);
+    const int shared = lane < 32 ? ek : ev;
+    const int e = spread ? min(power_above(odd ? 0 : biased_of(mag), lane < 32 ? kLeastKey : kLeastValue), shared) : shared;
+    const float unit = power_of_two(-e);
+    if (part == 0) s_unit[buffer][lane >> 5][32 * group + (lane & 31)] = power_of_two(lane < 32 ? e - ek : e);
     scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p17f);  // s <= 4 / 15 / unit: below 2^15.1
     offset = token_odd ? 0.f : offset * (unit * 0x1p-7f);
     const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
@@ -281,11 +306,9 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
 
   int slot = 1;  // of the round behind the one at hand
   if (any) {
-    int ek, ev;
     announce(cur, 0);
     __syncthreads();
-    exponents(0, own, ek, ev);
-    unpack(cur, ek, ev, s_tokens[0]);
+    unpack(cur, 0, 0);
     request(cur);
     look_up();
     announce(cur, 1);
@@ -306,10 +329,16 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
       const int tb0 = tb + 64 * y;
       if (idle || tb0 >= wave_hi || tb0 + 64 <= wave_lo) return;
       int ek, ev;
-      exponents(slot0, y, ek, ev);
+      const bool spread = exponents(slot0, y, ek, ev);
+      const float *const key_units = &s_unit[round & 1][0][64 * y + 4 * j], *const value_units = &s_unit[round & 1][1][64 * y + 4 * j];
       const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][2 * y])), static_cast<uint32_t>(uniform(s_valid[slot0][2 * y + 1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb0 >= inner_lo && tb0 + 64 <= inner_hi;
-      const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev), value_unit = power_of_two(ev);
+      const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev);
+      if (spread) {  // in front of the masks: a unit may be 0
+        for (int t = 0; t < kRowTiles; ++t)
+          for (int x = 0; x < 4; ++x)
+            for (int i = 0; i < 4; ++i) s[t][x][i] *= key_units[16 * x + i];
+      }
       if (!inner) {  // without branches in it the scores stay where they are, and inner rounds copy nothing
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
@@ -327,6 +356,12 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
           for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][x][i]);
         by[t] = fminf(fmaxf(alpha[t] * 128.f * key_unit, 0x1p-126f), 0x1p127f);
         bound[t] = top * by[t] + value_exp;
+        if (spread) {
+          bound[t] = kNone;
+          for (int x = 0; x < 4; ++x)
+            for (int i = 0; i < 4; ++i)
+              bound[t] = fmaxf(bound[t], __builtin_fmaf(s[t][x][i], by[t], static_cast<float>(biased_of(value_units[16 * x + i]) - 127)));
+        }
         over |= bound[t] > ref[t] + (kTop + kSlack);
       }
       if (__any(over)) {
@@ -350,7 +385,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
           for (int i = 0; i < 4; ++i) {
             const float p = exp2_raw(__builtin_fmaf(s[t][x][i], by[t], -r));
             sum[t] += p;
-            pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p * value_unit);
+            pf[t][x >> 1][4 * (x & 1) + i] = static_cast<_Float16>(p * value_units[16 * x + i]);
           }
       };
       for (int t = 0; t < kRowTiles; ++t) probabilities(t);
@@ -363,9 +398,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     const half8_t *tokens = s_tokens[round & 1];
     float4_t s[kRowTiles][4];
     scores(tokens, s);
-    int next_ek, next_ev;  // of the wave's tokens of the next round
-    exponents(slot, own, next_ek, next_ev);
-    unpack(cur, next_ek, next_ev, s_tokens[(round + 1) & 1]);
+    unpack(cur, slot, (round + 1) & 1);
     request(cur);  // past the end: hidden
     look_up();
     attend(tokens, s, 0);

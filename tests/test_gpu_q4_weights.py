@@ -52,6 +52,7 @@ SIZES = {
     "2^31, then 1": lambda t, S: np.where(t < S // 4, 2.0 ** 31, 1.0),
     "zero, then 2^40": lambda t, S: np.where(t < S // 2, 0.0, 2.0 ** 40),
     "zero, then 2^60": lambda t, S: np.where(t < S // 2, 0.0, 2.0 ** 60),
+    "2^-100, then 2^100": lambda t, S: np.where(t < S // 2, 2.0 ** -100, 2.0 ** 100),
     "2^100, then 2^-100": lambda t, S: np.where(t < S // 2, 2.0 ** 100, 2.0 ** -100),
 }
 
