@@ -5,13 +5,13 @@
 // tokens at a time. The waves unpack the tokens' rows once, between them, to fp16
 // keys and values in LDS, in the order in which the matrix cores take them, the
 // next ones while these are used. Unpacked, a score needs no more than its
-// multiply-add into the exponent: 8.5 vector instructions each, an exponential
-// among them (10.5 with four waves, which unpack for half the rows), where q4_attn.hip's
+// multiply-add into the exponent: 8 vector instructions each, an exponential
+// among them (10 with four waves, which unpack for half the rows), where q4_attn.hip's
 // exact sums over the codes take 14.5 (but no LDS, and no rounding of keys and values).
 //
-// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 520 us, 925
-// TFLOP/s. Vector (about 310 us) and matrix instructions (192 us) bound it, which add
-// on a SIMD. Four waves take 554 us, and the same without the LDS 1211; with few tiles
+// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 522 us, 921
+// TFLOP/s. Vector (about 320 us) and matrix instructions (192 us) bound it, which add
+// on a SIMD. Four waves take 616 us, and the same without the LDS (an earlier step) 1211; with few tiles
 // the smaller ones win, by parallelism and by a merge of splits over more workgroups.
 //
 // Keys and values are divided by 2^7 times a power of two at or above the largest
@@ -44,14 +44,7 @@ __device__ __forceinline__ int power_above(const int e, const int least) { retur
 constexpr int kLeastKey = -110, kLeastValue = -90;
 // Exponents of 64 tokens this far apart at most share one: the least keeps 2^-12 of its largest.
 constexpr int kSpread = 5;
-typedef short short2_t __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ int larger2(const int x, const int y) {  // of both halves
-  return __builtin_bit_cast(int, __builtin_elementwise_max(__builtin_bit_cast(short2_t, x), __builtin_bit_cast(short2_t, y)));
-}
-template <int N>
-__device__ __forceinline__ int larger2_of_row(const int x) {
-  return larger2(x, __builtin_amdgcn_update_dpp(0, x, 0x120 + N, 0xf, 0xf, false));
-}
+constexpr int kFinite = 0x7f7fffff;  // bits of the largest float
 __device__ __forceinline__ float power_of_two(const int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
 // W: waves of a workgroup, a multiple of four. ALIGNED: blocks of a multiple of 16 rows.
@@ -65,9 +58,11 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
   __shared__ half8_t s_tokens[2][kParts * kBuffer];
   __shared__ uint32_t s_rows[ALIGNED ? 1 : kWaves][32];
   __shared__ __align__(16) uint32_t s_pack[kWaves][64];
-  // [round mod 3][32 tokens][keys, values]: the largest biased exponent of their magnitudes, and in the high half less the smallest
-  __shared__ int s_exp[3][2 * kParts][2];
+  // [round mod 3][32 tokens][keys, values]: the largest magnitude, and by how many bits the smallest is below kFinite
+  __shared__ __align__(16) float s_mag[3][2 * kParts][2][2];
   __shared__ __align__(16) float s_unit[2][2][kTokens];  // [round mod 2][keys, values]: a token's power of two (of keys, over its 64 tokens')
+  // [round mod 2]: the part's exponents of keys and values, 128 added, and whether its tokens have their own
+  __shared__ int s_shared[2][kParts];
   __shared__ uint32_t s_valid[3][2 * kParts];
   __shared__ float s_inv[Lds::kRows];
   __shared__ int s_last;
@@ -157,24 +152,24 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
   auto announce = [&](const Round &r, const int slot) {
     float scale, offset;
     const float mag = scale_of(r, scale, offset);
-    const int e = biased_of(mag);
-    int both = mag > 0.f && mag < __builtin_inff() ? e | ((255 - e) << 16) : 0;
-    both = larger2_of_row<8>(both);
-    both = larger2_of_row<4>(both);
-    both = larger2_of_row<2>(both);
-    both = larger2_of_row<1>(both);
-    const lut::SwapPair rows = lut::swap_rows16(__builtin_bit_cast(float, both));  // over the 32 lanes of a side
-    both = larger2(__builtin_bit_cast(int, rows.a), __builtin_bit_cast(int, rows.b));
+    // of the two waves with these tokens, part 0 seeks the largest, part 1 the smallest that is not 0
+    float most = mag > 0.f && mag < __builtin_inff() ? part ? __builtin_bit_cast(float, kFinite - __builtin_bit_cast(int, mag)) : mag : 0.f;
+    most = fmaxf(most, lut::row_ror<8>(most));
+    most = fmaxf(most, lut::row_ror<4>(most));
+    most = fmaxf(most, lut::row_ror<2>(most));
+    most = fmaxf(most, lut::row_ror<1>(most));
+    most = max_rows16(most);  // over the 32 lanes of a side
     const uint32_t valid = static_cast<uint32_t>(__ballot(r.ok));
-    if (part == 0 && (lane & 31) == 0) s_exp[slot][group][lane >> 5] = both;
+    if ((lane & 31) == 0) s_mag[slot][group][lane >> 5][part] = most;
     if (part == 0 && lane == 0) s_valid[slot][group] = valid;
   };
   // the exponents of a round's part, and whether its tokens have their own
   auto exponents = [&](const int slot, const int y, int &ek, int &ev) {
     auto of = [&](const int side, const int least, int &e) {
-      const int both = uniform(larger2(s_exp[slot][2 * y][side], s_exp[slot][2 * y + 1][side]));
-      e = power_above(both & 0xffff, least);
-      return e - power_above(255 - (both >> 16), least) > kSpread;
+      const float *const m[2] = {s_mag[slot][2 * y][side], s_mag[slot][2 * y + 1][side]};
+      const int most = uniform(__builtin_bit_cast(int, fmaxf(m[0][0], m[1][0]))), left = uniform(__builtin_bit_cast(int, fmaxf(m[0][1], m[1][1])));
+      e = power_above(most >> 23, least);
+      return e - power_above((kFinite - left) >> 23, least) > kSpread;
     };
     const bool k = of(0, kLeastKey, ek), v = of(1, kLeastValue, ev);
     return k || v;
@@ -194,6 +189,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     const int shared = lane < 32 ? ek : ev;
     const int e = spread ? min(power_above(odd ? 0 : biased_of(mag), lane < 32 ? kLeastKey : kLeastValue), shared) : shared;
     const float unit = power_of_two(-e);
+    if (part == 0 && lane == 0) s_shared[buffer][own] = (ek + 128) | ((ev + 128) << 8) | (spread ? 1 << 16 : 0);
     if (part == 0) s_unit[buffer][lane >> 5][32 * group + (lane & 31)] = power_of_two(lane < 32 ? e - ek : e);
     scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p17f);  // s <= 4 / 15 / unit: below 2^15.1
     offset = token_odd ? 0.f : offset * (unit * 0x1p-7f);
@@ -328,8 +324,8 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     auto attend = [&](const half8_t *tokens, float4_t (&s)[kRowTiles][4], const int y) {
       const int tb0 = tb + 64 * y;
       if (idle || tb0 >= wave_hi || tb0 + 64 <= wave_lo) return;
-      int ek, ev;
-      const bool spread = exponents(slot0, y, ek, ev);
+      const int shared = uniform(s_shared[round & 1][y]), ek = (shared & 255) - 128, ev = ((shared >> 8) & 255) - 128;
+      const bool spread = shared >> 16;
       const float *const key_units = &s_unit[round & 1][0][64 * y + 4 * j], *const value_units = &s_unit[round & 1][1][64 * y + 4 * j];
       const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][2 * y])), static_cast<uint32_t>(uniform(s_valid[slot0][2 * y + 1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb0 >= inner_lo && tb0 + 64 <= inner_hi;

@@ -11,6 +11,7 @@ import torch
 
 from oracle import q4
 from test_gpu_q4_attn import BF, make_cache, nk, reference_and_bounds, say  # noqa: F401
+from test_gpu_q4_weights import check_sampled
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +68,18 @@ def test_tokens_of_no_weight_far_above(nk, size, D):  # noqa: F811
         # the output's rounding, a probability's and a value's to fp16, the sums'; of the large ones size e^-256 and less: nothing
         tol = np.abs(ref) * 2.0 ** -8 + V * (2.0 ** -11 + 2.0 ** -10 + 2.0 ** -18)
         assert (np.abs(got[0, i] - ref) <= tol).all(), i
+
+
+@pytest.mark.parametrize("side", ("k", "v"))
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("size", (1e4, 1e30))
+def test_hidden_tokens_of_large_tiles(nk, size, D, side):  # noqa: F811
+    """The same in tiles of 256 rows: tokens in front of every window."""
+    say(f"hidden {side} {size} D={D}, tiles of 256 rows")
+    rng = np.random.default_rng(63)
+    seqs, n, window = [641, 650, 700] * 5, 300, 20
+    cache, host = make_cache(nk, rng, seqs, 8, D, 16)
+    for b, S in enumerate(seqs):
+        put(cache, host, side, b, np.array([S - n - window, S - n - window - 3]), size, -3 * size)
+    q = torch.as_tensor(rng.standard_normal((len(seqs), n, 8, D))).to(BF).cuda()
+    check_sampled(nk, cache, host, q, seqs, rng, window)
