@@ -9,7 +9,7 @@
 // values below (nine instructions for eight codes), and the query times a power of two
 // that brings its row's largest magnitude to [2^13, 2^14): fp16 holds a bf16 number
 // exactly down to 2^-29 of the largest. (Two 7-bit digits on the integer cores take 32
-// instructions a round less, 405 us of the 410 below, but a coordinate 2^10 below the
+// instructions a round less, 405 us of the 409 below, but a coordinate 2^10 below the
 // largest keeps 4 bits of them.)
 // Of fp32 queries: on the 8-bit integer cores, exact. A word's codes are two words of
 // bytes (three instructions); the query is a fixed-point number of three digits of
@@ -22,9 +22,9 @@
 // value, and cut those bits off the sum: 1e-5 of an output, towards one side.)
 //
 // With 4 query heads a KV head, bf16 (8 KV heads of 128): 64 sequences of 32K tokens
-// take 410 us, 5.55 TB/s of HBM, which bounds them; one of 128K 38 us (34 from the
-// caches), the reads' 24 us, their ramp and 9 us of merge; one of 2000 tokens 9.7 us,
-// latency. fp32: 5 sequences of up to 5003 tokens, 10 rows a KV head, 19 us, latency and vector issue.
+// take 409 us, 5.6 TB/s of HBM, which bounds them; one of 128K 39 us, the reads'
+// 24 us, their ramp and 9 us of merge; one of 2000 tokens 9.8 us, latency.
+// fp32: 5 sequences of up to 5003 tokens, 10 rows a KV head, 19.7 us, latency and vector issue.
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -407,7 +407,7 @@ int most_splits(const int tile_rows, const long long tiles, const long long span
 // Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the
 // workgroup's waves dividing the tokens; more rows take 32 a wave, 128 or 256 a
 // workgroup (fp32: 16 and 128, which leaves registers for two waves a SIMD: 2 x 2048
-// over 8192 tokens 1462 us, 1756 with 32 a wave; 8 x 16 over 4096 60 us, 93).
+// over 8192 tokens 1504 us, 8 x 16 over 4096 61 us; 32 a wave took 1.2 and 1.5 times as long).
 Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads,
                         const int head_dim, const int q_bf16, const int max_seq_len, const int window) {
   Q4AttnPlan p{};
@@ -419,9 +419,9 @@ Q4AttnPlan plan_q4_attn(const int batch, const int n_q, const int num_q_heads, c
   // over both (8 KV heads of 128, bf16, us): one sequence of 128K tokens 36.2 in
   // 32 splits of 12 waves, 38.6 in 64 of 4 waves, 46.2 in 32 of 4; of 2000 tokens
   // 15.2 in 3 of 12, 10.4 in 16 of 4; 32 x 8192 55.6 whole by 12 waves, 57.2 in 3 of
-  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12; 64 queries over 32K tokens 123 in 16
-  // splits of 128 rows, 154 of 256; 8 x 64 over 2000 tokens 79 in tiles of 128, 98 of
-  // 256; 2 x 2048 over 8192 tokens 559 in tiles of 128, 503 of 256.
+  // 4; 64 x 500 12.8 whole by 4 waves, 19.5 by 12; 64 queries over 32K tokens 137 in 16
+  // splits of 128 rows, 158 of 256; 8 x 64 over 2000 tokens 82 in tiles of 128, 102 of
+  // 256; 2 x 2048 over 8192 tokens 620 in tiles of 128, 525 of 256.
   const double size = head_dim == 128 ? 1.0 : 0.75;
   // token[k - 1]: ns of a CU for a token where k workgroups share it
   auto consider = [&](const int tile_rows, const int waves, const int step, const int setup,

@@ -61,7 +61,7 @@ struct Q4AttnPlan {
 };
 Q4AttnPlan plan_q4_attn(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int q_bf16,
                         int max_seq_len, int window);
-// bf16 queries, tiles of 128 rows (q4_tile.hip); launch_q4_attn calls it.
+// bf16 queries, tiles of 128 or 256 rows (q4_tile.hip); launch_q4_attn calls it.
 hipError_t launch_q4_tile(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream);
 hipError_t launch_q4_attn(const Q4AttnArgs &a, const Q4AttnPlan &plan, hipStream_t stream);
 

@@ -6,12 +6,12 @@
 // keys and values in LDS, in the order in which the matrix cores take them, the
 // next ones while these are used. Unpacked, a score needs no more than its
 // multiply-add into the exponent: 8 vector instructions each, an exponential
-// among them (10 with four waves, which unpack for half the rows), where q4_attn.hip's
-// exact sums over the codes take 14.5 (but no LDS, and no rounding of keys and values).
+// among them (10.5 with four waves, which unpack for half the rows), where sums over
+// the codes, as in q4_attn.hip, took 14.5 (but no LDS, and no rounding of keys and values).
 //
-// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 522 us, 921
+// Two sequences' 2048 queries over 8192 tokens (32 query, 8 KV heads of 128): 525 us, 916
 // TFLOP/s. Vector (about 320 us) and matrix instructions (192 us) bound it, which add
-// on a SIMD. Four waves take 616 us, and the same without the LDS (an earlier step) 1211; with few tiles
+// on a SIMD. Four waves take 620 us, and the same without the LDS took 1211; with few tiles
 // the smaller ones win, by parallelism and by a merge of splits over more workgroups.
 //
 // Keys and values are divided by 2^7 times a power of two at or above the largest

@@ -10,8 +10,8 @@
 //
 // Memory bounds it: 32 x 4096 tokens of 32 query and 8 + 8 KV heads of 128 in bf16 are
 // rotated in 566 us, 3.22 GB read and written at 5.7 TB/s; to a cache (3.37 GB) 716 us, where
-// the vector instructions of the codes take about 580 us beside it. One token: 4.2 us,
-// 64 sequences' to a cache 4.9 us, launch and latency.
+// the vector instructions of the codes take about 580 us beside it. One token: 3.8 to 4.7 us,
+// 64 sequences' to a cache 5.0 us, launch and latency.
 #include <type_traits>
 
 #include "q4_internal.h"
