@@ -549,8 +549,8 @@ size_t nova_kv_q4_attn_workspace_bytes(const nova_kv_q4_cache *cache, int32_t ba
  * probabilities are rounded to fp16 for those sums, with F32 ones they keep 24
  * bits.  With BF16 queries and more than 32 of them per KV head (n_q * Hq / Hkv) keys
  * and values are rounded to fp16, by at most 2^-12 of the power of two above their
- * row's largest magnitude.  Results do not
- * depend on which workgroups finish first.
+ * row's largest magnitude.  Logits are taken to lie within 2^30 in magnitude (beyond,
+ * outputs may be NaN).  Results do not depend on which workgroups finish first.
  * batch == 0 or n_q == 0 is a valid no-op.
  */
 nova_kv_status nova_kv_q4_attn(const nova_kv_q4_cache *cache, const void *q, nova_kv_dtype q_dtype, int32_t batch,

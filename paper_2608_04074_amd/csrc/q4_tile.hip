@@ -60,8 +60,8 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
   __shared__ __align__(16) uint32_t s_pack[kWaves][64];
   // [round mod 3][32 tokens][keys, values]: the largest magnitude, and by how many bits the smallest is below kFinite
   __shared__ __align__(16) float s_mag[3][2 * kParts][2][2];
-  __shared__ __align__(16) float s_unit[2][2][kTokens];  // [round mod 2][keys, values]: a token's power of two (of keys, over its 64 tokens')
-  // [round mod 2]: the part's exponents of keys and values, 128 added, and whether its tokens have their own
+  __shared__ __align__(16) float s_unit[2][2][kTokens];  // [round mod 2][keys, values]: a token's power of two
+  // [round mod 2]: the part's exponents of keys and values, 128 added, or (bit 16) that its tokens have their own
   __shared__ int s_shared[2][kParts];
   __shared__ uint32_t s_valid[3][2 * kParts];
   __shared__ float s_inv[Lds::kRows];
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
     const int shared = lane < 32 ? ek : ev;
     const int e = spread ? min(power_above(odd ? 0 : biased_of(mag), lane < 32 ? kLeastKey : kLeastValue), shared) : shared;
     const float unit = power_of_two(-e);
-    if (part == 0 && lane == 0) s_shared[buffer][own] = (ek + 128) | ((ev + 128) << 8) | (spread ? 1 << 16 : 0);
-    if (part == 0) s_unit[buffer][lane >> 5][32 * group + (lane & 31)] = power_of_two(lane < 32 ? e - ek : e);
+    if (part == 0 && lane == 0) s_shared[buffer][own] = spread ? 128 | (128 << 8) | (1 << 16) : (ek + 128) | ((ev + 128) << 8);
+    if (part == 0) s_unit[buffer][lane >> 5][32 * group + (lane & 31)] = power_of_two(e);
     scale = token_odd ? (lane < 32 ? __builtin_nanf("") : 0.f) : scale * (unit * 0x1p17f);  // s <= 4 / 15 / unit: below 2^15.1
     offset = token_odd ? 0.f : offset * (unit * 0x1p-7f);
     const lut::half2_t both = {static_cast<_Float16>(scale), static_cast<_Float16>(offset)};
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * W, 2) void q4_tile_kernel(const Q4AttnArgs a) 
       const uint32_t valid[2] = {static_cast<uint32_t>(uniform(s_valid[slot0][2 * y])), static_cast<uint32_t>(uniform(s_valid[slot0][2 * y + 1]))};
       const bool inner = (valid[0] & valid[1]) == 0xffffffffu && tb0 >= inner_lo && tb0 + 64 <= inner_hi;
       const float key_unit = power_of_two(ek), value_exp = static_cast<float>(ev);
-      if (spread) {  // in front of the masks: a unit may be 0
+      if (spread) {
         for (int t = 0; t < kRowTiles; ++t)
           for (int x = 0; x < 4; ++x)
             for (int i = 0; i < 4; ++i) s[t][x][i] *= key_units[16 * x + i];

@@ -70,16 +70,29 @@ def test_tokens_of_no_weight_far_above(nk, size, D):  # noqa: F811
         assert (np.abs(got[0, i] - ref) <= tol).all(), i
 
 
-@pytest.mark.parametrize("side", ("k", "v"))
+@pytest.mark.parametrize("side,size", (("k", 1e3), ("k", 1e4), ("v", 1e4), ("v", 1e30)))
 @pytest.mark.parametrize("D", (64, 128))
-@pytest.mark.parametrize("size", (1e4, 1e30))
 def test_hidden_tokens_of_large_tiles(nk, size, D, side):  # noqa: F811
-    """The same in tiles of 256 rows: tokens in front of every window."""
+    """The same in tiles of 256 rows: tokens that only the last queries attend."""
     say(f"hidden {side} {size} D={D}, tiles of 256 rows")
     rng = np.random.default_rng(63)
     seqs, n, window = [641, 650, 700] * 5, 300, 20
     cache, host = make_cache(nk, rng, seqs, 8, D, 16)
     for b, S in enumerate(seqs):
-        put(cache, host, side, b, np.array([S - n - window, S - n - window - 3]), size, -3 * size)
+        put(cache, host, side, b, np.array([S - 3, S - 60]), size, -3 * size)
     q = torch.as_tensor(rng.standard_normal((len(seqs), n, 8, D))).to(BF).cuda()
     check_sampled(nk, cache, host, q, seqs, rng, window)
+
+
+@pytest.mark.parametrize("D", (64, 128))
+def test_hidden_keys_near_the_end_of_fp32(nk, D):  # noqa: F811
+    """Hidden keys of 1e38 beside keys of 1e-5 under queries of 1e5, whose products are ordinary."""
+    rng = np.random.default_rng(64)
+    S, n, window = 200, 40, 20
+    cache, host = make_cache(nk, rng, [S], 2, D, 16, key_size=1e-5)
+    put(cache, host, "k", 0, np.array([S - 1]), 1e36, -1e38)   # only the last query attends it
+    q = torch.as_tensor(1e5 * rng.standard_normal((1, n, 8, D))).to(BF).cuda()
+    out = nk.q4_attn(cache, q, torch.tensor([S], dtype=torch.int32, device="cuda"), S, window=window).double().cpu().numpy()
+    ref, tol = reference_and_bounds(host, q.double().cpu().numpy(), [S], [n], window, None, 1 / math.sqrt(D), True)
+    off = (np.abs(out - ref) - tol)[:, :n - 1]
+    assert (off <= 0).all(), f"{off.max():.3e} over the bound"
