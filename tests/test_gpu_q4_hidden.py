@@ -96,3 +96,16 @@ def test_hidden_keys_near_the_end_of_fp32(nk, D):  # noqa: F811
     ref, tol = reference_and_bounds(host, q.double().cpu().numpy(), [S], [n], window, None, 1 / math.sqrt(D), True)
     off = (np.abs(out - ref) - tol)[:, :n - 1]
     assert (off <= 0).all(), f"{off.max():.3e} over the bound"
+
+
+@pytest.mark.parametrize("seqs,n,Hq,H,D", (([700, 431], 40, 8, 2, 128), ([641, 650, 700] * 5, 300, 8, 8, 64), ([9000], 70, 8, 2, 64)))
+def test_repeatable(nk, seqs, n, Hq, H, D):  # noqa: F811
+    """Tiles of either size, whole and in splits, with and without tokens far above the others: the same every time."""
+    rng = np.random.default_rng(65)
+    cache, host = make_cache(nk, rng, seqs, H, D, 16)
+    put(cache, host, "v", 0, np.arange(0, seqs[0], 150), 1e4, -3e4)
+    q = torch.as_tensor(rng.standard_normal((len(seqs), n, Hq, D))).to(BF).cuda()
+    seq = torch.tensor(seqs, dtype=torch.int32, device="cuda")
+    want = nk.q4_attn(cache, q, seq, max(seqs))
+    for _ in range(20):
+        assert torch.equal(nk.q4_attn(cache, q, seq, max(seqs)), want)
