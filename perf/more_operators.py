@@ -338,8 +338,9 @@ def _handle(s):
             return nk.prepare_q4_read(cache, s["start"], s["k_out"], s["v_out"], lens=s["lens"])
         return nk.prepare_q4_append_axes(rot, axes, cache, s["q"], s["k"], s["v"], s["start"], s["positions"], s["q_out"],
                                          new_lens=s["new_lens"], k_held=s["k_out"], v_held=s["v_out"])
-    params = nk.NovaKVParams(s["kbar"], s["t_k"], s["t_k_inv_t"], s["t_v"], s["cb_k"], None if c["sq"] else s["cb_v"],
-                             key_scale=c["key_scale"], sq_values=c["sq"])
+    dense = [s[name].contiguous() for name in ("t_k", "t_k_inv_t", "t_v")]
+    params = nk.NovaKVParams(s["kbar"], *dense, s["cb_k"], None if c["sq"] else s["cb_v"], key_scale=c["key_scale"],
+                             sq_values=c["sq"])
     more = {"k_scales": s["k_scales"], "v_sq": s["v_sq"],
             "band": nk.Band(*BAND, s["band_k"], s["band_v"]) if c["band"] else None}
     if c["op"] == "read":
