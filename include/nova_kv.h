@@ -32,6 +32,16 @@
  *   nova_kv_q4_attn      attention of one or more query tokens per sequence over
  *                        that 4-bit cache.
  *
+ * and those of prompts that come in chunks, with images in them, and of prefixes:
+ *
+ *   nova_kv_chunk_attn   causal attention of one or more query tokens per sequence
+ *                        over the 2-bit cache.
+ *   nova_kv_rotate_qkv_axes, nova_kv_q4_append_axes
+ *                        the norm and rotation (and 4-bit append) at positions of
+ *                        several axes, such as time, height and width.
+ *   nova_kv_read, nova_kv_q4_read
+ *                        tokens of the 2-bit and of the 4-bit cache as dense rows.
+ *
  * Conventions for every call
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library
  *     never allocates, frees or synchronizes inside these calls.  All work is
@@ -376,6 +386,94 @@ nova_kv_status nova_kv_append_decode_attn_noalloc(const nova_kv_params *p, const
                                                   float *out, void *hip_stream);
 
 /*
+ * Bytes of device workspace nova_kv_chunk_attn needs for this shape, whatever its
+ * window, band and layout. Returns 0 on invalid input, and where none is needed.
+ */
+size_t nova_kv_chunk_attn_workspace_bytes(const nova_kv_params *p, int32_t batch, int32_t n_q, int32_t num_q_heads,
+                                          int32_t max_seq_len);
+
+/*
+ * nova_kv_chunk_attn -- causal attention of n_q query tokens per sequence (drafted
+ * tokens, a chunk of a prompt, a step's single token) over the 2-bit cache, which
+ * holds their keys and values already (nova_kv_encode in front of it).
+ *
+ *   q          [B][n_q][Hq][D] device, dtype q_dtype (F32 or BF16), dense, 16-byte
+ *              aligned; query head h reads KV head h / (Hq / Hkv), any number of them
+ *   q_lens     [B] int32 device, or NULL = n_q for every sequence: rows
+ *              i >= q_lens[b] are padding, and their outputs are left as they were
+ *   k_codes, v_codes, k_scales, v_sq  as in nova_kv_decode_attn, in every format
+ *   band       NULL, or the sink-plus-recent band as the last append left it: with
+ *              S = seq_lens[b], positions [0, n_sink) and [S - n_rec, S) are attended
+ *              with its exact rows by all of the call's queries, so a chunk of up to
+ *              n_rec tokens attends itself exactly. Blocks of the pools that only
+ *              hold such positions are not read.
+ *   seq_lens   [B] int32 device: cached tokens of each sequence, the queries' own
+ *              included; precondition 0 <= seq_lens[b] <= max_seq_len (a longer one
+ *              is taken as max_seq_len, a negative one as 0).  Query i sits at
+ *              position p = seq_lens[b] - q_lens[b] + i and attends the positions
+ *              j <= p, with window W > 0 only those with j > p - W.  Block-table
+ *              entries of attended positions must be physical blocks; others are not
+ *              looked up (with blocks of a multiple of 16 rows: of the attended
+ *              positions' aligned runs of 16).
+ *   max_seq_len, window, sinks, softmax_scale  as in nova_kv_decode_attn
+ *   out        [B][n_q][Hq][D] device, dtype q_dtype, 16-byte aligned, apart from the
+ *              inputs: as in nova_kv_decode_attn, rounded to q_dtype.  A row that
+ *              attends nothing is written as zeros.
+ *   workspace  device scratch of at least nova_kv_chunk_attn_workspace_bytes(...)
+ *              bytes, 256-byte aligned (may be NULL where that is 0); zero-filled
+ *              before its first use, left ready for the next call by every call
+ *              (replays of a captured call included).  Calls that share a workspace
+ *              must be ordered on one stream; one may serve nova_kv_q4_attn too.
+ *
+ * Precision: codewords and levels enter exactly, the band's rows too. With F32 queries
+ * the queries (in the key transform's coordinates) and the probabilities keep 22 bits,
+ * with BF16 ones they are rounded to fp16 (the band's probabilities to 16 bits);
+ * softmax statistics and sums over values in fp32. Logits are taken to lie within 2^30 in magnitude (beyond,
+ * outputs may be NaN), codebooks and transforms to be finite.  Results do not depend
+ * on which workgroups finish first.
+ * batch == 0 or n_q == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout *layout, const void *q,
+                                  nova_kv_dtype q_dtype, int32_t batch, int32_t n_q, int32_t num_q_heads,
+                                  const int32_t *q_lens, const uint8_t *k_codes, const uint8_t *v_codes,
+                                  const uint16_t *k_scales, const uint16_t *v_sq, const nova_kv_band *band,
+                                  const int32_t *seq_lens, int32_t max_seq_len, int32_t window, const float *sinks,
+                                  float softmax_scale, void *out, void *workspace, size_t workspace_bytes,
+                                  void *hip_stream);
+
+/*
+ * nova_kv_read -- n tokens per sequence of the 2-bit cache as dense rows, in the
+ * domain of the keys and values that were appended: a prefix for another engine,
+ * or for attention by other means over what later steps will read.
+ *
+ *   k_hat = rho (r_hat t_k_inv_t^T) + kbar,  v_hat = s_hat t_v^T
+ *
+ *   k_codes, v_codes, k_scales, v_sq  as in nova_kv_decode_attn, in every format; a
+ *              side's pools may be NULL where its output is
+ *   band       NULL, or the band as the last append left it: its positions are read
+ *              from it, exactly.  It needs seq_lens.
+ *   seq_lens   [B] int32 device: cached tokens of each sequence, or NULL without a
+ *              band: the capacity
+ *   start_pos  [B] int32 device: position of the first token of each sequence
+ *   lens       [B] int32 device, or NULL = n for every sequence: rows i >= lens[b]
+ *              are padding, and left as they were; so are those of positions outside
+ *              [0, seq_lens[b]).  Block-table entries of the others (but the band's)
+ *              must be physical blocks.
+ *   k_out, v_out  [B][n][Hkv][D] device, dtype `dtype` (F32 or BF16), 16-byte aligned,
+ *              apart from each other and from the inputs.  Either may be NULL, and is
+ *              then left out.
+ *
+ * Products of exact codewords (levels) with transforms of 22 bits (bf16 ones: exact),
+ * summed in fp32 and rounded to dtype.
+ * batch == 0 or n == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_read(const nova_kv_params *p, const nova_kv_layout *layout, const uint8_t *k_codes,
+                            const uint8_t *v_codes, const uint16_t *k_scales, const uint16_t *v_sq,
+                            const nova_kv_band *band, const int32_t *seq_lens, nova_kv_dtype dtype, int32_t batch,
+                            int32_t n, const int32_t *start_pos, const int32_t *lens, void *k_out, void *v_out,
+                            void *hip_stream);
+
+/*
  * Rows of heads in the caller's memory: head h of token i of sequence b starts at
  *
  *   data + (b * batch_stride + i * token_stride + h * D) * (bytes of an element)
@@ -448,6 +546,37 @@ nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q
                                   void *v_out, void *hip_stream);
 
 /*
+ * Positions of several axes (time, row and column of an image's patches in a
+ * prompt): every rotated pair follows one axis, and is turned by the angle of the
+ * token's position on that axis.
+ *
+ *   num_axes   1 .. NOVA_KV_MAX_AXES
+ *   pair_axis  the axis of pair j (see nova_kv_rotary), j < rotary_dim / 2, below
+ *              num_axes: blocks of neighbouring pairs, every third pair, or any other
+ *              order. Column j of cos_sin holds pair j's angles, so frequencies that
+ *              start again with each axis are a matter of that table alone.
+ */
+#define NOVA_KV_MAX_AXES 4
+
+typedef struct {
+    int32_t num_axes;
+    uint8_t pair_axis[64];
+} nova_kv_axes;
+
+/*
+ * nova_kv_rotate_qkv_axes -- nova_kv_rotate_qkv at positions of several axes.
+ *
+ *   positions  [num_axes][B][n_new] int32 device: of each token on each axis. A token
+ *              with one outside [0, num_positions) is left out like padding.
+ *   all other arguments as in nova_kv_rotate_qkv; rotary_dim must not be 0.
+ */
+nova_kv_status nova_kv_rotate_qkv_axes(const nova_kv_rotary *r, const nova_kv_axes *axes, const nova_kv_rows *q,
+                                       const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype,
+                                       int32_t batch, int32_t n_new, const int32_t *new_lens,
+                                       const int32_t *positions, void *q_out, void *k_out, void *v_out,
+                                       void *hip_stream);
+
+/*
  * A cache held in 4 bits, for layers that need more than 2 bits per element
  * (4.25 at D = 128): every key and value of a token and KV head is a row of D
  * 4-bit codes c_i and stands for offset + scale * c_i.
@@ -509,6 +638,36 @@ nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache
                                  const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch,
                                  int32_t n_new, const int32_t *new_lens, const int32_t *start_pos, void *q_out,
                                  void *k_held, void *v_held, void *hip_stream);
+
+/*
+ * nova_kv_q4_append_axes -- nova_kv_q4_append with rotations at positions of several
+ * axes: start_pos[b] + i is the token's place in the cache only.
+ *
+ *   positions  as in nova_kv_rotate_qkv_axes
+ *   all other arguments as in nova_kv_q4_append; rotary_dim must not be 0.
+ */
+nova_kv_status nova_kv_q4_append_axes(const nova_kv_rotary *r, const nova_kv_axes *axes,
+                                      const nova_kv_q4_cache *cache, const nova_kv_rows *q, const nova_kv_rows *k,
+                                      const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                                      const int32_t *new_lens, const int32_t *start_pos, const int32_t *positions,
+                                      void *q_out, void *k_held, void *v_held, void *hip_stream);
+
+/*
+ * nova_kv_q4_read -- n tokens per sequence of a 4-bit cache as dense rows: what
+ * nova_kv_q4_append gives as k_held and v_held, and nova_kv_q4_attn attends.
+ *
+ *   start_pos  [B] int32 device: position of the first token of each sequence
+ *   lens       [B] int32 device, or NULL = n for every sequence: rows i >= lens[b]
+ *              are padding, and left as they were; so are those of positions outside
+ *              [0, block_size * blocks_per_seq) and in blocks that hold nothing
+ *   k_out, v_out  [B][n][Hkv][D] device, dtype `dtype`, 16-byte aligned, apart from
+ *              each other and from the cache: fp32(scale * c) + offset, rounded to
+ *              dtype. Either may be NULL, and is then left out.
+ * batch == 0 or n == 0 is a valid no-op.
+ */
+nova_kv_status nova_kv_q4_read(const nova_kv_q4_cache *cache, nova_kv_dtype dtype, int32_t batch, int32_t n,
+                               const int32_t *start_pos, const int32_t *lens, void *k_out, void *v_out,
+                               void *hip_stream);
 
 /*
  * Bytes of device workspace nova_kv_q4_attn needs for this shape, whatever its
@@ -589,14 +748,15 @@ nova_kv_status nova_kv_check_metadata(const nova_kv_layout *layout, int32_t num_
  * from the start when the environment variable NOVA_KV_DEBUG is a nonzero
  * number).  When on, nova_kv_encode, nova_kv_decode_attn,
  * nova_kv_append_decode_attn (and its allocation-free variant),
- * nova_kv_q4_append and nova_kv_q4_attn wait for their stream, copy seq_lens /
+ * nova_kv_chunk_attn, nova_kv_read, nova_kv_q4_append (nova_kv_q4_append_axes),
+ * nova_kv_q4_attn and nova_kv_q4_read wait for their stream, copy seq_lens /
  * start_pos / new_lens / the block table to the host and run
  * nova_kv_check_metadata (with num_blocks as given here, <= 0: unknown)
- * before launching; a failing check launches nothing.  This synchronizes,
+ * before launching; a failing check launches nothing.  (The reading calls check
+ * the positions that they read: sequences may share blocks there.)  This synchronizes,
  * so it is for debugging and not for graph capture.
  *
- * nova_kv_q4_append and nova_kv_q4_attn check against their cache's own
- * num_blocks.  A negative block-table entry (a block not held yet, or released in
+ * The 4-bit cache's calls check against its own num_blocks.  A negative block-table entry (a block not held yet, or released in
  * front of a window) passes.  What else these calls would leave out or cut is
  * reported, as a likely mistake: entries from num_blocks on, new tokens outside
  * the capacity (beyond new_lens), lengths outside [0, max_seq_len].

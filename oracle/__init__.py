@@ -24,6 +24,8 @@ Contents (each function cites the passage of the paper it follows):
   accounting   cache byte and parameter counts
   q4           norm and rotation of heads, 4-bit rows and causal attention over
                them (from their formulas; not in the paper)
+  chunk        the 2-bit cache read back, causal attention of several query tokens
+               over it, angles of positions on several axes
 
 Parity status: every function is pinned by tests in ``tests/test_oracle_*.py``.
 Lloyd training is pinned by its invariants (monotone distortion, lossless on
@@ -36,4 +38,4 @@ of M_o and the raw-coordinate order all differ.  The pins of these steps are
 also run against planted mistakes, which they must catch.
 """
 
-from . import accounting, attention, calibration, codec, fp8, grouping, q4, vq  # noqa: F401
+from . import accounting, attention, calibration, chunk, codec, fp8, grouping, q4, vq  # noqa: F401

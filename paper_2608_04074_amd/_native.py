@@ -32,8 +32,14 @@ EXPORTED = (
     "nova_kv_decode_attn",
     "nova_kv_append_decode_attn",
     "nova_kv_append_decode_attn_noalloc",
+    "nova_kv_chunk_attn_workspace_bytes",
+    "nova_kv_chunk_attn",
+    "nova_kv_read",
     "nova_kv_rotate_qkv",
+    "nova_kv_rotate_qkv_axes",
     "nova_kv_q4_append",
+    "nova_kv_q4_append_axes",
+    "nova_kv_q4_read",
     "nova_kv_q4_attn_workspace_bytes",
     "nova_kv_q4_attn",
     "nova_kv_check_metadata",
@@ -101,6 +107,13 @@ class Rotary(ctypes.Structure):
     ]
 
 
+class Axes(ctypes.Structure):
+    _fields_ = [
+        ("num_axes", ctypes.c_int32),
+        ("pair_axis", ctypes.c_uint8 * 64),
+    ]
+
+
 class Q4Cache(ctypes.Structure):
     _fields_ = [
         ("num_kv_heads", ctypes.c_int32),
@@ -115,6 +128,7 @@ class Q4Cache(ctypes.Structure):
 
 
 NOVA_KV_MAX_BAND = 1024
+NOVA_KV_MAX_AXES = 4
 
 
 class NovaKVError(RuntimeError):
@@ -161,6 +175,30 @@ def lib() -> ctypes.CDLL:
         L.nova_kv_append_decode_attn_noalloc.argtypes = [P(Params), P(Layout), vp, vp, ctypes.c_int, vp,
                                                          ctypes.c_int, i32, i32, vp, vp, vp, vp, P(Band), vp,
                                                          i32, i32, vp, ctypes.c_float, vp, vp]
+        L.nova_kv_chunk_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.nova_kv_chunk_attn_workspace_bytes.argtypes = [P(Params), i32, i32, i32, i32]
+        L.nova_kv_chunk_attn.restype = ctypes.c_int
+        # (params, layout, q, q_dtype, batch, n_q, num_q_heads, q_lens, k_codes, v_codes, k_scales, v_sq, band,
+        #  seq_lens, max_seq_len, window, sinks, softmax_scale, out, workspace, bytes, stream)
+        L.nova_kv_chunk_attn.argtypes = [P(Params), P(Layout), vp, ctypes.c_int, i32, i32, i32, vp, vp, vp, vp, vp,
+                                         P(Band), vp, i32, i32, vp, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+        L.nova_kv_read.restype = ctypes.c_int
+        # (params, layout, k_codes, v_codes, k_scales, v_sq, band, seq_lens, dtype, batch, n, start_pos, lens,
+        #  k_out, v_out, stream)
+        L.nova_kv_read.argtypes = [P(Params), P(Layout), vp, vp, vp, vp, P(Band), vp, ctypes.c_int, i32, i32, vp, vp,
+                                   vp, vp, vp]
+        L.nova_kv_rotate_qkv_axes.restype = ctypes.c_int
+        # (rotary, axes, q, k, v, dtype, batch, n_new, new_lens, positions, q_out, k_out, v_out, stream)
+        L.nova_kv_rotate_qkv_axes.argtypes = [P(Rotary), P(Axes), P(Rows), P(Rows), P(Rows), ctypes.c_int, i32, i32,
+                                              vp, vp, vp, vp, vp, vp]
+        L.nova_kv_q4_append_axes.restype = ctypes.c_int
+        # (rotary, axes, cache, q, k, v, dtype, batch, n_new, new_lens, start_pos, positions, q_out, k_held,
+        #  v_held, stream)
+        L.nova_kv_q4_append_axes.argtypes = [P(Rotary), P(Axes), P(Q4Cache), P(Rows), P(Rows), P(Rows), ctypes.c_int,
+                                             i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.nova_kv_q4_read.restype = ctypes.c_int
+        # (cache, dtype, batch, n, start_pos, lens, k_out, v_out, stream)
+        L.nova_kv_q4_read.argtypes = [P(Q4Cache), ctypes.c_int, i32, i32, vp, vp, vp, vp, vp]
         L.nova_kv_rotate_qkv.restype = ctypes.c_int
         # (rotary, q, k, v, dtype, batch, n_new, new_lens, start_pos, q_out, k_out, v_out, stream)
         L.nova_kv_rotate_qkv.argtypes = [P(Rotary), P(Rows), P(Rows), P(Rows), ctypes.c_int, i32, i32, vp, vp, vp,

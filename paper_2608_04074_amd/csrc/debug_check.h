@@ -16,4 +16,9 @@ nova_kv_status debug_check(const nova_kv_layout *lay, int32_t batch, const int32
                            const int32_t *start_pos, int32_t n_new, hipStream_t stream,
                            const int32_t *new_lens = nullptr, int32_t num_blocks = 0);
 
+// The same for a call that reads tokens from start_pos[b] on (check_reads).
+nova_kv_status debug_check_reads(const nova_kv_layout *lay, int32_t batch, const int32_t *start_pos, int32_t n,
+                                 const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
+                                 hipStream_t stream, int32_t num_blocks = 0);
+
 }  // namespace novakv

@@ -198,6 +198,35 @@ nova_kv_status check_overlaps(const nova_kv_rotary *r, const nova_kv_rows *q, co
   return NOVA_KV_OK;
 }
 
+nova_kv_status check_axes(const nova_kv_axes *axes, const nova_kv_rotary *r, const int32_t *positions) {
+  if (!axes) return fail(NOVA_KV_ERR_INVALID_ARG, "axes is NULL");
+  if (axes->num_axes < 1 || axes->num_axes > NOVA_KV_MAX_AXES)
+    return fail(NOVA_KV_ERR_INVALID_ARG, "%d axes (1 .. %d)", axes->num_axes, NOVA_KV_MAX_AXES);
+  if (r->rotary_dim == 0) return fail(NOVA_KV_ERR_INVALID_ARG, "positions of several axes need a rotation");
+  for (int j = 0; j < r->rotary_dim / 2; ++j)
+    if (axes->pair_axis[j] >= axes->num_axes)
+      return fail(NOVA_KV_ERR_INVALID_ARG, "pair %d follows axis %d of %d", j, axes->pair_axis[j], axes->num_axes);
+  if (!positions) return fail(NOVA_KV_ERR_INVALID_ARG, "positions is NULL");
+  return NOVA_KV_OK;
+}
+
+nova_kv_status check_read_outputs(nova_kv_dtype dtype, int32_t batch, int32_t n, int32_t heads, int32_t head_dim,
+                                  const void *k_out, const void *v_out) {
+  if (dtype != NOVA_KV_F32 && dtype != NOVA_KV_BF16)
+    return fail(NOVA_KV_ERR_INVALID_ARG, "dtype must be NOVA_KV_F32 or NOVA_KV_BF16");
+  if (batch < 0 || n < 0) return fail(NOVA_KV_ERR_INVALID_ARG, "batch and n must be >= 0");
+  if (batch > 65535) return fail(NOVA_KV_ERR_INVALID_ARG, "batch > 65535");
+  if (batch == 0 || n == 0) return NOVA_KV_OK;
+  // a launch's threads: 512 for 64 tokens of a head and side
+  if ((static_cast<long long>(n) + 63) / 64 * batch > (1LL << 21) / heads)
+    return fail(NOVA_KV_ERR_UNSUPPORTED, "too many tokens in a call");
+  if (!aligned(k_out, 16) || !aligned(v_out, 16)) return fail(NOVA_KV_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  const unsigned long long bytes = static_cast<unsigned long long>(batch) * n * heads * head_dim * (dtype == NOVA_KV_BF16 ? 2 : 4);
+  const unsigned long long k = reinterpret_cast<uintptr_t>(k_out), v = reinterpret_cast<uintptr_t>(v_out);
+  if (k_out && v_out && (k < v ? v - k : k - v) < bytes) return fail(NOVA_KV_ERR_INVALID_ARG, "k_out and v_out overlap");
+  return NOVA_KV_OK;
+}
+
 nova_kv_status check_q4_cache(const nova_kv_q4_cache *c) {
   if (!c) return fail(NOVA_KV_ERR_INVALID_ARG, "cache is NULL");
   if (c->num_kv_heads <= 0) return fail(NOVA_KV_ERR_INVALID_ARG, "num_kv_heads must be > 0");
@@ -305,6 +334,30 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
     }
   }
   return ok();
+}
+
+nova_kv_status check_reads(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch, const int32_t *start_pos,
+                           int32_t n, const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
+                           bool may_be_absent) {
+  const long long cap = capacity_of(lay);
+  for (int b = 0; b < batch; ++b) {
+    if (seq_lens && (seq_lens[b] < 0 || seq_lens[b] > cap))
+      return fail(NOVA_KV_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [0, %lld]", b, seq_lens[b], cap);
+    const long long size = seq_lens ? seq_lens[b] : cap, from = start_pos[b];
+    const long long to = from + (!lens ? n : lens[b] < 0 ? 0 : lens[b] < n ? lens[b] : n);
+    if (from < to && (from < 0 || to > size))
+      return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d: positions [%lld, %lld) are read of [0, %lld)", b, from, to, size);
+    for (long long t = from; t < to; ++t) {
+      if (band && (t < band->n_sink || t >= size - band->n_rec)) continue;
+      const long long blk = t / lay->block_size, logical = static_cast<long long>(b) * lay->blocks_per_seq + blk;
+      const long long p = lay->block_table ? lay->block_table[logical] : logical;
+      if (may_be_absent && p < 0) continue;
+      if (p < 0 || (num_blocks > 0 && p >= num_blocks))
+        return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d: block %lld maps to physical block %lld outside [0, %d)", b, blk,
+                    p, num_blocks > 0 ? num_blocks : 0x7fffffff);
+    }
+  }
+  return NOVA_KV_OK;
 }
 
 namespace {

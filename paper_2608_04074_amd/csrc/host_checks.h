@@ -49,6 +49,8 @@ nova_kv_status check_rows(const char *name, const nova_kv_rows *rows, const void
 nova_kv_status check_overlaps(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
                               const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
                               const void *q_out, const void *k_out, const void *v_out);
+// Positions of several axes, for the rotation r.
+nova_kv_status check_axes(const nova_kv_axes *axes, const nova_kv_rotary *r, const int32_t *positions);
 // A 4-bit cache.
 nova_kv_status check_q4_cache(const nova_kv_q4_cache *c);
 
@@ -59,6 +61,16 @@ nova_kv_status check_q4_cache(const nova_kv_q4_cache *c);
 nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch,
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
                               int32_t n_new, const int32_t *new_lens = nullptr, bool may_be_absent = false);
+
+// Dense rows [batch][n][heads][head_dim] that a cache is read to: either may be NULL.
+nova_kv_status check_read_outputs(nova_kv_dtype dtype, int32_t batch, int32_t n, int32_t heads, int32_t head_dim,
+                                  const void *k_out, const void *v_out);
+// The tokens that such a call reads, on host copies: the first lens[b] (NULL: n) from
+// start_pos[b] on, which must lie in [0, seq_lens[b]) (NULL: the capacity) and, but for a
+// band's positions, in blocks of the pool.
+nova_kv_status check_reads(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch, const int32_t *start_pos,
+                           int32_t n, const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
+                           bool may_be_absent);
 
 // Debug mode (nova_kv_set_debug; initially on when the environment variable
 // NOVA_KV_DEBUG is a nonzero number): entry points copy their metadata to

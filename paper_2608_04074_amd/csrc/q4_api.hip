@@ -1,4 +1,4 @@
-// C ABI of the norm and rotation of heads and of the cache held in 4 bits:
+// C ABI of the norm and rotation of heads (positions of one axis or of several) and of the cache held in 4 bits:
 // host-side validation, workspace planning and dispatch.  Every check runs
 // before any HIP call, so an invalid call launches nothing.
 #include <math.h>
@@ -6,9 +6,9 @@
 #include <exception>
 
 #include "../../include/nova_kv.h"
+#include "chunk_internal.h"
 #include "debug_check.h"
 #include "host_checks.h"
-#include "q4_internal.h"
 
 using namespace novakv::host;
 
@@ -73,14 +73,17 @@ novakv::RotateArgs rotate_args(const nova_kv_rotary *r, const nova_kv_rows *q, c
   return a;
 }
 
-}  // namespace
+void set_axes(novakv::RotateArgs &a, const nova_kv_axes *axes, const int32_t *positions) {
+  a.num_axes = axes->num_axes;
+  a.positions = positions;
+  for (int j = 0; j < a.rotary_dim / 2; ++j) a.pair_axis[j / 32] |= static_cast<uint64_t>(axes->pair_axis[j]) << (2 * (j % 32));
+}
 
-extern "C" {
-
-nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
-                                  const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
-                                  const int32_t *new_lens, const int32_t *start_pos, void *q_out, void *k_out,
-                                  void *v_out, void *hip_stream) {
+// nova_kv_rotate_qkv, or with axes nova_kv_rotate_qkv_axes.
+nova_kv_status rotate_call(const nova_kv_rotary *r, bool with_axes, const nova_kv_axes *axes, const nova_kv_rows *q,
+                           const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                           const int32_t *new_lens, const int32_t *start_pos, const int32_t *positions, void *q_out,
+                           void *k_out, void *v_out, void *hip_stream) {
   nova_kv_status st = check_rotary(r, q != nullptr, k != nullptr);
   if (st != NOVA_KV_OK) return st;
   if ((st = check_tokens(r, dtype, batch, n_new)) != NOVA_KV_OK) return st;
@@ -90,8 +93,13 @@ nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q
   if ((st = check_rows("v", v, v_out, dtype, true)) != NOVA_KV_OK) return st;
   if (!q && !k && !v) return ok();
   if ((st = check_overlaps(r, q, k, v, dtype, batch, n_new, q_out, k_out, v_out)) != NOVA_KV_OK) return st;
-  if (r->rotary_dim && !start_pos) return fail(NOVA_KV_ERR_INVALID_ARG, "start_pos is NULL");
+  if (with_axes) {
+    if ((st = check_axes(axes, r, positions)) != NOVA_KV_OK) return st;
+  } else if (r->rotary_dim && !start_pos) {
+    return fail(NOVA_KV_ERR_INVALID_ARG, "start_pos is NULL");
+  }
   novakv::RotateArgs a = rotate_args(r, q, k, v, dtype, batch, n_new, new_lens, start_pos);
+  if (with_axes) set_axes(a, axes, positions);
   a.q_out = q_out;
   a.k_out = k_out;
   a.v_out = v_out;
@@ -100,10 +108,11 @@ nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q
   return ok();
 }
 
-nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache *cache, const nova_kv_rows *q,
-                                 const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch,
-                                 int32_t n_new, const int32_t *new_lens, const int32_t *start_pos, void *q_out,
-                                 void *k_held, void *v_held, void *hip_stream) {
+// nova_kv_q4_append, or with axes nova_kv_q4_append_axes.
+nova_kv_status append_call(const nova_kv_rotary *r, bool with_axes, const nova_kv_axes *axes, const nova_kv_q4_cache *cache,
+                           const nova_kv_rows *q, const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype,
+                           int32_t batch, int32_t n_new, const int32_t *new_lens, const int32_t *start_pos,
+                           const int32_t *positions, void *q_out, void *k_held, void *v_held, void *hip_stream) {
   return guarded([&]() -> nova_kv_status {
     nova_kv_status st = check_rotary(r, q != nullptr, true);
     if (st != NOVA_KV_OK) return st;
@@ -119,11 +128,13 @@ nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache
     if ((st = check_rows("v", v, v_held, dtype, false)) != NOVA_KV_OK) return st;
     if ((st = check_overlaps(r, q, k, v, dtype, batch, n_new, q_out, k_held, v_held)) != NOVA_KV_OK) return st;
     if (!start_pos) return fail(NOVA_KV_ERR_INVALID_ARG, "start_pos is NULL");
+    if (with_axes && (st = check_axes(axes, r, positions)) != NOVA_KV_OK) return st;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if ((st = novakv::debug_check(&cache->layout, batch, nullptr, 0, start_pos, n_new, stream, new_lens,
                                   cache->num_blocks)) != NOVA_KV_OK)
       return st;
     novakv::RotateArgs a = rotate_args(r, q, k, v, dtype, batch, n_new, new_lens, start_pos);
+    if (with_axes) set_axes(a, axes, positions);
     a.q_out = q_out;
     a.k_out = k_held;
     a.v_out = v_held;
@@ -136,6 +147,79 @@ nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache
     a.v_sq = cache->v_sq;
     const hipError_t e = novakv::launch_rotate(a, stream);
     if (e != hipSuccess) return fail(NOVA_KV_ERR_HIP, "4-bit append launch: %s", hipGetErrorString(e));
+    return ok();
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+nova_kv_status nova_kv_rotate_qkv(const nova_kv_rotary *r, const nova_kv_rows *q, const nova_kv_rows *k,
+                                  const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                                  const int32_t *new_lens, const int32_t *start_pos, void *q_out, void *k_out,
+                                  void *v_out, void *hip_stream) {
+  return rotate_call(r, false, nullptr, q, k, v, dtype, batch, n_new, new_lens, start_pos, nullptr, q_out, k_out, v_out,
+                     hip_stream);
+}
+
+nova_kv_status nova_kv_rotate_qkv_axes(const nova_kv_rotary *r, const nova_kv_axes *axes, const nova_kv_rows *q,
+                                       const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype,
+                                       int32_t batch, int32_t n_new, const int32_t *new_lens,
+                                       const int32_t *positions, void *q_out, void *k_out, void *v_out,
+                                       void *hip_stream) {
+  return rotate_call(r, true, axes, q, k, v, dtype, batch, n_new, new_lens, nullptr, positions, q_out, k_out, v_out,
+                     hip_stream);
+}
+
+nova_kv_status nova_kv_q4_append(const nova_kv_rotary *r, const nova_kv_q4_cache *cache, const nova_kv_rows *q,
+                                 const nova_kv_rows *k, const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch,
+                                 int32_t n_new, const int32_t *new_lens, const int32_t *start_pos, void *q_out,
+                                 void *k_held, void *v_held, void *hip_stream) {
+  return append_call(r, false, nullptr, cache, q, k, v, dtype, batch, n_new, new_lens, start_pos, nullptr, q_out, k_held,
+                     v_held, hip_stream);
+}
+
+nova_kv_status nova_kv_q4_append_axes(const nova_kv_rotary *r, const nova_kv_axes *axes,
+                                      const nova_kv_q4_cache *cache, const nova_kv_rows *q, const nova_kv_rows *k,
+                                      const nova_kv_rows *v, nova_kv_dtype dtype, int32_t batch, int32_t n_new,
+                                      const int32_t *new_lens, const int32_t *start_pos, const int32_t *positions,
+                                      void *q_out, void *k_held, void *v_held, void *hip_stream) {
+  return append_call(r, true, axes, cache, q, k, v, dtype, batch, n_new, new_lens, start_pos, positions, q_out, k_held,
+                     v_held, hip_stream);
+}
+
+nova_kv_status nova_kv_q4_read(const nova_kv_q4_cache *cache, nova_kv_dtype dtype, int32_t batch, int32_t n,
+                               const int32_t *start_pos, const int32_t *lens, void *k_out, void *v_out,
+                               void *hip_stream) {
+  return guarded([&]() -> nova_kv_status {
+    nova_kv_status st = check_q4_cache(cache);
+    if (st != NOVA_KV_OK) return st;
+    if ((st = check_read_outputs(dtype, batch, n, cache->num_kv_heads, cache->head_dim, k_out, v_out)) != NOVA_KV_OK) return st;
+    if (batch == 0 || n == 0 || (!k_out && !v_out)) return ok();
+    if (!start_pos) return fail(NOVA_KV_ERR_INVALID_ARG, "start_pos is NULL");
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if ((st = novakv::debug_check_reads(&cache->layout, batch, start_pos, n, lens, nullptr, nullptr, stream,
+                                        cache->num_blocks)) != NOVA_KV_OK)
+      return st;
+    novakv::ReadArgs a{};
+    a.batch = batch;
+    a.n = n;
+    a.num_kv_heads = cache->num_kv_heads;
+    a.head_dim = cache->head_dim;
+    a.layout = novakv::CacheLayout{cache->layout.block_size, cache->layout.blocks_per_seq, cache->layout.block_table};
+    a.lens = lens;
+    a.start_pos = start_pos;
+    a.k_out = k_out;
+    a.v_out = v_out;
+    a.bf16 = dtype == NOVA_KV_BF16;
+    a.k_codes = cache->k_codes;
+    a.v_codes = cache->v_codes;
+    a.num_blocks = cache->num_blocks;
+    a.k_sq = cache->k_sq;
+    a.v_sq = cache->v_sq;
+    const hipError_t e = novakv::launch_q4_read(a, stream);
+    if (e != hipSuccess) return fail(NOVA_KV_ERR_HIP, "4-bit read launch: %s", hipGetErrorString(e));
     return ok();
   });
 }

@@ -136,81 +136,42 @@ struct FinishLds {
   int *last;
 };
 
-// Writes a tile's outputs from its waves' partials: out = acc / sum of a row's
-// weights exp2(z - ref). The waves share the rows, or (TILED) have 16 NT each.
-template <int D, int NT, int W, bool TILED>
-__device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, const FinishLds<D, NT, W, TILED> &lds,
-                                            const int wave, const int lane, const float4_t (&acc)[NT][D / 16],
-                                            const float (&ref)[NT], const float (&sum)[NT]) {
-  using Lds = FinishLds<D, NT, W, TILED>;
-  constexpr int kThreads = 64 * W, kWaves = W, kTiles = D / 16, kRows = Lds::kRows, kStride = Lds::kStride;
-  const int n = lane & 15, j = lane >> 4;
-  const int b = g.b, kv = g.kv, wg_row0 = g.row0, wg_row1 = g.row1, split = g.split;
-  const int row0 = g.row0 + (TILED ? wave * 16 * NT : 0);
-  float *const s_merge = lds.merge, *const s_inv = lds.inv;
-  auto s_ref = lds.ref, s_sum = lds.sum;
-  int &s_last = *lds.last;
-  const int rows_here = wg_row1 - wg_row0;
-  const size_t slot = static_cast<size_t>(kRows) * (D + 2);
-  float *part = nullptr;
-  if (a.n_split > 1) part = a.part + ((static_cast<size_t>(g.unit) * a.row_tiles + g.tile) * a.n_split + split) * slot;
-  auto head_of = [&](const int r) { return kv * a.gqa + (wg_row0 + r) % a.gqa; };
-  auto out_at = [&](const int r) {
-    return ((static_cast<size_t>(b) * a.n_q + (wg_row0 + r) / a.gqa) * a.num_q_heads + head_of(r)) * D;
-  };
+// Where a tile's rows and partials lie, and what makes outputs of them.
+template <int D, int kRows>
+struct TileRows {
+  const Q4AttnArgs &a;
+  const Tile &g;
+  static constexpr size_t kSlot = static_cast<size_t>(kRows) * (D + 2);  // floats of a split's partials
+  __device__ __forceinline__ int rows_here() const { return g.row1 - g.row0; }
+  __device__ __forceinline__ int head_of(const int r) const { return g.kv * a.gqa + (g.row0 + r) % a.gqa; }
+  __device__ __forceinline__ size_t out_at(const int r) const {
+    return ((static_cast<size_t>(g.b) * a.n_q + (g.row0 + r) / a.gqa) * a.num_q_heads + head_of(r)) * D;
+  }
+  // the split's own partials (nullptr: the tile has one split)
+  __device__ __forceinline__ float *part() const {
+    return a.n_split > 1 ? a.part + ((static_cast<size_t>(g.unit) * a.row_tiles + g.tile) * a.n_split + g.split) * kSlot : nullptr;
+  }
   // 1 / the sum of a row's weights with its sink; 0 where nothing is attended
-  auto inverse = [&](const int r, const float most, float l) {
+  __device__ __forceinline__ float inverse(const int r, const float most, float l) const {
     if (a.sinks && most != kNone) l += exp2_raw(a.sinks[head_of(r)] * 1.44269504088896341f - most);
     return most == kNone ? 0.f : 1.f / l;
-  };
-  auto scaled = [](const float4 v, const float f) { return make_float4(v.x * f, v.y * f, v.z * f, v.w * f); };
-  // a lane's values in chunks of four coordinates
-  auto chunk = [&](const int t, const int x) {
-    const int o = 4 * (x / 4), i = x % 4;
-    return make_float4(acc[t][o][i], acc[t][o + 1][i], acc[t][o + 2][i], acc[t][o + 3][i]);
-  };
-  auto chunk_coord = [&](const int x) { return out_coord<D>(4 * (x / 4), x % 4, j); };
-  if constexpr (!TILED) {  // over the waves, which hold the same rows
-    for (int t = 0; t < NT; ++t) {
-      float *row = s_merge + (wave * 16 * NT + 16 * t + n) * kStride;
-      for (int x = 0; x < kTiles; ++x) *reinterpret_cast<float4 *>(row + chunk_coord(x)) = chunk(t, x);
-      if (j == 0) s_ref[wave][16 * t + n] = ref[t], s_sum[wave][16 * t + n] = sum[t];
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < rows_here * (D / 4); x += kThreads) {
-      const int r = x / (D / 4), c = 4 * (x % (D / 4));
-      float most = kNone, l = 0.f;
-      for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][r]);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int u = 0; u < kWaves; ++u) {
-        if (s_ref[u][r] == kNone) continue;
-        const float f = half_factor(s_ref[u][r] - most);
-        const float4 y = *reinterpret_cast<const float4 *>(s_merge + (u * 16 * NT + r) * kStride + c);
-        l += f * s_sum[u][r] * f;
-        v.x += f * y.x * f, v.y += f * y.y * f, v.z += f * y.z * f, v.w += f * y.w * f;
-      }
-      if (part) {
-        publish4(part + r * D + c, v);
-        if (c == 0) publish2(part + kRows * D + 2 * r, most, l);
-      } else {
-        store_out(a, out_at(r) + c, scaled(v, inverse(r, most, l)));
-      }
-    }
-  } else {
-    for (int t = 0; t < NT; ++t) {
-      const int r = row0 + 16 * t + n - wg_row0;
-      if (r >= rows_here) continue;
-      const float f = part ? 1.f : inverse(r, ref[t], sum[t]);
-      for (int x = 0; x < kTiles; ++x) {
-        if (part) publish4(part + r * D + chunk_coord(x), chunk(t, x));
-        else store_out(a, out_at(r) + chunk_coord(x), scaled(chunk(t, x), f));
-      }
-      if (part && j == 0) publish2(part + kRows * D + 2 * r, ref[t], sum[t]);
-    }
   }
-  if (!part) return;
+  static __device__ __forceinline__ float4 scaled(const float4 v, const float f) { return make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
+};
 
-  // Over the splits: the last one to arrive merges them, in their order.
+// Over the splits, once a workgroup has published its partials: the last one to arrive
+// merges them, in their order. n: the thread's lane modulo 16.
+template <int D, int NT, int W, bool TILED>
+__device__ __forceinline__ void merge_splits(const Q4AttnArgs &a, const Tile &g, const FinishLds<D, NT, W, TILED> &lds, const int n) {
+  constexpr int kThreads = 64 * W, kRows = FinishLds<D, NT, W, TILED>::kRows;
+  const TileRows<D, kRows> place{a, g};
+  const int rows_here = place.rows_here();
+  const size_t slot = place.kSlot;
+  float *const s_merge = lds.merge, *const s_inv = lds.inv;
+  int &s_last = *lds.last;
+  auto out_at = [&](const int r) { return place.out_at(r); };
+  auto inverse = [&](const int r, const float most, const float l) { return place.inverse(r, most, l); };
+  auto scaled = [&](const float4 v, const float f) { return place.scaled(v, f); };
   __builtin_amdgcn_s_waitcnt(0);  // this thread's words have landed
   __syncthreads();
   int *counter = a.counters + static_cast<size_t>(g.unit) * a.row_tiles + g.tile;
@@ -219,7 +180,7 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
   __syncthreads();
   if (!s_last) return;
   if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const float *parts = part - split * slot;
+  const float *parts = place.part() - g.split * slot;
   float2 *weight = reinterpret_cast<float2 *>(s_merge);
   // All words are requested before any is used: the statistics, and each
   // thread's first values (in groups that share the splits where there are fewer
@@ -296,6 +257,72 @@ __device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, 
       store_out(a, out_at(r) + c, scaled(o, s_inv[r]));
     }
   }
+}
+
+// Writes a tile's outputs from its waves' partials: out = acc / sum of a row's
+// weights exp2(z - ref). The waves share the rows, or (TILED) have 16 NT each.
+template <int D, int NT, int W, bool TILED>
+__device__ __forceinline__ void finish_rows(const Q4AttnArgs &a, const Tile &g, const FinishLds<D, NT, W, TILED> &lds,
+                                            const int wave, const int lane, const float4_t (&acc)[NT][D / 16],
+                                            const float (&ref)[NT], const float (&sum)[NT]) {
+  using Lds = FinishLds<D, NT, W, TILED>;
+  constexpr int kThreads = 64 * W, kWaves = W, kTiles = D / 16, kRows = Lds::kRows, kStride = Lds::kStride;
+  const int n = lane & 15, j = lane >> 4;
+  const int wg_row0 = g.row0;
+  const int row0 = g.row0 + (TILED ? wave * 16 * NT : 0);
+  float *const s_merge = lds.merge;
+  auto s_ref = lds.ref, s_sum = lds.sum;
+  const TileRows<D, kRows> place{a, g};
+  const int rows_here = place.rows_here();
+  float *const part = place.part();
+  auto out_at = [&](const int r) { return place.out_at(r); };
+  auto inverse = [&](const int r, const float most, const float l) { return place.inverse(r, most, l); };
+  auto scaled = [&](const float4 v, const float f) { return place.scaled(v, f); };
+  // a lane's values in chunks of four coordinates
+  auto chunk = [&](const int t, const int x) {
+    const int o = 4 * (x / 4), i = x % 4;
+    return make_float4(acc[t][o][i], acc[t][o + 1][i], acc[t][o + 2][i], acc[t][o + 3][i]);
+  };
+  auto chunk_coord = [&](const int x) { return out_coord<D>(4 * (x / 4), x % 4, j); };
+  if constexpr (!TILED) {  // over the waves, which hold the same rows
+    for (int t = 0; t < NT; ++t) {
+      float *row = s_merge + (wave * 16 * NT + 16 * t + n) * kStride;
+      for (int x = 0; x < kTiles; ++x) *reinterpret_cast<float4 *>(row + chunk_coord(x)) = chunk(t, x);
+      if (j == 0) s_ref[wave][16 * t + n] = ref[t], s_sum[wave][16 * t + n] = sum[t];
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < rows_here * (D / 4); x += kThreads) {
+      const int r = x / (D / 4), c = 4 * (x % (D / 4));
+      float most = kNone, l = 0.f;
+      for (int u = 0; u < kWaves; ++u) most = fmaxf(most, s_ref[u][r]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int u = 0; u < kWaves; ++u) {
+        if (s_ref[u][r] == kNone) continue;
+        const float f = half_factor(s_ref[u][r] - most);
+        const float4 y = *reinterpret_cast<const float4 *>(s_merge + (u * 16 * NT + r) * kStride + c);
+        l += f * s_sum[u][r] * f;
+        v.x += f * y.x * f, v.y += f * y.y * f, v.z += f * y.z * f, v.w += f * y.w * f;
+      }
+      if (part) {
+        publish4(part + r * D + c, v);
+        if (c == 0) publish2(part + kRows * D + 2 * r, most, l);
+      } else {
+        store_out(a, out_at(r) + c, scaled(v, inverse(r, most, l)));
+      }
+    }
+  } else {
+    for (int t = 0; t < NT; ++t) {
+      const int r = row0 + 16 * t + n - wg_row0;
+      if (r >= rows_here) continue;
+      const float f = part ? 1.f : inverse(r, ref[t], sum[t]);
+      for (int x = 0; x < kTiles; ++x) {
+        if (part) publish4(part + r * D + chunk_coord(x), chunk(t, x));
+        else store_out(a, out_at(r) + chunk_coord(x), scaled(chunk(t, x), f));
+      }
+      if (part && j == 0) publish2(part + kRows * D + 2 * r, ref[t], sum[t]);
+    }
+  }
+  if (part) merge_splits<D, NT, W, TILED>(a, g, lds, n);
 }
 
 }  // namespace q4

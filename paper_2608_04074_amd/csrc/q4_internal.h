@@ -20,6 +20,11 @@ struct RotateArgs {
   const int32_t *new_lens, *start_pos;
   const float *cos_sin;  // [num_positions][rotary_dim], or nullptr when rotary_dim == 0
   int rotary_dim, interleaved, num_positions;
+  // Positions of several axes (0: a token's own position turns all pairs): [axis][B][n_new],
+  // and the axis of pair j in bits 2 (j % 32) of word j / 32.
+  int num_axes;
+  const int32_t *positions;
+  uint64_t pair_axis[2];
   const float *q_norm, *k_norm;  // weights, or nullptr
   int q_norm_stride, k_norm_stride;  // elements from one head's weights to the next one's: 0 or head_dim
   float eps;
@@ -32,6 +37,7 @@ struct RotateArgs {
   uint16_t *k_sq, *v_sq;
 };
 hipError_t launch_rotate(const RotateArgs &a, hipStream_t stream);
+hipError_t launch_rotate_axes(const RotateArgs &a, hipStream_t stream);  // num_axes > 0; launch_rotate calls it
 
 struct Q4AttnArgs {
   int batch, n_q, num_q_heads, num_kv_heads, head_dim, gqa;

@@ -1,4 +1,5 @@
-"""Python binding of the norm and rotation of heads and of the cache held in 4 bits.
+"""Python binding of the norm and rotation of heads (at positions of one axis or of several)
+and of the cache held in 4 bits.
 
 As in api.py, every step runs in the HIP kernels of libnovakv.so; this module
 checks dtypes, shapes and devices and hands over raw device pointers and the
@@ -8,15 +9,16 @@ stream.  The calls run on the device of their tensors, whichever is current.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
 from . import _native as nat
 from .api import CacheLayout, PreparedCall, _dtype_code, _require
 
-__all__ = ["Rotary", "Q4Cache", "q4_code_shape", "q4_sq_shape", "rotate_qkv", "q4_append", "q4_attn",
-           "q4_attn_workspace_bytes", "prepare_rotate_qkv", "prepare_q4_append", "prepare_q4_attn"]
+__all__ = ["Rotary", "RotaryAxes", "Q4Cache", "q4_code_shape", "q4_sq_shape", "rotate_qkv", "rotate_qkv_axes", "q4_append",
+           "q4_append_axes", "q4_attn", "q4_attn_workspace_bytes", "q4_read", "prepare_rotate_qkv", "prepare_rotate_qkv_axes",
+           "prepare_q4_append", "prepare_q4_append_axes", "prepare_q4_attn", "prepare_q4_read"]
 
 _DTYPES = (torch.float32, torch.bfloat16)
 _SQ_DTYPES = (torch.bfloat16, torch.int16, torch.uint16)
@@ -97,6 +99,43 @@ class Rotary:
     @property
     def tensors(self):
         return (self.cos_sin, self.q_norm, self.k_norm)
+
+
+class RotaryAxes:
+    """Which axis (time, row, column) each rotated pair follows (see nova_kv_axes):
+    ``pair_axis[j]`` for pair j < rotary_dim / 2, any order.  ``blocks`` and ``cycle`` make the
+    usual ones from the number of pairs of each axis."""
+
+    def __init__(self, pair_axis: Sequence[int], num_axes: Optional[int] = None):
+        self.pair_axis = tuple(int(a) for a in pair_axis)
+        if not 1 <= len(self.pair_axis) <= 64:
+            raise ValueError(f"{len(self.pair_axis)} pairs (1 .. 64)")
+        self.num_axes = max(self.pair_axis) + 1 if num_axes is None else int(num_axes)
+        if not 1 <= self.num_axes <= nat.NOVA_KV_MAX_AXES:
+            raise ValueError(f"{self.num_axes} axes (1 .. {nat.NOVA_KV_MAX_AXES})")
+        if min(self.pair_axis) < 0 or max(self.pair_axis) >= self.num_axes:
+            raise ValueError(f"a pair follows none of {self.num_axes} axes")
+        self._c = nat.Axes(self.num_axes, (ctypes.c_uint8 * 64)(*self.pair_axis))
+
+    @classmethod
+    def blocks(cls, lengths: Sequence[int]) -> "RotaryAxes":
+        """The first lengths[0] pairs follow axis 0, the next lengths[1] axis 1, ..."""
+        return cls([a for a, m in enumerate(lengths) for _ in range(m)], len(lengths))
+
+    @classmethod
+    def cycle(cls, lengths: Sequence[int]) -> "RotaryAxes":
+        """Pairs dealt in turn to the axes that have some of their lengths[a] left."""
+        left, order = list(lengths), []
+        while any(m > 0 for m in left):
+            for a, m in enumerate(left):
+                if m > 0:
+                    order.append(a)
+                    left[a] -= 1
+        return cls(order, len(lengths))
+
+    @property
+    def c(self) -> nat.Axes:
+        return self._c
 
 
 def q4_code_shape(num_kv_heads: int, head_dim: int, layout: CacheLayout, batch: int, num_blocks: Optional[int] = None):
@@ -209,24 +248,37 @@ def _first(*tensors):
     for t in tensors:
         if t is not None:
             if not isinstance(t, torch.Tensor) or t.dim() != 4:
-                raise ValueError("q, k and v must be tensors [B][n_new][heads][D]")
+                raise ValueError("rows must be tensors [B][tokens][heads][D]")
             return t
-    raise ValueError("none of q, k and v is given")
+    raise ValueError("no rows are given")
 
 
-def _rotate_call(rotary, q, k, v, start_pos, q_out, k_out, v_out, new_lens, stream):
+def _positions(axes: RotaryAxes, rotary: Rotary, positions, batch: int, n_new: int):
+    """The device pointer of positions [num_axes][B][n_new]."""
+    pairs = 0 if rotary.cos_sin is None else rotary.cos_sin.shape[1] // 2
+    if len(axes.pair_axis) != pairs:
+        raise ValueError(f"axes of {len(axes.pair_axis)} pairs for a rotation of {pairs}")
+    _require(positions, "positions", (torch.int32,))
+    if tuple(positions.shape) != (axes.num_axes, batch, n_new):
+        raise ValueError(f"positions must be [{axes.num_axes}][{batch}][{n_new}], got {tuple(positions.shape)}")
+    return positions.data_ptr()
+
+
+def _rotate_call(rotary, q, k, v, start_pos, q_out, k_out, v_out, new_lens, stream, axes=None, positions=None):
     x = _first(q, k, v)
     b, n, d, dt = x.shape[0], x.shape[1], rotary.head_dim, x.dtype
     hq, hkv = rotary.num_q_heads, rotary.num_kv_heads
     rows = [_rows(t, name, b, n, h, d, dt) for t, name, h in ((q, "q", hq), (k, "k", hkv), (v, "v", hkv))]
     outs = [_dense(t, name, (b, n, h, d), dt) for t, name, h in ((q_out, "q_out", hq), (k_out, "k_out", hkv), (v_out, "v_out", hkv))]
-    tensors = (q, k, v, start_pos, q_out, k_out, v_out, new_lens) + rotary.tensors
-    device = _one_device(tensors)
+    tensors = (q, k, v, start_pos, positions, q_out, k_out, v_out, new_lens) + rotary.tensors
     vp = ctypes.c_void_p
-    args = (ctypes.byref(rotary.c), *map(_ref, rows), ctypes.c_int(_dtype_code(x)), ctypes.c_int32(b),
-            ctypes.c_int32(n), vp(_lens(new_lens, "new_lens", b)), vp(_lens(start_pos, "start_pos", b)),
+    at = _lens(start_pos, "start_pos", b) if axes is None else _positions(axes, rotary, positions, b, n)
+    device = _one_device(tensors)
+    args = (ctypes.byref(rotary.c), *(() if axes is None else (_ref(axes.c),)), *map(_ref, rows),
+            ctypes.c_int(_dtype_code(x)), ctypes.c_int32(b), ctypes.c_int32(n), vp(_lens(new_lens, "new_lens", b)), vp(at),
             *map(vp, outs), vp(_stream_of(stream, device)))
-    return _DeviceCall(nat.lib().nova_kv_rotate_qkv, args, (rotary, tensors, rows), device)
+    fn = nat.lib().nova_kv_rotate_qkv if axes is None else nat.lib().nova_kv_rotate_qkv_axes
+    return _DeviceCall(fn, args, (rotary, axes, tensors, rows), device)
 
 
 def _fresh(t, whole, stream):
@@ -261,20 +313,43 @@ def prepare_rotate_qkv(rotary: Rotary, q, k, v, start_pos, q_out, k_out, v_out, 
     return _rotate_call(rotary, q, k, v, start_pos, q_out, k_out, v_out, new_lens, stream)
 
 
-def _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream):
+def rotate_qkv_axes(rotary: Rotary, axes: RotaryAxes, q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                    v: Optional[torch.Tensor], positions: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
+                    q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                    v_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """nova_kv_rotate_qkv_axes: as rotate_qkv, every pair turned at its own axis' position of
+    positions [num_axes][B][n_new] (int32).
+
+    Tokens i >= new_lens[b] and those with a position outside the table are left out: their
+    output rows stay as they were (zeros in outputs that the call makes itself)."""
+    q_out, k_out, v_out = (o if o is not None or t is None else _fresh(t, False, stream)
+                           for t, o in ((q, q_out), (k, k_out), (v, v_out)))
+    _rotate_call(rotary, q, k, v, None, q_out, k_out, v_out, new_lens, stream, axes, positions)()
+    return q_out, k_out, v_out
+
+
+def prepare_rotate_qkv_axes(rotary: Rotary, axes: RotaryAxes, q, k, v, positions, q_out, k_out, v_out, new_lens=None,
+                            stream: Optional[torch.cuda.Stream] = None) -> PreparedCall:
+    """nova_kv_rotate_qkv_axes with the arguments of rotate_qkv_axes(), marshalled once."""
+    return _rotate_call(rotary, q, k, v, None, q_out, k_out, v_out, new_lens, stream, axes, positions)
+
+
+def _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream, axes=None, positions=None):
     x = _first(k)
     b, n, d, dt = x.shape[0], x.shape[1], rotary.head_dim, x.dtype
     hq, hkv = rotary.num_q_heads, rotary.num_kv_heads
     rows = [_rows(t, name, b, n, h, d, dt) for t, name, h in ((q, "q", hq), (k, "k", hkv), (v, "v", hkv))]
     outs = [_dense(t, name, (b, n, h, d), dt) for t, name, h in ((q_out, "q_out", hq), (k_held, "k_held", hkv), (v_held, "v_held", hkv))]
     cache.check_batch(b)
-    tensors = (q, k, v, start_pos, q_out, k_held, v_held, new_lens) + rotary.tensors + cache.tensors
-    device = _one_device(tensors)
+    tensors = (q, k, v, start_pos, positions, q_out, k_held, v_held, new_lens) + rotary.tensors + cache.tensors
     vp = ctypes.c_void_p
-    args = (ctypes.byref(rotary.c), ctypes.byref(cache.c), *map(_ref, rows), ctypes.c_int(_dtype_code(x)),
-            ctypes.c_int32(b), ctypes.c_int32(n), vp(_lens(new_lens, "new_lens", b)),
-            vp(_lens(start_pos, "start_pos", b)), *map(vp, outs), vp(_stream_of(stream, device)))
-    return _DeviceCall(nat.lib().nova_kv_q4_append, args, (rotary, cache, tensors, rows), device)
+    at = () if axes is None else (vp(_positions(axes, rotary, positions, b, n)),)
+    device = _one_device(tensors)
+    args = (ctypes.byref(rotary.c), *(() if axes is None else (_ref(axes.c),)), ctypes.byref(cache.c), *map(_ref, rows),
+            ctypes.c_int(_dtype_code(x)), ctypes.c_int32(b), ctypes.c_int32(n), vp(_lens(new_lens, "new_lens", b)),
+            vp(_lens(start_pos, "start_pos", b)), *at, *map(vp, outs), vp(_stream_of(stream, device)))
+    fn = nat.lib().nova_kv_q4_append if axes is None else nat.lib().nova_kv_q4_append_axes
+    return _DeviceCall(fn, args, (rotary, axes, cache, tensors, rows), device)
 
 
 def q4_append(rotary: Rotary, cache: Q4Cache, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
@@ -300,6 +375,72 @@ def prepare_q4_append(rotary: Rotary, cache: Q4Cache, q, k, v, start_pos, q_out,
                       v_held=None, stream: Optional[torch.cuda.Stream] = None) -> PreparedCall:
     """nova_kv_q4_append with the arguments of q4_append(), marshalled once."""
     return _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream)
+
+
+def q4_append_axes(rotary: Rotary, axes: RotaryAxes, cache: Q4Cache, q: Optional[torch.Tensor], k: torch.Tensor,
+                   v: torch.Tensor, start_pos: torch.Tensor, positions: torch.Tensor,
+                   new_lens: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                   k_held: Optional[torch.Tensor] = None, v_held: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+    """nova_kv_q4_append_axes: as q4_append, every pair turned at its own axis' position of
+    positions [num_axes][B][n_new] (int32); start_pos[b] + i is the token's place in the cache."""
+    if q is not None and q_out is None:
+        q_out = _fresh(q, False, stream)
+    _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream, axes, positions)()
+    return q_out
+
+
+def prepare_q4_append_axes(rotary: Rotary, axes: RotaryAxes, cache: Q4Cache, q, k, v, start_pos, positions, q_out,
+                           new_lens=None, k_held=None, v_held=None,
+                           stream: Optional[torch.cuda.Stream] = None) -> PreparedCall:
+    """nova_kv_q4_append_axes with the arguments of q4_append_axes(), marshalled once."""
+    return _append_call(rotary, cache, q, k, v, start_pos, q_out, new_lens, k_held, v_held, stream, axes, positions)
+
+
+def _read_shape(k_out, v_out, heads: int, head_dim: int):
+    """(batch, n, dtype) of the dense rows that a cache is read to."""
+    x = _first(k_out, v_out)
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {x.dtype}")
+    if tuple(x.shape[2:]) != (heads, head_dim):
+        raise ValueError(f"outputs must be [B][n][{heads}][{head_dim}], got {tuple(x.shape)}")
+    return x.shape[0], x.shape[1], x
+
+
+def _q4_read_call(cache, start_pos, k_out, v_out, lens, stream):
+    b, n, x = _read_shape(k_out, v_out, cache.num_kv_heads, cache.head_dim)
+    outs = [_dense(t, name, tuple(x.shape), x.dtype) for t, name in ((k_out, "k_out"), (v_out, "v_out"))]
+    cache.check_batch(b)
+    tensors = (start_pos, k_out, v_out, lens) + cache.tensors
+    vp = ctypes.c_void_p
+    args = (ctypes.byref(cache.c), ctypes.c_int(_dtype_code(x)), ctypes.c_int32(b), ctypes.c_int32(n),
+            vp(_lens(start_pos, "start_pos", b)), vp(_lens(lens, "lens", b)), *map(vp, outs))
+    device = _one_device(tensors)
+    return _DeviceCall(nat.lib().nova_kv_q4_read, args + (vp(_stream_of(stream, device)),), (cache, tensors), device)
+
+
+def q4_read(cache: Q4Cache, start_pos: torch.Tensor, n: int, lens: Optional[torch.Tensor] = None,
+            dtype: torch.dtype = torch.bfloat16, k_out: Optional[torch.Tensor] = None,
+            v_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """nova_kv_q4_read: the tokens start_pos[b] + i, i < n, of the 4-bit cache as dense rows
+    (k, v) [B][n][Hkv][D] of `dtype` (of k_out and v_out, when given).
+
+    Rows i >= lens[b], of positions outside the cache and in blocks that hold nothing stay as
+    they were: zeros in outputs that the call makes itself."""
+    if k_out is None and v_out is None:
+        shape = (start_pos.numel(), n, cache.num_kv_heads, cache.head_dim)
+        with torch.cuda.stream(stream):
+            k_out, v_out = (torch.zeros(shape, dtype=dtype, device=cache.device) for _ in range(2))
+    elif _first(k_out, v_out).shape[1] != n:
+        raise ValueError(f"outputs of {_first(k_out, v_out).shape[1]} tokens, {n} are read")
+    _q4_read_call(cache, start_pos, k_out, v_out, lens, stream)()
+    return k_out, v_out
+
+
+def prepare_q4_read(cache: Q4Cache, start_pos, k_out, v_out, lens=None,
+                    stream: Optional[torch.cuda.Stream] = None) -> PreparedCall:
+    """nova_kv_q4_read to k_out and v_out [B][n][Hkv][D] (either may be None), marshalled once."""
+    return _q4_read_call(cache, start_pos, k_out, v_out, lens, stream)
 
 
 def q4_attn_workspace_bytes(cache: Q4Cache, batch: int, n_q: int, num_q_heads: int, max_seq_len: int) -> int:
