@@ -48,6 +48,7 @@ struct ChunkPlan {
   size_t off_part, total;  // workspace: arrival counters, then the split partials (needed when n_split > 1)
 };
 ChunkPlan plan_chunk(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int q_bf16, int max_seq_len, int window);
+hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // more than 32 rows; launch_chunk calls it
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);
 
 }  // namespace novakv

@@ -17,38 +17,14 @@
 #include <type_traits>
 
 #include "chunk_common.h"
-#include "q4_common.h"
 
 namespace novakv {
 
 namespace {
 
 using namespace chunk;
-using q4::exp2_raw;
-using q4::half_factor;
-using q4::kNone;
-using q4::Tile;
-using lut::add_rows16;
-using lut::add_rows32;
-using lut::max_rows16;
-using lut::max_rows32;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRound = 32;  // tokens a wave takes at a time
-// log2 of the largest probability (times its value's scale) after a rescale, and how far it may grow
-constexpr float kTop = 6.f, kSlack = 8.f;
-constexpr int kLeastValue = -70;  // exponent of the smallest value scale that the reference follows
-
-// Coordinate of output tile o's row m: of sums over codewords, and over a band's rows.
-template <int D>
-__device__ __forceinline__ int code_coord(const int o, const int m) {
-  return D == 128 ? 16 * (m & 7) + 8 * (m >> 3) + o : 16 * (m & 3) + 4 * (m >> 2) + o;
-}
-template <int D>
-__device__ __forceinline__ int band_coord(const int o, const int m) {
-  return (D / 16) * m + o;
-}
 
 template <int D, bool WIDE, int NT, bool SQ, int W>
 struct Lds {
@@ -70,16 +46,6 @@ struct Lds {
   static constexpr int kBytes = kLast + 16;
   static_assert(kBytes <= 160 * 1024, "LDS of a workgroup");
 };
-
-// Three bf16 parts of an fp32 value: 24 bits.
-__device__ __forceinline__ void split_bf16(const float x, __bf16 &a, __bf16 &b, __bf16 &c) {
-  float y = x;
-  asm volatile("" : "+v"(y));
-  a = static_cast<__bf16>(y);
-  y -= static_cast<float>(a);
-  b = static_cast<__bf16>(y);
-  c = static_cast<__bf16>(y - static_cast<float>(b));
-}
 
 // D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows. SQ: the scalar value arm. W: waves.
 // ALIGNED: blocks of a multiple of 16 rows.
@@ -105,16 +71,11 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
   q4::place_tile(a, kRows, g);
   if (!q4::find_span(a, kRows, kRound * W, g)) return;
   const int b = g.b, kv = g.kv;
-  // what the split attends: codes [c0, c1), and the band's positions in front of and behind them
-  const int low = max(g.t0, g.lo);
-  const int rec = a.band_k ? max(g.S - a.n_rec, a.n_sink) : g.t1;
-  const int c0 = max(low, a.n_sink), c1 = min(g.t1, rec);
-  const int sink1 = min(g.t1, a.n_sink), rec0 = max(low, rec);
-  const bool codes = c0 < c1, banded = a.band_k && (low < sink1 || rec0 < g.t1);
+  const Spans span(a, g);
+  const int c0 = span.c0, c1 = span.c1;
 
   // this lane's rows: their queries, and the attended positions [row_lo, row_hi)
   int row_lo[NT], row_hi[NT];
-  size_t q_at[NT];
   float q[NT][kSteps][8];  // coordinates 32 s + 8 j + e
   for (int t = 0; t < NT; ++t) {
     const int row = g.row0 + 16 * t + n;
@@ -122,49 +83,16 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
     const int i = row / a.gqa, h = row - i * a.gqa;
     row_hi[t] = on ? g.last_pos(a, row) + 1 : 0;
     row_lo[t] = on ? g.first_pos(a, row) : 0;
-    q_at[t] = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + h) * D + 8 * j;
+    const size_t at = ((static_cast<size_t>(b) * a.n_q + i) * a.num_q_heads + kv * a.gqa + h) * D + 8 * j;
     for (int s = 0; s < kSteps; ++s)
       for (int e = 0; e < 8; ++e) q[t][s][e] = 0.f;
     if (!on) continue;
-    for (int s = 0; s < kSteps; ++s) {
-      if constexpr (WIDE) {
-        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + q_at[t] + 32 * s);
-        const float4 u = p[0], v = p[1];
-        q[t][s][0] = u.x, q[t][s][1] = u.y, q[t][s][2] = u.z, q[t][s][3] = u.w;
-        q[t][s][4] = v.x, q[t][s][5] = v.y, q[t][s][6] = v.z, q[t][s][7] = v.w;
-      } else {
-        const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + q_at[t] + 32 * s);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-        for (int e = 0; e < 4; ++e) q[t][s][2 * e] = __uint_as_float(u[e] << 16), q[t][s][2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-      }
-    }
+    for (int s = 0; s < kSteps; ++s) load_query<WIDE>(a.q, at + 32 * s, q[t][s]);
   }
 
-  float ref[NT], sum[NT], off_sum[NT];
-  float4_t acc[NT][kTiles];
-  auto clear = [&]() {
-    for (int t = 0; t < NT; ++t) {
-      ref[t] = kNone, sum[t] = 0.f, off_sum[t] = 0.f;
-      for (int o = 0; o < kTiles; ++o) acc[t][o] = float4_t{0.f, 0.f, 0.f, 0.f};
-    }
-  };
-  // A round's weights from its scores s (kNone: hidden): exp2(s by - ref), the references raised
-  // where a weight (times 2^exponent of its value's scale) would leave fp16.
-  auto raise = [&](const float (&bound)[NT]) {
-    bool over = false;
-    for (int t = 0; t < NT; ++t) over |= bound[t] > ref[t] + (kTop + kSlack);
-    if (!__any(over)) return;
-    for (int t = 0; t < NT; ++t) {
-      const float to = fmaxf(ref[t], max_rows32(max_rows16(bound[t])) - kTop);
-      const float f = to == kNone ? 1.f : half_factor(ref[t] - to);
-      ref[t] = to;
-      for (int y = 0; y < 2; ++y) {
-        sum[t] *= f;
-        off_sum[t] *= f;
-        for (int o = 0; o < kTiles; ++o) acc[t][o] *= f;
-      }
-    }
-  };
+  Sums<D, NT> y;
+  auto &ref = y.ref, &sum = y.sum, &off_sum = y.off_sum;
+  auto &acc = y.acc;
   // The waves' sums, whose tile o's row m is coordinate coord(o, m), merged: s_merged, s_mref, s_msum.
   // shift: what the logits of a row lack.
   auto merge_waves = [&](auto coord, const float (&shift)[NT]) {
@@ -203,91 +131,16 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
   float4 other[NT];
   float other_ref[NT], other_sum[NT];
   for (int t = 0; t < NT; ++t) other[t] = make_float4(0.f, 0.f, 0.f, 0.f), other_ref[t] = kNone, other_sum[t] = 0.f;
-  if (banded) {
-    constexpr int kQParts = WIDE ? 3 : 1, kPParts = WIDE ? 3 : 2;
-    clear();
-    bf16x8 qb[NT][kSteps][kQParts];
-    for (int t = 0; t < NT; ++t)
-      for (int s = 0; s < kSteps; ++s)
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (WIDE) {
-            __bf16 u, v, w;
-            split_bf16(q[t][s][e], u, v, w);
-            qb[t][s][0][e] = u, qb[t][s][1][e] = v, qb[t][s][2][e] = w;
-          } else {
-            qb[t][s][0][e] = static_cast<__bf16>(q[t][s][e]);
-          }
-        }
-    const size_t rows = (static_cast<size_t>(b) * a.num_kv_heads + kv) * (a.n_sink + a.n_rec);
-    auto attend = [&](const int tb, const int from, const int to) {  // positions [from, to) of the 32 from tb on
-      auto row_of = [&](const int tok) {
-        return (rows + band_slot(min(max(tok, from), to - 1), a.n_sink, a.n_rec)) * D;
-      };
-      float4_t s[NT][2];
-      for (int x = 0; x < 2; ++x) {
-        const uint16_t *k = a.band_k + row_of(tb + 16 * x + n) + 8 * j;
-        for (int t = 0; t < NT; ++t) s[t][x] = float4_t{0.f, 0.f, 0.f, 0.f};
-        for (int st = 0; st < kSteps; ++st) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k + 32 * st);
-          for (int t = 0; t < NT; ++t)
-            for (int p = 0; p < kQParts; ++p) s[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qb[t][st][p], s[t][x], 0, 0, 0);
-        }
-      }
-      // a lane's eight tokens 16 x + 4 j + i, D / 16 coordinates of each
-      uint32_t v[8][D / 32];
-      bool odd[8];
-      for (int e = 0; e < 8; ++e) {
-        const int tok = tb + 16 * (e >> 2) + 4 * j + (e & 3);
-        const uint32_t *p = reinterpret_cast<const uint32_t *>(a.band_v + row_of(tok) + (D / 16) * n);
-        bool bad = false;
-        for (int y = 0; y < D / 32; ++y) {
-          v[e][y] = p[y];
-          bad |= (v[e][y] & 0x7f80u) == 0x7f80u || (v[e][y] & 0x7f800000u) == 0x7f800000u;
-        }
-        // A value that is not finite would reach the rows it is hidden from (0 * NaN): the token's
-        // score becomes NaN instead, and the value 0.
-        const uint64_t any = __ballot(bad);
-        odd[e] = (any >> (16 * j)) & 0xffffu;
-        for (int y = 0; y < D / 32; ++y) v[e][y] = odd[e] ? 0u : v[e][y];
-      }
-      float bound[NT];
-      for (int t = 0; t < NT; ++t) {
-        bound[t] = kNone;
-        for (int x = 0; x < 2; ++x)
-          for (int i = 0; i < 4; ++i) {
-            const int tok = tb + 16 * x + 4 * j + i;
-            const bool seen = tok >= max(from, row_lo[t]) && tok < min(to, row_hi[t]);
-            const float z = s[t][x][i] * a.qscale;
-            s[t][x][i] = seen ? (odd[4 * x + i] ? __builtin_nanf("") : z) : kNone;
-            bound[t] = fmaxf(bound[t], s[t][x][i]);
-          }
-      }
-      raise(bound);
-      bf16x8 pf[NT][kPParts];
-      for (int t = 0; t < NT; ++t) {
-        const float r = ref[t] == kNone ? 0.f : ref[t];
-        for (int e = 0; e < 8; ++e) {
-          const float p = exp2_raw(s[t][e >> 2][e & 3] - r);
-          sum[t] += p;
-          __bf16 u, w, y;
-          split_bf16(p, u, w, y);
-          pf[t][0][e] = u, pf[t][1][e] = w;
-          if constexpr (kPParts == 3) pf[t][2][e] = y;
-        }
-      }
-      for (int o = 0; o < kTiles; ++o) {
-        uint32_t w[4];
-        for (int y = 0; y < 4; ++y) w[y] = __builtin_amdgcn_perm(v[2 * y + 1][o / 2], v[2 * y][o / 2], o & 1 ? 0x07060302u : 0x05040100u);
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        for (int t = 0; t < NT; ++t)
-          for (int p = 0; p < kPParts; ++p) acc[t][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][p], acc[t][o], 0, 0, 0);
-      }
-    };
-    for (int tb = (low & ~31) + kRound * wave; tb < sink1; tb += kRound * W) attend(tb, low, sink1);
-    for (int tb = (rec0 & ~31) + kRound * wave; tb < g.t1; tb += kRound * W) attend(tb, rec0, g.t1);
+  if (span.banded) {
+    y.clear();
+    Band<D, WIDE, NT> band(a, b, kv, lane);
+    for (int t = 0; t < NT; ++t) band.set_queries(t, q[t]);
+    for (int tb = (span.low & ~31) + kRound * wave; tb < span.sink1; tb += kRound * W)
+      band.attend(tb, span.low, span.sink1, row_lo, row_hi, y);
+    for (int tb = (span.rec0 & ~31) + kRound * wave; tb < g.t1; tb += kRound * W) band.attend(tb, span.rec0, g.t1, row_lo, row_hi, y);
     float none[NT];
     for (int t = 0; t < NT; ++t) none[t] = 0.f;
-    merge_waves([&](const int o, const int m) { return band_coord<D>(o, m); }, none);
+    merge_waves([](const int o, const int m) { return q4::out_coord<D>(o, m & 3, m >> 2); }, none);
     for (int t = 0; t < NT; ++t) {
       other[t] = *reinterpret_cast<const float4 *>(s_merged + (16 * t + n) * M::kStride + 16 * (wave & (kTiles - 1)) + 4 * j);
       other_ref[t] = s_mref[16 * t + n];
@@ -296,10 +149,10 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
     __syncthreads();
   }
 
-  clear();
+  y.clear();
   float shift[NT];
   for (int t = 0; t < NT; ++t) shift[t] = 0.f;
-  if (codes) {
+  if (span.codes) {
     // ---- q' = q R_K^-T: each wave makes 16 of its coordinates for all rows
     const void *tk = transform_of(a.t_k_inv_t, kv, D, a.t_bf16);
     const bool makes = wave < kTiles;
@@ -420,9 +273,6 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
       if constexpr (SQ) r.sq = reinterpret_cast<const uint32_t *>(a.v_sq)[mine];
     };
     const int inner_lo = g.first_pos(a, g.row1 - 1), inner_hi = g.last_pos(a, g.row0) + 1;  // seen by all rows
-    auto pair = [](const uint32_t x, const uint32_t y, const bool high) {
-      return __builtin_amdgcn_perm(y, x, high ? 0x07060302u : 0x05040100u);
-    };
     Round cur;
     look_up();
     request(cur);
@@ -437,16 +287,8 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
         const bool in = tok >= c0 && tok < c1;
         float rho = a.k_scales ? bf16_bits_to_float(now.rho) : 1.f;
         if constexpr (SQ) {
-          float scale = in ? __uint_as_float(now.sq << 16) : 0.f, offset = in ? __uint_as_float(now.sq & 0xffff0000u) : 0.f;
-          offset = __builtin_fmaf(1.5f, scale, offset);
-          // A value that is not finite: the token's score becomes NaN and the value 0, so that rows it is hidden from stay.
-          if (!(fabsf(scale) < __builtin_inff() && fabsf(offset) < __builtin_inff())) rho = __builtin_nanf(""), scale = offset = 0.f;
-          // the power of two above the scale or, where that is less, 2^-8 of the offset
-          const float size = fmaxf(fabsf(scale), 0x1p-8f * fabsf(offset));
-          if (lane < 32) {
-            s_tok[kRound + lane] = scale, s_tok[2 * kRound + lane] = offset;
-            s_tok[3 * kRound + lane] = static_cast<float>(max((__builtin_bit_cast(int, size) >> 23) - 126, kLeastValue));
-          }
+          const Grid v = grid_of(now.sq, in, rho);
+          if (lane < 32) s_tok[kRound + lane] = v.scale, s_tok[2 * kRound + lane] = v.offset, s_tok[3 * kRound + lane] = v.expo;
         }
         if (lane < 32) s_tok[lane] = rho;
         __builtin_amdgcn_wave_barrier();
@@ -500,7 +342,7 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
           bound[t] *= alpha[t];
         }
       }
-      raise(bound);
+      y.raise(bound);
       half8_t pf[NT][kParts];
       for (int t = 0; t < NT; ++t) {
         const float r = ref[t] == kNone ? 0.f : ref[t];
@@ -524,18 +366,18 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
         uint2 w[8];
         for (int e = 0; e < 8; ++e) {
           const uint32_t code = D == 128 ? (now.vw[e] >> (16 * (n >> 3) + 8 * p)) & 0xffu : (now.vw[e] >> (8 * (n >> 2))) & 0xffu;
-          const int group = D == 128 ? 4 * (n & 7) + 2 * (n >> 3) + p : 4 * (n & 3) + (n >> 2);
+          const int group = value_group<D>(n, p);
           if constexpr (SQ) w[e] = centred_levels(code);
           else w[e] = s_value[group * kCodebookSize + code];
         }
         for (int c = 0; c < 4; ++c) {
           uint32_t u[4];
-          for (int y = 0; y < 4; ++y)
-            u[y] = c < 2 ? pair(w[2 * y].x, w[2 * y + 1].x, c & 1) : pair(w[2 * y].y, w[2 * y + 1].y, c & 1);
+          for (int x = 0; x < 4; ++x)
+            u[x] = c < 2 ? half_pair(w[2 * x].x, w[2 * x + 1].x, c & 1) : half_pair(w[2 * x].y, w[2 * x + 1].y, c & 1);
           const half8_t vf = __builtin_bit_cast(half8_t, make_uint4(u[0], u[1], u[2], u[3]));
           for (int t = 0; t < NT; ++t)
-            for (int y = 0; y < kParts; ++y)
-              acc[t][4 * p + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][y], acc[t][4 * p + c], 0, 0, 0);
+            for (int x = 0; x < kParts; ++x)
+              acc[t][4 * p + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][x], acc[t][4 * p + c], 0, 0, 0);
         }
       }
     }
@@ -616,7 +458,7 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
 }
 
 template <int W>
-hipError_t launch_rows(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
+hipError_t launch_few(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
   const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
   auto go = [&](auto d, auto wide, auto nt, auto sq, auto aligned) {
     chunk_rows_kernel<d(), wide(), nt(), sq(), W, aligned()><<<groups, 64 * W, 0, stream>>>(a);
@@ -638,18 +480,18 @@ hipError_t launch_rows(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t st
 
 }  // namespace
 
-// Rows per workgroup: 16, or 32 where there are more.
+// Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the workgroup's waves dividing the
+// tokens; more rows take 16 or 32 a wave, 128 or 256 a workgroup.
 ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads, const int head_dim, const int q_bf16,
                      const int max_seq_len, const int window) {
   ChunkPlan p{};
   const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
-  p.tile_rows = rows <= 16 ? 16 : 32;
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
   const long long tiles = static_cast<long long>(p.row_tiles) * batch * num_kv_heads;
   const long long span = window > 0 ? std::min<long long>(max_seq_len, window + n_q) : max_seq_len;
-  auto most = [&](const long long s) {
-    return std::max(1LL, std::min<long long>({q4::kMaxSplits, (s + 127) / 128, q4::kMaxCounters / tiles}));
-  };
+  const long long limit = p.tile_rows >= 128 ? q4::kMaxSplitsTiled : q4::kMaxSplits;
+  auto most = [&](const long long s) { return std::max(1LL, std::min<long long>({limit, (s + 127) / 128, q4::kMaxCounters / tiles})); };
   // splits until the CUs have a workgroup each
   p.n_split = static_cast<int>(std::max(1LL, std::min({most(span), (span + 511) / 512, 256 / tiles})));
   p.off_part = q4::kMaxCounters * sizeof(int);
@@ -661,6 +503,8 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
   return p;
 }
 
-hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) { return launch_rows<8>(a, plan, stream); }
+hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
+  return plan.tile_rows >= 128 ? launch_chunk_tile(a, plan, stream) : launch_few<8>(a, plan, stream);
+}
 
 }  // namespace novakv

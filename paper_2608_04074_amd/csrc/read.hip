@@ -18,8 +18,6 @@ namespace {
 
 using namespace chunk;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
 // ------------------------------------------------------------------ 2 bits
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
