@@ -146,6 +146,7 @@ nova_kv_status nova_kv_read(const nova_kv_params *p, const nova_kv_layout *layou
     if ((st = check_layout(layout)) != NOVA_KV_OK) return st;
     if ((st = check_read_outputs(dtype, batch, n, p->num_kv_heads, p->head_dim, k_out, v_out)) != NOVA_KV_OK) return st;
     if (batch == 0 || n == 0 || (!k_out && !v_out)) return ok();
+    if (p->num_kv_heads > 4096) return fail(NOVA_KV_ERR_UNSUPPORTED, "num_kv_heads > 4096");  // a round's rows: 31 bits of bytes
     if (k_out && (st = check_scales(p, k_scales)) != NOVA_KV_OK) return st;
     if (v_out && (st = check_sq(p, v_sq)) != NOVA_KV_OK) return st;
     if ((st = check_band(band)) != NOVA_KV_OK) return st;

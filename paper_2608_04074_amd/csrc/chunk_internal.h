@@ -6,6 +6,21 @@
 
 namespace novakv {
 
+// position / block_size without a division or a branch: with 2^(l - 1) < d <= 2^l, ceil(2^(31 + l) / d) d lies
+// less than 2^l above 2^(31 + l), so the products of positions below 2^31 are cut to their quotients.
+struct BlockDivisor {
+  uint32_t factor;
+  int shift;
+  __host__ void set(const uint32_t d) {
+    shift = 31;
+    while ((1ull << (shift - 31)) < d) ++shift;
+    factor = static_cast<uint32_t>(((1ull << shift) + d - 1) / d);
+  }
+  __host__ __device__ __forceinline__ int operator()(const int pos) const {
+    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(pos)) * factor) >> shift);
+  }
+};
+
 // Tokens of a cache to be read as dense rows. k_out, v_out: [B][n][Hkv][D], nullptr: left out.
 struct ReadArgs {
   int batch, n, num_kv_heads, head_dim;
@@ -22,6 +37,7 @@ struct ReadArgs {
   int n_sink, n_rec;
   const uint16_t *band_k, *band_v;
   int chunk;  // tokens of a workgroup
+  BlockDivisor block_of;
   // 4-bit cache
   int num_blocks;
   const uint16_t *k_sq;  // and v_sq above

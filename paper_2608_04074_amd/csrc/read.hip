@@ -7,6 +7,11 @@
 // registers, as two fp16 parts (22 bits; one part where they are stored as bf16). The scalar
 // arm's levels enter as level - 1.5, exact, and meet the transform's row sums with the
 // token's offset + 1.5 scale.
+//
+// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 182 us, of
+// which the matrix cores work 62 and a copy of as many bytes would take 123. On the way there (241 us at first):
+// stores of 64 bytes of a row instead of 16, marked as streamed; no branch around them; the transform's
+// rows through LDS; one workgroup a CU for the whole call.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,15 +26,226 @@ using namespace chunk;
 // ------------------------------------------------------------------ 2 bits
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kStream = 2;  // stores of rows that are not read again here: 230 -> 198 us for 16 sequences' 8192 tokens
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// PARTS: fp16 parts of the transform.
-template <int D, int PARTS>
-__global__ __launch_bounds__(kThreads, 1) void read_kernel(const ReadArgs a) {
-  constexpr int L = D / kGroupDim, kSteps = D / 32, kTiles = 4;  // a wave has 64 of the coordinates
-  constexpr int kHalves = D / 64, kGroups = kWaves / kHalves;    // waves on tokens of their own
-  __shared__ uint2 s_book[L * kCodebookSize];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+// One side of a workgroup's tokens [first, last) of a sequence and KV head. LEVELS: the scalar
+// value arm. PARTS: fp16 parts of the transform. BAND: some positions are held in the band.
+template <int D, int PARTS, bool LEVELS, bool BAND, bool BF16>
+__device__ __forceinline__ void read_side(const ReadArgs &a, uint2 *s_book, float *s_rows, const bool value, const int kv, const int b, const int first,
+                                          const int last, const int place, const int places) {
+  constexpr int L = D / kGroupDim, kSteps = D / 16, kTiles = 2;  // a wave has 64 of the coordinates, 32 tokens at a time
+  constexpr int kHalves = D / 64, kTeams = kWaves / kHalves, kStride = 32 * kTeams;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 31, j = lane >> 5;
   const int half = wave % kHalves, team = wave / kHalves;
+  const long long cap = static_cast<long long>(a.layout.block_size) * a.layout.blocks_per_seq;
+  const int size = static_cast<int>(a.seq_lens ? min(max(static_cast<long long>(a.seq_lens[b]), 0LL), cap) : min(cap, 0x7fffffffLL));
+
+  // Loads and stores of the loop stand outside branches (a store that may not have been made would
+  // be waited for with every load), so lanes whose token is not there, or in the band, read the codes of the
+  // nearest that is: code positions [c0, c1); where there are none, the pool's first row.
+  const long long start = a.start_pos[b];
+  const int sinks = BAND ? a.n_sink : 0, recent = BAND ? min(max(size - a.n_rec, sinks), size) : size;
+  const int c0 = static_cast<int>(min(max(start + first, static_cast<long long>(sinks)), static_cast<long long>(size)));
+  const int c1 = static_cast<int>(min(max(start + last, 0LL), static_cast<long long>(recent)));
+  const bool coded = c0 < c1;
+  const uint8_t *codes = value ? a.v_codes : a.k_codes;
+  const int bs = a.layout.block_size;
+  // without a table (or codes): entries of a place that can be read, times 0
+  const bool mapped = a.layout.block_table && coded;
+  const int32_t *table = mapped ? a.layout.block_table + static_cast<size_t>(b) * a.layout.blocks_per_seq : a.start_pos + b;
+  int by_table = __builtin_amdgcn_readfirstlane(mapped ? 1 : 0);
+  asm volatile("" : "+s"(by_table));  // not turned into a branch
+  const int first_block = mapped || !coded ? 0 : b * a.layout.blocks_per_seq, by_order = coded ? 1 - by_table : 0;  // blocks are counted in 32 bits
+  const uint16_t *const extras = LEVELS ? a.v_sq : value ? nullptr : a.k_scales;
+  // Places are looked up two rounds of tokens ahead, codes requested one.
+  struct Place {
+    int phys, row;
+  };
+  struct Codes {
+    uint32_t w[L / 8], extra;
+  };
+  // The workgroups start at different rounds of their tokens, and go round: those of a large call would write to
+  // the same memory channels at the same time.
+  const int rounds = (last - first + kStride - 1) / kStride;
+  const int turn0 = static_cast<int>(static_cast<long long>(rounds) * place / places);
+  int turn = turn0;  // the next round to look up
+  auto find = [&](Place &k) {
+    const int pos = static_cast<int>(min(max(start + first + 32 * team + turn * kStride + n, static_cast<long long>(c0)), static_cast<long long>(c1) - 1));
+    const int blk = a.block_of(pos);
+    k.row = coded ? pos - blk * bs : 0;
+    k.phys = table[by_table * blk] * by_table + by_order * blk + first_block;
+    turn = turn + 1 == rounds ? 0 : turn + 1;
+  };
+  auto request = [&](const Place &k, Codes &c) {
+    const size_t row = (static_cast<size_t>(k.phys) * a.num_kv_heads + (coded ? kv : 0)) * bs + k.row;
+    const uint8_t *p = codes + row * L + (L / 2) * j;
+    if constexpr (D == 128) {
+      const uint4 w = *reinterpret_cast<const uint4 *>(p);
+      c.w[0] = w.x, c.w[1] = w.y, c.w[2] = w.z, c.w[3] = w.w;
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2 *>(p);
+      c.w[0] = w.x, c.w[1] = w.y;
+    }
+    if constexpr (LEVELS) {
+      c.extra = reinterpret_cast<const uint32_t *>(extras)[row];
+    } else {
+      const uint32_t rho = *(extras ? extras + row : reinterpret_cast<const uint16_t *>(a.start_pos + b));
+      c.extra = extras ? rho : 0x3f80u;  // 1
+    }
+  };
+  Place ahead;
+  Codes c;
+  find(ahead);
+
+  // A lane's results e = 16 o + i (of tile o) are kRun coordinates that follow each other, its other half's (j)
+  // beside them: coord_of(e, j). The transform's rows are dealt to the tiles that way; the contraction is in the
+  // codewords' order.
+  constexpr int kRun = BF16 ? 8 : 4;
+  auto coord_of = [](const int e, const int j) { return 2 * kRun * (e / kRun) + kRun * j + e % kRun; };
+  {
+    // through LDS, where rows are apart by an odd number of 16 bytes: a wave's loads of 64 rows' parts would
+    // otherwise be 64 requests each (12 us of a workgroup's time at head_dim 128)
+    constexpr int kPieces = D * D / 4 / kThreads;
+    const void *t = transform_of(value ? a.t_v : a.t_k_inv_t, kv, D, a.t_bf16);
+    T4 piece[kPieces];
+    for (int i = 0; i < kPieces; ++i) piece[i] = load_t4(t, 4 * (static_cast<size_t>(i) * kThreads + threadIdx.x), a.t_bf16);
+    if constexpr (!LEVELS) stage_book<L, kThreads>(s_book, value ? a.cb_v : a.cb_k, a.cb_fp8, kv);
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = 4 * (i * kThreads + threadIdx.x);
+      *reinterpret_cast<float4 *>(s_rows + (x / D) * (D + 4) + x % D) = t4_value(piece[i], a.t_bf16);
+    }
+  }
+  __syncthreads();
+  half8_t tr[kTiles][kSteps][PARTS];
+  float unscale[kTiles];
+#pragma unroll
+  for (int o = 0; o < kTiles; ++o) {
+    const int row = 64 * half + coord_of(16 * o + 4 * (n >> 3) + (n & 3), (n >> 2) & 1);
+    Eight raw[kSteps];
+    float top = 0.f;
+    for (int s = 0; s < kSteps; ++s) {
+      const float4 *p = reinterpret_cast<const float4 *>(s_rows + row * (D + 4) + (D / 2) * j + 8 * s);
+      const float4 u = p[0], v = p[1];
+      raw[s] = {{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}};
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(raw[s].x[e]));
+    }
+    const int up = up_to_14(wave_max(top));
+    const float scale = ldexpf(1.f, up);
+    unscale[o] = ldexpf(1.f, -up);
+    for (int s = 0; s < kSteps; ++s)
+      for (int e = 0; e < 8; ++e) {
+        _Float16 hi, lo;
+        split_half(raw[s].x[e] * scale, hi, lo);
+        tr[o][s][0][e] = hi;
+        if constexpr (PARTS == 2) tr[o][s][1][e] = lo;
+      }
+  }
+  request(ahead, c);
+  find(ahead);
+  auto times = [&](const half8_t (&x)[kSteps], float16_t (&acc)[kTiles]) {
+    for (int o = 0; o < kTiles; ++o)
+      for (int i = 0; i < 16; ++i) acc[o][i] = 0.f;
+    for (int s = 0; s < kSteps; ++s)
+      for (int p = 0; p < PARTS; ++p)
+        for (int o = 0; o < kTiles; ++o) acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(tr[o][s][p], x[s], acc[o], 0, 0, 0);
+  };
+  // what is added to a lane's 32 coordinates: k_bar, or the transform's row sums
+  float16_t bias[kTiles];
+  if constexpr (LEVELS) {
+    const _Float16 one = 1;
+    half8_t ones[kSteps];
+    for (int s = 0; s < kSteps; ++s) ones[s] = half8_t{one, one, one, one, one, one, one, one};
+    times(ones, bias);
+    for (int o = 0; o < kTiles; ++o) bias[o] *= unscale[o];
+  } else {
+    const float *kbar = a.kbar + kv * D + 64 * half;
+    for (int o = 0; o < kTiles; ++o)
+      for (int i = 0; i < 16; ++i) bias[o][i] = kbar[coord_of(16 * o + i, j)];
+    if (value)
+      for (int o = 0; o < kTiles; ++o)
+        for (int i = 0; i < 16; ++i) bias[o][i] = 0.f;
+  }
+
+  // the chunk's rows of the output; stores of lanes that have no token fall behind their end
+  constexpr int kBytes = BF16 ? 2 : 4;
+  const size_t row_bytes = static_cast<size_t>(a.num_kv_heads) * D * kBytes;
+  uint8_t *const out = static_cast<uint8_t *>(value ? a.v_out : a.k_out) + (static_cast<size_t>(b) * a.n + first) * row_bytes;
+  const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(out, 0, static_cast<int>((last - first) * row_bytes), 0x00020000);
+  constexpr int kOutside = -0x7fffffff - 1;  // 2^31, above any chunk's bytes, and some more stays so
+  const uint32_t book = (L / 2) * j * kCodebookSize;
+  for (int r = 0; r < rounds; ++r) {
+    const int at = r + turn0 < rounds ? r + turn0 : r + turn0 - rounds, tile = first + 32 * team + at * kStride;
+    half8_t x[kSteps];
+    for (int s = 0; s < kSteps; ++s) {
+      uint2 w[2];
+      for (int y = 0; y < 2; ++y) {
+        const int g = 2 * s + y;
+        const uint32_t code = (c.w[g / 4] >> (8 * (g & 3))) & 0xffu;
+        if constexpr (LEVELS) w[y] = centred_levels(code);
+        else w[y] = s_book[book + g * kCodebookSize + code];
+      }
+      x[s] = __builtin_bit_cast(half8_t, make_uint4(w[0].x, w[0].y, w[1].x, w[1].y));
+    }
+    const uint32_t extra = c.extra;
+    request(ahead, c);
+    find(ahead);
+    float16_t acc[kTiles];
+    times(x, acc);
+    float y[32];
+    if constexpr (LEVELS) {
+      const float scale = bf16_bits_to_float(extra & 0xffffu), offset = bf16_bits_to_float(extra >> 16);
+      const float add = __builtin_fmaf(1.5f, scale, offset);
+      for (int e = 0; e < 32; ++e) y[e] = __builtin_fmaf(scale, acc[e >> 4][e & 15] * unscale[e >> 4], add * bias[e >> 4][e & 15]);
+    } else {
+      const float rho = bf16_bits_to_float(extra), by[kTiles] = {rho * unscale[0], rho * unscale[1]};
+      for (int e = 0; e < 32; ++e) y[e] = __builtin_fmaf(by[e >> 4], acc[e >> 4][e & 15], bias[e >> 4][e & 15]);
+    }
+    auto there = [&](const int i) { return static_cast<int>(i < last) & static_cast<int>(start + i >= 0) & static_cast<int>(start + i < size); };
+    if constexpr (BAND) {
+      const long long pos = start + tile + n;
+      if (there(tile + n) && (pos < sinks || pos >= size - a.n_rec)) {
+        const int slot = band_slot(static_cast<int>(pos), a.n_sink, a.n_rec);
+        const uint16_t *row = (value ? a.band_v : a.band_k) +
+                              ((static_cast<size_t>(b) * a.num_kv_heads + kv) * (a.n_sink + a.n_rec) + slot) * D + 64 * half;
+        for (int e = 0; e < 32; e += 4) {
+          const uint2 w = *reinterpret_cast<const uint2 *>(row + coord_of(e, j));
+          y[e] = __uint_as_float(w.x << 16), y[e + 1] = __uint_as_float(w.x & 0xffff0000u);
+          y[e + 2] = __uint_as_float(w.y << 16), y[e + 3] = __uint_as_float(w.y & 0xffff0000u);
+        }
+      }
+    }
+    // Runs of two tokens 16 apart change places, so that a store has 64 bytes of a row from four lanes.
+    int to[2];
+    for (int x = 0; x < 2; ++x) {
+      const int i = tile + 16 * x + (n & 15);
+      to[x] = there(i) ? static_cast<int>((i - first) * row_bytes) + (kv * D + 64 * half + 2 * kRun * (n >> 4) + kRun * j) * kBytes : kOutside;
+    }
+    for (int h = 0; h < 32 / kRun; h += 2) {
+      uint32_t w[2][4];
+      for (int x = 0; x < 2; ++x)
+        for (int u = 0; u < 4; ++u) {
+          const float *from = y + kRun * (h + x) + (BF16 ? 2 * u : u);
+          if constexpr (BF16) w[x][u] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(from[0]), static_cast<__bf16>(from[1])});
+          else w[x][u] = __float_as_uint(from[0]);
+        }
+      for (int u = 0; u < 4; ++u) {
+        const auto s = __builtin_amdgcn_permlane16_swap(w[0][u], w[1][u], false, false);
+        w[0][u] = s[0], w[1][u] = s[1];
+      }
+      for (int x = 0; x < 2; ++x)
+        __builtin_amdgcn_raw_buffer_store_b128(uint4_t{w[x][0], w[x][1], w[x][2], w[x][3]}, rows, to[x], 2 * kRun * kBytes * h, kStream);
+    }
+  }
+}
+
+// SQ: values are the scalar arm's levels.
+template <int D, int PARTS, bool SQ, bool BAND, bool BF16>
+__global__ __launch_bounds__(kThreads, D == 64 && PARTS == 1 ? 4 : 2) void read_kernel(const ReadArgs a) {
+  __shared__ __align__(16) uint2 s_book[D / kGroupDim * kCodebookSize];
+  __shared__ __align__(16) float s_rows[D * (D + 4)];
   // (chunk, side, KV head fastest): the heads of a token, whose output rows follow each other, run together
   int wg = lut::xcd_contiguous(blockIdx.x, gridDim.x);
   const int kv = wg % a.num_kv_heads;
@@ -38,167 +254,16 @@ __global__ __launch_bounds__(kThreads, 1) void read_kernel(const ReadArgs a) {
   const bool value = !a.k_out || wg % sides == 1;
   wg /= sides;
   const int chunks = (a.n + a.chunk - 1) / a.chunk;
+  const int places = a.batch * chunks * sides, place = wg * sides + (value ? sides - 1 : 0);
   const int b = wg / chunks, first = (wg - b * chunks) * a.chunk;
   const int count = a.lens ? min(max(a.lens[b], 0), a.n) : a.n;
   const int last = min(first + a.chunk, count);
   if (first >= last) return;
-  const long long start = a.start_pos[b];
-  const long long cap = static_cast<long long>(a.layout.block_size) * a.layout.blocks_per_seq;
-  const long long size = a.seq_lens ? min(max(static_cast<long long>(a.seq_lens[b]), 0LL), cap) : cap;
-  const bool levels = value && a.v_sq;
-
-  // the transform's rows: tile o's row m is coordinate 64 half + 16 (m / 4) + 4 o + m % 4, so that a
-  // lane's results are 16 that follow each other; the contraction in the codewords' order
-  const void *t = transform_of(value ? a.t_v : a.t_k_inv_t, kv, D, a.t_bf16);
-  half8_t tr[kTiles][kSteps][PARTS];
-  float unscale;
-  {
-    Eight raw[kTiles][kSteps];
-    float top = 0.f;
-    for (int o = 0; o < kTiles; ++o) {
-      const int c = 64 * half + 16 * (n >> 2) + 4 * o + (n & 3);
-      for (int s = 0; s < kSteps; ++s) {
-        raw[o][s] = load_eight(t, static_cast<size_t>(c) * D + (D / 4) * j + 8 * s, a.t_bf16);
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(raw[o][s].x[e]));
-      }
-    }
-    const int up = up_to_14(wave_max(top));
-    const float scale = ldexpf(1.f, up);
-    unscale = ldexpf(1.f, -up);
-    for (int o = 0; o < kTiles; ++o)
-      for (int s = 0; s < kSteps; ++s)
-        for (int e = 0; e < 8; ++e) {
-          _Float16 hi, lo;
-          split_half(raw[o][s].x[e] * scale, hi, lo);
-          tr[o][s][0][e] = hi;
-          if constexpr (PARTS == 2) tr[o][s][1][e] = lo;
-        }
-  }
-  if (!levels) stage_book<L, kThreads>(s_book, value ? a.cb_v : a.cb_k, a.cb_fp8, kv);
-  auto times = [&](const half8_t (&x)[kSteps], float4_t (&acc)[kTiles]) {
-    for (int o = 0; o < kTiles; ++o) acc[o] = float4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < kSteps; ++s)
-      for (int p = 0; p < PARTS; ++p)
-        for (int o = 0; o < kTiles; ++o) acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(tr[o][s][p], x[s], acc[o], 0, 0, 0);
-  };
-  // what is added to a lane's 16 coordinates: k_bar, or the transform's row sums
-  const int coord = 64 * half + 16 * j;
-  float4_t bias[kTiles];
-  if (levels) {
-    const _Float16 one = 1;
-    half8_t ones[kSteps];
-    for (int s = 0; s < kSteps; ++s) ones[s] = half8_t{one, one, one, one, one, one, one, one};
-    times(ones, bias);
+  if constexpr (SQ) {
+    if (value) read_side<D, PARTS, true, BAND, BF16>(a, s_book, s_rows, true, kv, b, first, last, place, places);
+    else read_side<D, PARTS, false, BAND, BF16>(a, s_book, s_rows, false, kv, b, first, last, place, places);
   } else {
-    for (int o = 0; o < kTiles; ++o)
-      for (int i = 0; i < 4; ++i) bias[o][i] = value ? 0.f : a.kbar[kv * D + coord + 4 * o + i];
-  }
-  __syncthreads();
-
-  const uint8_t *codes = value ? a.v_codes : a.k_codes;
-  const int bs = a.layout.block_size;
-  const int32_t *table = a.layout.block_table ? a.layout.block_table + static_cast<size_t>(b) * a.layout.blocks_per_seq : nullptr;
-  const long long first_block = static_cast<long long>(b) * a.layout.blocks_per_seq;
-  // A lane's token: its place, its row, then its codes, each requested a tile of 16 tokens ahead.
-  struct Token {
-    int i;          // of the call, -1: none
-    int pos;
-    bool held;      // in the band
-    int phys, row;  // block (read from the table), row in it
-    uint32_t w[D / 64];
-    uint32_t extra;
-  };
-  constexpr int kStride = 16 * kGroups;
-  int at = first + 16 * team + n;
-  auto find = [&](Token &k) {
-    k.i = -1, k.held = false, k.phys = 0, k.row = 0, k.pos = 0;
-    const long long p = start + at;
-    if (at < last && p >= 0 && p < size) {
-      k.i = at;
-      k.pos = static_cast<int>(p);
-      k.held = a.band_k && (k.pos < a.n_sink || k.pos >= size - a.n_rec);
-      if (!k.held) {
-        const int blk = k.pos / bs;
-        k.row = k.pos - blk * bs;
-        k.phys = table ? table[blk] : static_cast<int>(first_block + blk);
-      }
-    }
-    at += kStride;
-  };
-  auto request = [&](Token &k) {  // of tokens that are not there or in the band: the pool's first row
-    const size_t row = (static_cast<size_t>(k.phys) * a.num_kv_heads + (k.i < 0 || k.held ? 0 : kv)) * bs + k.row;
-    const uint8_t *p = codes + row * L + (L / 4) * j;
-    if constexpr (D == 128) {
-      const uint2 w = *reinterpret_cast<const uint2 *>(p);
-      k.w[0] = w.x, k.w[1] = w.y;
-    } else {
-      k.w[0] = *reinterpret_cast<const uint32_t *>(p);
-    }
-    k.extra = 0;
-    if (levels) k.extra = reinterpret_cast<const uint32_t *>(a.v_sq)[row];
-    else if (!value && a.k_scales) k.extra = a.k_scales[row];
-  };
-  Token cur, next;
-  find(cur);
-  request(cur);
-  find(next);
-  const uint32_t book = (L / 4) * j * kCodebookSize;
-  for (int tile = first + 16 * team; tile < last; tile += kStride) {
-    half8_t x[kSteps];
-    for (int s = 0; s < kSteps; ++s) {
-      uint2 w[2];
-      for (int y = 0; y < 2; ++y) {
-        const int g = 2 * s + y;
-        const uint32_t code = (cur.w[g / 4] >> (8 * (g & 3))) & 0xffu;
-        w[y] = levels ? centred_levels(code) : s_book[book + g * kCodebookSize + code];
-      }
-      x[s] = __builtin_bit_cast(half8_t, make_uint4(w[0].x, w[0].y, w[1].x, w[1].y));
-    }
-    const Token mine = cur;
-    cur = next;
-    request(cur);
-    find(next);
-    float4_t acc[kTiles];
-    times(x, acc);
-    if (mine.i < 0) continue;
-    float by = unscale, add = 1.f;
-    if (levels) {
-      const float scale = bf16_bits_to_float(mine.extra & 0xffffu), offset = bf16_bits_to_float(mine.extra >> 16);
-      by = scale, add = __builtin_fmaf(1.5f, scale, offset);
-    } else if (!value && a.k_scales) {
-      by = bf16_bits_to_float(mine.extra) * unscale;
-    }
-    float y[16];
-    for (int o = 0; o < kTiles; ++o)
-      for (int i = 0; i < 4; ++i) {
-        if (levels) y[4 * o + i] = __builtin_fmaf(by, acc[o][i] * unscale, add * (bias[o][i] * unscale));
-        else y[4 * o + i] = __builtin_fmaf(by, acc[o][i], bias[o][i]);
-      }
-    const size_t to = ((static_cast<size_t>(b) * a.n + mine.i) * a.num_kv_heads + kv) * D + coord;
-    if (mine.held) {
-      const int slot = band_slot(mine.pos, a.n_sink, a.n_rec);
-      const uint16_t *row = (value ? a.band_v : a.band_k) +
-                            ((static_cast<size_t>(b) * a.num_kv_heads + kv) * (a.n_sink + a.n_rec) + slot) * D + coord;
-      for (int h = 0; h < 2; ++h) {
-        const uint4 w = reinterpret_cast<const uint4 *>(row)[h];
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-        for (int e = 0; e < 4; ++e) {
-          y[8 * h + 2 * e] = __uint_as_float(u[e] << 16);
-          y[8 * h + 2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-        }
-      }
-    }
-    void *out = value ? a.v_out : a.k_out;
-    if (a.bf16) {
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 v;
-        for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(y[8 * h + e]);
-        *reinterpret_cast<bf16x8 *>(static_cast<__bf16 *>(out) + to + 8 * h) = v;
-      }
-    } else {
-      for (int h = 0; h < 4; ++h)
-        reinterpret_cast<float4 *>(static_cast<float *>(out) + to)[h] = make_float4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
-    }
+    read_side<D, PARTS, false, BAND, BF16>(a, s_book, s_rows, value, kv, b, first, last, place, places);
   }
 }
 
@@ -265,16 +330,36 @@ hipError_t launch_read(const ReadArgs &args, hipStream_t stream) {
   ReadArgs a = args;
   const int sides = (a.k_out ? 1 : 0) + (a.v_out ? 1 : 0);
   const long long units = static_cast<long long>(a.batch) * a.num_kv_heads * sides;
-  const int step = 16 * kWaves / (a.head_dim / 64);
-  const long long want = std::max(1LL, 512 / units);  // chunks that fill the CUs with two workgroups each
-  a.chunk = static_cast<int>(((a.n + want - 1) / want + step - 1) / step * step);
+  const int step = 32 * kWaves / (a.head_dim / 64);
+  // Chunks: their number c that takes the least time, a workgroup's set-up being worth about 128 tokens; a CU holds
+  // one workgroup at head_dim 128, two at 64.
+  const long long seats = a.head_dim == 128 ? 256 : 512, rounds = (a.n + step - 1) / step;
+  long long best = 0;
+  for (int k = 0; k < 8; ++k) {
+    const long long c = std::max(1LL, k < 4 ? k + 1 : (k - 3) * seats / units);
+    const long long size = (rounds + c - 1) / c * step, time = (units * ((a.n + size - 1) / size) + seats - 1) / seats * (size + 128);
+    if (best == 0 || time < best) best = time, a.chunk = static_cast<int>(size);
+  }
+  a.block_of.set(static_cast<uint32_t>(a.layout.block_size));
+  // its rows' bytes are counted in 31 bits
+  const long long row_bytes = static_cast<long long>(a.num_kv_heads) * a.head_dim * (a.bf16 ? 2 : 4);
+  a.chunk = static_cast<int>(std::min<long long>(a.chunk, std::max(1LL, ((1LL << 31) - 1) / row_bytes / step) * step));
   const unsigned grid = static_cast<unsigned>(units * ((a.n + a.chunk - 1) / a.chunk));
+  using std::false_type;
   using std::integral_constant;
-  auto go = [&](auto d, auto parts) {
-    read_kernel<d(), parts()><<<grid, kThreads, 0, stream>>>(a);
+  using std::true_type;
+  auto go = [&](auto d, auto parts, auto sq, auto band, auto bf16) {
+    read_kernel<d(), parts(), sq(), band(), bf16()><<<grid, kThreads, 0, stream>>>(a);
     return hipGetLastError();
   };
-  auto by_parts = [&](auto d) { return a.t_bf16 ? go(d, integral_constant<int, 1>{}) : go(d, integral_constant<int, 2>{}); };
+  auto by_type = [&](auto d, auto parts, auto sq, auto band) {
+    return a.bf16 ? go(d, parts, sq, band, true_type{}) : go(d, parts, sq, band, false_type{});
+  };
+  auto by_band = [&](auto d, auto parts, auto sq) { return a.band_k ? by_type(d, parts, sq, true_type{}) : by_type(d, parts, sq, false_type{}); };
+  auto by_values = [&](auto d, auto parts) {
+    return a.v_out && a.v_sq ? by_band(d, parts, true_type{}) : by_band(d, parts, false_type{});
+  };
+  auto by_parts = [&](auto d) { return a.t_bf16 ? by_values(d, integral_constant<int, 1>{}) : by_values(d, integral_constant<int, 2>{}); };
   return a.head_dim == 128 ? by_parts(integral_constant<int, 128>{}) : by_parts(integral_constant<int, 64>{});
 }
 

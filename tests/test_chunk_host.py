@@ -103,6 +103,11 @@ def test_read_refusals(call, kw, status):
     assert nat.lib().nova_kv_last_error()
 
 
+def test_read_refuses_more_heads_than_a_round_holds():
+    more = dict(n=1, k_out=1 << 40, v_out=2 << 40)
+    assert read(params(num_kv_heads=4097), **more) == UNSUPPORTED and "4096" in nat.lib().nova_kv_last_error().decode()
+
+
 def test_read_refuses_bad_caches():
     assert read(k=None) == read(v=None) == read(k=(1 << 30) + 8) == INVALID
     assert read(params(flags=nat.NOVA_KV_KEY_SCALE)) == read(params(flags=nat.NOVA_KV_SQ_VALUES)) == INVALID
