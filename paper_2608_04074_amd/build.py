@@ -16,7 +16,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libnovakv.so")
 SOURCES = ["api.hip", "decode.hip", "decode_lut.hip", "decode_lut64.hip", "step_lut.hip", "step_lut64.hip",
-           "decode_vq.hip", "encode.hip", "chunk_rows.hip", "chunk_tile.hip", "rotate.hip", "rotate_axes.hip", "q4_attn.hip", "q4_tile.hip",
+           "decode_vq.hip", "encode.hip", "chunk_rows.hip", "chunk_tile.hip", "chunk_wide.hip", "rotate.hip", "rotate_axes.hip", "q4_attn.hip", "q4_tile.hip",
            "q4_api.hip", "read.hip", "chunk_api.hip", "host_checks.cpp"]
 ARCH = "gfx950"
 

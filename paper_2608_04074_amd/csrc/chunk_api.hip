@@ -99,6 +99,7 @@ nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout 
     a.gqa = num_q_heads / p->num_kv_heads;
     a.layout = novakv::CacheLayout{layout->block_size, layout->blocks_per_seq, layout->block_table};
     a.k_codes = k_codes;
+    a.block_of.set(static_cast<uint32_t>(layout->block_size));
     a.v_codes = v_codes;
     a.v_sq = (p->flags & NOVA_KV_SQ_VALUES) ? v_sq : nullptr;
     a.q = q;

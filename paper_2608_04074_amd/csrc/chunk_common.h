@@ -21,6 +21,20 @@ using q4::Tile;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// The physical blocks of a sequence, without a branch: a load that may not have been made would be waited
+// for at once. Without a table a place that can be read is, times 0.
+struct Blocks {
+  const int32_t *table;
+  int mapped, first;
+  __device__ __forceinline__ Blocks(const CacheLayout &layout, const int b, const int32_t *readable) {
+    mapped = __builtin_amdgcn_readfirstlane(layout.block_table ? 1 : 0);
+    asm volatile("" : "+s"(mapped));  // not turned back into a branch
+    table = layout.block_table ? layout.block_table + static_cast<size_t>(b) * layout.blocks_per_seq : readable;
+    first = layout.block_table ? 0 : b * layout.blocks_per_seq;
+  }
+  __device__ __forceinline__ int phys(const int blk) const { return table[mapped * blk] * mapped + (1 - mapped) * blk + first; }
+};
+
 // log2 of the largest probability (times its value's scale) after a rescale, and how far it may grow
 constexpr float kTop = 6.f, kSlack = 8.f;
 constexpr int kLeastValue = -70;  // exponent of the smallest value scale that the reference follows

@@ -54,6 +54,7 @@ struct ChunkArgs : Q4AttnArgs {
   const uint16_t *k_scales;  // key-scale format, else nullptr (v_sq: the scalar value arm, else nullptr)
   int n_sink, n_rec;
   const uint16_t *band_k, *band_v;
+  BlockDivisor block_of;
 };
 
 // Plan of a nova_kv_chunk_attn call: rows (query tokens * query heads per KV head) in tiles
@@ -64,7 +65,8 @@ struct ChunkPlan {
   size_t off_part, total;  // workspace: arrival counters, then the split partials (needed when n_split > 1)
 };
 ChunkPlan plan_chunk(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int q_bf16, int max_seq_len, int window);
-hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // more than 32 rows; launch_chunk calls it
+hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // tiles of 128 rows; launch_chunk calls it
+hipError_t launch_chunk_wide(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // of 256
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);
 
 }  // namespace novakv

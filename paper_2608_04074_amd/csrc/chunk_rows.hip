@@ -504,7 +504,9 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
 }
 
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
-  return plan.tile_rows >= 128 ? launch_chunk_tile(a, plan, stream) : launch_few<8>(a, plan, stream);
+  return plan.tile_rows == 256   ? launch_chunk_wide(a, plan, stream)
+         : plan.tile_rows == 128 ? launch_chunk_tile(a, plan, stream)
+                                 : launch_few<8>(a, plan, stream);
 }
 
 }  // namespace novakv
