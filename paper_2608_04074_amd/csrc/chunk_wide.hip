@@ -4,9 +4,12 @@
 // A workgroup of eight waves takes 256 rows, 32 a wave, and 64 (32) tokens a round. The waves
 // gather the tokens' codewords once, between them, from the codebooks in LDS to fragments in LDS,
 // in the order in which the matrix cores take them: a key's pairs of groups as they come, values
-// transposed in registers, a few tokens at a time. Both codebooks of head_dim 128 leave 32 KiB
-// beside them, so keys and values have one buffer each, used and filled in turn: while a round's
-// scores are made its values are gathered, while its weights meet the values the next round's keys are.
+// transposed in registers, a few tokens at a time. What a token has beside its codes (key scale, the
+// scalar arm's grid) every lane loads for one of 16 tokens, and the row of 16 lanes shares it.
+//
+// The two waves of a SIMD work in turn: while the first four make a round's scores, the last four weigh
+// the round before and meet its values, so that the matrix cores have work during either's softmax. Keys
+// and values so have two buffers each, which just fit beside both codebooks of head_dim 128 with 32 tokens.
 //
 // Queries go through R_K^-T and sums back through R_V on the matrix cores, without leaving the
 // wave: the transform's rows are dealt to the tiles so that a lane's results are its next operand.
@@ -25,6 +28,20 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 
 // A lane (row n = lane % 32, j = lane / 32) holds, of a tile of 32 by its 32 rows, the tile's rows 8 (i / 4) + 4 j + i % 4.
 __device__ __forceinline__ constexpr int tile_row(const int i, const int j) { return 8 * (i >> 2) + 4 * j + (i & 3); }
+// f(0) .. f(15), as constants.
+template <typename F>
+__device__ __forceinline__ void each16(F f) {
+  using std::integral_constant;
+  f(integral_constant<int, 0>{}), f(integral_constant<int, 1>{}), f(integral_constant<int, 2>{}), f(integral_constant<int, 3>{});
+  f(integral_constant<int, 4>{}), f(integral_constant<int, 5>{}), f(integral_constant<int, 6>{}), f(integral_constant<int, 7>{});
+  f(integral_constant<int, 8>{}), f(integral_constant<int, 9>{}), f(integral_constant<int, 10>{}), f(integral_constant<int, 11>{});
+  f(integral_constant<int, 12>{}), f(integral_constant<int, 13>{}), f(integral_constant<int, 14>{}), f(integral_constant<int, 15>{});
+}
+// The value of lane I of the lane's row of 16 (DPP row_newbcast).
+template <int I>
+__device__ __forceinline__ float of_row16(const float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x150 + I, 0xf, 0xf, false));
+}
 // Coordinate of output tile c's row m: a lane's codewords of a group are rows of all tiles.
 template <int D>
 __device__ __forceinline__ int coord(const int c, const int m) {
@@ -32,17 +49,15 @@ __device__ __forceinline__ int coord(const int c, const int m) {
 }
 
 // LDS of a workgroup, in bytes.
-template <int D, bool SQ, bool KS>
+template <int D, bool SQ>
 struct Lds {
   static constexpr int kTiles = D / 32, kSteps = D / 16;
-  static constexpr int kTokens = D == 128 && !SQ && KS ? 32 : 64, kRuns = kTokens / 32;  // a round's tokens, runs of 32
+  static constexpr int kTokens = D == 128 && !SQ ? 32 : 64, kRuns = kTokens / 32;  // a round's tokens, runs of 32
   static constexpr int kKeyFrags = kRuns * kSteps, kValueFrags = 2 * kRuns * kTiles;
   static constexpr int kBook = D / kGroupDim * kCodebookSize * 8;
-  static constexpr int kKeys = (SQ ? 1 : 2) * kBook;         // [run * kSteps + step][lane] 16 bytes
-  static constexpr int kValues = kKeys + kKeyFrags * 1024;   // [(2 * run + half) * kTiles + tile][lane]
-  static constexpr int kTok = kValues + kValueFrags * 1024;  // [round mod 2][rho, scale, offset, exponent][kTokens] fp32
-  static constexpr int kTokRound = (SQ ? 4 : KS ? 1 : 0) * kTokens;
-  static constexpr int kLoopEnd = kTok + 2 * kTokRound * 4;
+  static constexpr int kKeys = (SQ ? 1 : 2) * kBook;             // [round mod 2][run * kSteps + step][lane] 16 bytes
+  static constexpr int kValues = kKeys + 2 * kKeyFrags * 1024;   // [round mod 2][(2 * run + half) * kTiles + tile][lane]
+  static constexpr int kLoopEnd = kValues + 2 * kValueFrags * 1024;
   // in front of and behind the loop: a transform's parts [tile][step][hi, lo][lane] 16 bytes, made of its rows [D][D + 1]
   static constexpr int kRaw = kTiles * kSteps * 2 * 1024, kTops = kRaw + D * (D + 1) * 4, kTransformEnd = kTops + kWaves * 4;
   // at the end: the splits' merge
@@ -208,14 +223,13 @@ struct Band32 {
 // D: head_dim. WIDE: fp32 queries. SQ: the scalar value arm. KS: key scales. ALIGNED: blocks of a multiple of 16 rows.
 template <int D, bool WIDE, bool SQ, bool KS, bool ALIGNED>
 __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs a) {
-  using M = Lds<D, SQ, KS>;
+  using M = Lds<D, SQ>;
   constexpr int kParts = WIDE ? 2 : 1, L = D / kGroupDim, kSteps = M::kSteps, kTiles = M::kTiles, kTokens = M::kTokens, kRuns = M::kRuns;
   constexpr int kKeyUnits = M::kKeyFrags / kWaves;                // of a wave: fragments of keys
   constexpr int kValueTokens = kTokens * L / (64 * kWaves);       // of a lane: tokens of a value group, 2 or 4
   __shared__ __align__(16) uint8_t s_lds[M::kBytes];
   uint2 *const s_key_book = reinterpret_cast<uint2 *>(s_lds), *const s_value_book = s_key_book + L * kCodebookSize;
   half8_t *const s_keys = reinterpret_cast<half8_t *>(s_lds + M::kKeys), *const s_values = reinterpret_cast<half8_t *>(s_lds + M::kValues);
-  float *const s_tok = reinterpret_cast<float *>(s_lds + M::kTok);
   const half8_t *const s_frags = reinterpret_cast<const half8_t *>(s_lds);
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -298,12 +312,17 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
     const int eight = D == 64 ? (lane >> 4) & 1 : kTokens == 64 ? wave & 1 : (wave >> 1) & 1;
     const int pair = kValueTokens == 4 ? 0 : wave & 1;
     const int group = D == 128 ? n : lane & 15, value_token = 8 * eight + 4 * j + 2 * pair;
+    const int extra_token = tile_row(lane & 15, j);  // of a run, whose scale or grid this lane has for its row of 16 lanes
     const int bs = a.layout.block_size;
     const Blocks blocks(a.layout, b, a.seq_lens + b);
-    // Where a token's rows lie: the lane's key, then its values (ALIGNED: the first row of their 16).
-    constexpr int kPlaces = ALIGNED ? 2 : 1 + kValueTokens;
+    // Where a round's tokens lie. ALIGNED: the first row of each 16, looked up by a lane of each row; else the rows of the
+    // lane's key, its values and its extras' tokens.
+    constexpr int kPlaces = ALIGNED ? 1 : 1 + kValueTokens + kRuns;
     struct Look {
       int phys[kPlaces], row[kPlaces];
+    };
+    struct Places {
+      size_t key[2], value[ALIGNED ? 1 : kValueTokens], extra[2 * kRuns];  // key, extra: of both runs of 16 (else: [0] the lane's own)
     };
     int look_tb = c0 & ~31;
     auto look_up = [&](Look &k) {
@@ -314,56 +333,72 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
         k.phys[i] = blocks.phys(blk);
       };
       if constexpr (ALIGNED) {
-        auto inside = [&](const int tok) { return min(max(tok, c0 & ~15), (c1 - 1) & ~15); };
-        find(0, inside(look_tb + 32 * run + (n & 16)) + (n & 15));
-        find(1, __builtin_amdgcn_readfirstlane(inside(look_tb + 16 * step16)));
+        find(0, min(max(look_tb + 16 * ((lane >> 4) & (2 * kRuns - 1)), c0 & ~15), (c1 - 1) & ~15));
       } else {
         auto inside = [&](const int tok) { return min(max(tok, c0), c1 - 1); };
         find(0, inside(look_tb + 32 * run + n));
         for (int i = 0; i < kValueTokens; ++i) find(1 + i, inside(look_tb + 16 * step16 + value_token + i));
+        if constexpr (KS || SQ)
+          for (int x = 0; x < kRuns; ++x) find(1 + kValueTokens + x, inside(look_tb + 32 * x + extra_token));
       }
       look_tb += kTokens;
     };
-    auto row_at = [&](const Look &k, const int i) { return (static_cast<size_t>(k.phys[i]) * a.num_kv_heads + kv) * bs + k.row[i]; };
+    auto place = [&](const Look &k) {
+      auto row_of = [&](const int phys, const int row) { return (static_cast<size_t>(phys) * a.num_kv_heads + kv) * bs + row; };
+      Places p;
+      if constexpr (ALIGNED) {
+        auto first_of = [&](const int run16) {
+          return row_of(__builtin_amdgcn_readlane(k.phys[0], 16 * run16), __builtin_amdgcn_readlane(k.row[0], 16 * run16));
+        };
+        p.key[0] = first_of(2 * run), p.key[1] = first_of(2 * run + 1), p.value[0] = first_of(step16);
+        for (int i = 0; i < 2 * kRuns; ++i) p.extra[i] = KS || SQ ? first_of(i) : 0;
+      } else {
+        p.key[0] = row_of(k.phys[0], k.row[0]);
+        for (int i = 0; i < kValueTokens; ++i) p.value[i] = row_of(k.phys[1 + i], k.row[1 + i]);
+        for (int x = 0; x < kRuns; ++x) p.extra[2 * x] = KS || SQ ? row_of(k.phys[kPlaces - kRuns + x], k.row[kPlaces - kRuns + x]) : 0;
+      }
+      return p;
+    };
+    // row of a lane's token of a run of 32
+    auto row_in = [&](const size_t first, const size_t second, const int tok) { return ALIGNED ? (tok & 16 ? second : first) + (tok & 15) : first; };
     struct KeyCodes {
-      uint16_t code[kKeyUnits], rho;
-      uint32_t sq;
+      uint16_t code[kKeyUnits];
     };
     struct ValueCodes {
       uint8_t code[kValueTokens];
     };
-    auto request_keys = [&](const Look &k, KeyCodes &c) {
-      const size_t at = row_at(k, 0);
-      for (int u = 0; u < kKeyUnits; ++u)
-        c.code[u] = *reinterpret_cast<const uint16_t *>(a.k_codes + at * L + (L / 2) * j + 2 * (key_step + u * (kWaves / kRuns)));
-      if constexpr (KS) c.rho = a.k_scales[at];
-      if constexpr (SQ) c.sq = reinterpret_cast<const uint32_t *>(a.v_sq)[at];
+    struct Extras {
+      uint16_t rho[kRuns];
+      uint32_t sq[kRuns];
     };
-    auto request_values = [&](const Look &k, ValueCodes &c) {
-      for (int i = 0; i < kValueTokens; ++i)
-        c.code[i] = a.v_codes[(ALIGNED ? row_at(k, 1) + value_token + i : row_at(k, ALIGNED ? 1 : 1 + i)) * L + group];
+    auto request_keys = [&](const Places &p, KeyCodes &c) {
+      const uint8_t *from = a.k_codes + row_in(p.key[0], p.key[1], n) * L + (L / 2) * j + 2 * key_step;
+      for (int u = 0; u < kKeyUnits; ++u) c.code[u] = *reinterpret_cast<const uint16_t *>(from + 2 * u * (kWaves / kRuns));
     };
-    auto put_keys = [&](const KeyCodes &c, const int tb, const int parity) {
+    auto request_values = [&](const Places &p, ValueCodes &c, Extras &x) {
+      if constexpr (ALIGNED) {
+        const uint8_t *from = a.v_codes + p.value[0] * L + (value_token * L + group);
+        for (int i = 0; i < kValueTokens; ++i) c.code[i] = from[i * L];
+      } else {
+        for (int i = 0; i < kValueTokens; ++i) c.code[i] = a.v_codes[p.value[i] * L + group];
+      }
+      for (int r = 0; r < kRuns; ++r) {
+        if constexpr (KS || SQ) {
+          const size_t at = row_in(p.extra[2 * r], p.extra[2 * r + 1], extra_token);
+          if constexpr (KS) x.rho[r] = a.k_scales[at];
+          if constexpr (SQ) x.sq[r] = reinterpret_cast<const uint32_t *>(a.v_sq)[at];
+        }
+      }
+    };
+    auto put_keys = [&](const KeyCodes &c, const int parity) {
       for (int u = 0; u < kKeyUnits; ++u) {
         const int st = key_step + u * (kWaves / kRuns);
         const uint2 *book = s_key_book + ((L / 2) * j + 2 * st) * kCodebookSize;
         const uint2 w0 = book[c.code[u] & 0xffu], w1 = book[kCodebookSize + (c.code[u] >> 8)];
-        s_keys[(run * kSteps + st) * 64 + lane] = __builtin_bit_cast(half8_t, make_uint4(w0.x, w0.y, w1.x, w1.y));
-      }
-      if constexpr (KS || SQ) {
-        if (wave < kRuns && lane < 32) {
-          const int tok = tb + 32 * run + lane;
-          float *to = s_tok + parity * M::kTokRound + 32 * run + lane;
-          float rho = KS ? bf16_bits_to_float(c.rho) : 1.f;
-          if constexpr (SQ) {
-            const Grid v = grid_of(c.sq, tok >= c0 && tok < c1, rho);
-            to[kTokens] = v.scale, to[2 * kTokens] = v.offset, to[3 * kTokens] = v.expo;
-          }
-          to[0] = rho;
-        }
+        s_keys[(parity * M::kKeyFrags + run * kSteps + st) * 64 + lane] = __builtin_bit_cast(half8_t, make_uint4(w0.x, w0.y, w1.x, w1.y));
       }
     };
-    auto put_values = [&](const ValueCodes &c) {
+    auto put_values = [&](const ValueCodes &c, const int parity) {
       uint2 w[kValueTokens];
       for (int i = 0; i < kValueTokens; ++i) {
         if constexpr (SQ) w[i] = centred_levels(c.code[i]);
@@ -371,7 +406,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       }
       for (int x = 0; x < 4; ++x) {  // coordinate x of the group: tile and row of the fragment's lanes
         const int tile = D == 128 ? x : x & 1, m = D == 128 ? n : group + 16 * (x >> 1);
-        uint32_t *to = reinterpret_cast<uint32_t *>(s_values + (step16 * kTiles + tile) * 64 + 32 * j + m) + 2 * eight + pair;
+        uint32_t *to = reinterpret_cast<uint32_t *>(s_values + (parity * M::kValueFrags + step16 * kTiles + tile) * 64 + 32 * j + m) + 2 * eight + pair;
         uint32_t u[kValueTokens / 2];
         for (int i = 0; i < kValueTokens / 2; ++i)
           u[i] = x < 2 ? half_pair(w[2 * i].x, w[2 * i + 1].x, x & 1) : half_pair(w[2 * i].y, w[2 * i + 1].y, x & 1);
@@ -380,100 +415,122 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       }
     };
 
-    Look here, ahead, next;
+    // ---- a round's scores
+    auto make_scores = [&](const int parity, float16_t (&s)[kRuns]) {
+      for (int x = 0; x < kRuns; ++x)
+        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+      for (int st = 0; st < kSteps; ++st)
+        for (int x = 0; x < kRuns; ++x) {
+          const half8_t k = s_keys[(parity * M::kKeyFrags + x * kSteps + st) * 64 + lane];
+          for (int p = 0; p < kParts; ++p) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[st][p], s[x], 0, 0, 0);
+        }
+    };
+    // ---- their weights, which meet the values
+    auto weigh = [&](const int tb, const int parity, const Extras &extra, float16_t (&s)[kRuns]) {
+      float scale[kRuns], offset[kRuns], expo[kRuns];
+      if constexpr (KS || SQ) {
+        for (int x = 0; x < kRuns; ++x) {
+          float rho = 1.f;
+          if constexpr (KS) rho = bf16_bits_to_float(extra.rho[x]);
+          if constexpr (SQ) {
+            const int tok = tb + 32 * x + extra_token;
+            const Grid v = grid_of(extra.sq[x], tok >= c0 && tok < c1, rho);
+            scale[x] = v.scale, offset[x] = v.offset, expo[x] = v.expo;
+          }
+          each16([&](auto i) { s[x][i()] *= of_row16<i()>(rho); });
+        }
+      }
+      if (!(tb >= max(inner_lo, c0) && tb + kTokens <= min(inner_hi, c1))) {
+        for (int x = 0; x < kRuns; ++x)
+          for (int i = 0; i < 16; ++i) {
+            const int m = tb + 32 * x + tile_row(i, j);
+            const bool seen = static_cast<int>(m >= max(c0, row_lo)) & static_cast<int>(m < min(c1, row_hi));
+            s[x][i] = seen ? s[x][i] : kNone;
+          }
+      }
+      float bound = kNone;
+      for (int x = 0; x < kRuns; ++x) {
+        if constexpr (SQ) each16([&](auto i) { bound = fmaxf(bound, __builtin_fmaf(s[x][i()], alpha, of_row16<i()>(expo[x]))); });
+        else
+          for (int i = 0; i < 16; ++i) bound = fmaxf(bound, s[x][i]);
+      }
+      if constexpr (!SQ) bound *= alpha;
+      y.raise(bound);
+      const float r = y.ref == kNone ? 0.f : y.ref;
+      half8_t pf[2 * kRuns][kParts];
+      for (int x = 0; x < kRuns; ++x)
+        each16([&](auto i) {
+          float p = exp2_raw(__builtin_fmaf(s[x][i()], alpha, -r));
+          if constexpr (SQ || WIDE) y.sum += p;
+          if constexpr (SQ) {
+            y.off_sum = __builtin_fmaf(of_row16<i()>(offset[x]), p, y.off_sum);
+            p *= of_row16<i()>(scale[x]);
+          }
+          half8_t *to = pf[2 * x + i() / 8];
+          if constexpr (WIDE) {
+            _Float16 hi, lo;
+            split_half(p, hi, lo);
+            to[0][i() % 8] = hi, to[kParts - 1][i() % 8] = lo;
+          } else {
+            to[0][i() % 8] = static_cast<_Float16>(p);
+          }
+        });
+      if constexpr (!SQ && !WIDE) {  // the weights as they meet the values
+        const half2_t ones = {static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
+        for (int u = 0; u < 2 * kRuns; ++u)
+          for (int e = 0; e < 8; e += 2) y.sum = __builtin_amdgcn_fdot2(half2_t{pf[u][0][e], pf[u][0][e + 1]}, ones, y.sum, false);
+      }
+      for (int u = 0; u < 2 * kRuns; ++u)
+        for (int o = 0; o < kTiles; ++o) {
+          const half8_t v = s_values[(parity * M::kValueFrags + u * kTiles + o) * 64 + lane];
+          for (int p = 0; p < kParts; ++p) y.acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[u][p], y.acc[o], 0, 0, 0);
+        }
+    };
+
+    // Round i: the next round's scores, this one's weights; the codes of keys of round i + 2 and values of i + 1 become
+    // fragments, those of the rounds behind are requested (past the end: the last tokens again).
+    Look look;
     KeyCodes keys;
     ValueCodes values;
-    look_up(here);
-    look_up(ahead);
-    request_keys(here, keys);
-    request_values(here, values);
-    look_up(next);
+    Extras extra, extra_next;
+    float16_t s0[kRuns], s1[kRuns];
+    look_up(look);
+    Places ahead = place(look);
+    request_keys(ahead, keys);
+    request_values(ahead, values, extra);
+    look_up(look);
+    ahead = place(look);
+    look_up(look);
     __syncthreads();  // the codebooks are there
-    put_keys(keys, c0 & ~31, 0);
+    put_keys(keys, 0);
+    put_values(values, 0);
+    request_keys(ahead, keys);
+    request_values(ahead, values, extra_next);
+    ahead = place(look);
+    look_up(look);
+    put_keys(keys, 1);
     request_keys(ahead, keys);
     __syncthreads();
-    for (int tb = c0 & ~31, parity = 0; tb < c1; tb += kTokens, parity ^= 1) {
-      const bool mine = !idle && tb < wave_hi && tb + kTokens > wave_lo;
-      float16_t s[kRuns];
-      if (mine) {
-        for (int x = 0; x < kRuns; ++x)
-          for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
-        for (int st = 0; st < kSteps; ++st)
-          for (int x = 0; x < kRuns; ++x) {
-            const half8_t k = s_keys[(x * kSteps + st) * 64 + lane];
-            for (int p = 0; p < kParts; ++p) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[st][p], s[x], 0, 0, 0);
-          }
-      }
-      put_values(values);
-      request_values(ahead, values);
+    make_scores(0, s0);
+    __syncthreads();
+    auto round = [&](const int tb, const int parity, float16_t (&now)[kRuns], float16_t (&next)[kRuns]) {
+      make_scores(parity ^ 1, next);
+      put_values(values, parity ^ 1);
+      put_keys(keys, parity);
+      const Extras beside = extra;
+      extra = extra_next;
+      request_values(ahead, values, extra_next);
+      ahead = place(look);
+      request_keys(ahead, keys);
+      look_up(look);
+      weigh(tb, parity, beside, now);
       __syncthreads();
-      put_keys(keys, tb + kTokens, parity ^ 1);  // past the end: the last tokens again
-      request_keys(next, keys);
-      ahead = next;
-      look_up(next);
-      if (mine) {
-        const float *tok = s_tok + parity * M::kTokRound + 4 * j;
-        if constexpr (KS || SQ) {
-          for (int x = 0; x < kRuns; ++x)
-            for (int z = 0; z < 4; ++z) {
-              const float4 rho = *reinterpret_cast<const float4 *>(tok + 32 * x + 8 * z);
-              s[x][4 * z] *= rho.x, s[x][4 * z + 1] *= rho.y, s[x][4 * z + 2] *= rho.z, s[x][4 * z + 3] *= rho.w;
-            }
-        }
-        if (!(tb >= max(inner_lo, c0) && tb + kTokens <= min(inner_hi, c1))) {
-          for (int x = 0; x < kRuns; ++x)
-            for (int i = 0; i < 16; ++i) {
-              const int m = tb + 32 * x + tile_row(i, j);
-              const bool seen = static_cast<int>(m >= max(c0, row_lo)) & static_cast<int>(m < min(c1, row_hi));
-              s[x][i] = seen ? s[x][i] : kNone;
-            }
-        }
-        float bound = kNone;
-        for (int x = 0; x < kRuns; ++x)
-          for (int z = 0; z < 4; ++z) {
-            if constexpr (SQ) {
-              const float4 e = *reinterpret_cast<const float4 *>(tok + 3 * kTokens + 32 * x + 8 * z);
-              bound = fmaxf(fmaxf(bound, __builtin_fmaf(s[x][4 * z], alpha, e.x)), __builtin_fmaf(s[x][4 * z + 1], alpha, e.y));
-              bound = fmaxf(fmaxf(bound, __builtin_fmaf(s[x][4 * z + 2], alpha, e.z)), __builtin_fmaf(s[x][4 * z + 3], alpha, e.w));
-            } else {
-              for (int i = 4 * z; i < 4 * z + 4; ++i) bound = fmaxf(bound, s[x][i]);
-            }
-          }
-        if constexpr (!SQ) bound *= alpha;
-        y.raise(bound);
-        const float r = y.ref == kNone ? 0.f : y.ref;
-        half8_t pf[2 * kRuns][kParts];
-        for (int x = 0; x < kRuns; ++x)
-          for (int z = 0; z < 4; ++z) {
-            float p[4];
-            for (int i = 0; i < 4; ++i) {
-              p[i] = exp2_raw(__builtin_fmaf(s[x][4 * z + i], alpha, -r));
-              y.sum += p[i];
-            }
-            if constexpr (SQ) {
-              const float4 o = *reinterpret_cast<const float4 *>(tok + 2 * kTokens + 32 * x + 8 * z);
-              const float4 v = *reinterpret_cast<const float4 *>(tok + kTokens + 32 * x + 8 * z);
-              y.off_sum = __builtin_fmaf(p[0], o.x, __builtin_fmaf(p[1], o.y, __builtin_fmaf(p[2], o.z, __builtin_fmaf(p[3], o.w, y.off_sum))));
-              p[0] *= v.x, p[1] *= v.y, p[2] *= v.z, p[3] *= v.w;
-            }
-            for (int i = 0; i < 4; ++i) {
-              const int e = 4 * (z & 1) + i;
-              if constexpr (WIDE) {
-                _Float16 hi, lo;
-                split_half(p[i], hi, lo);
-                pf[2 * x + (z >> 1)][0][e] = hi, pf[2 * x + (z >> 1)][1][e] = lo;
-              } else {
-                pf[2 * x + (z >> 1)][0][e] = static_cast<_Float16>(p[i]);
-              }
-            }
-          }
-        for (int u = 0; u < 2 * kRuns; ++u)
-          for (int o = 0; o < kTiles; ++o) {
-            const half8_t v = s_values[(u * kTiles + o) * 64 + lane];
-            for (int p = 0; p < kParts; ++p) y.acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[u][p], y.acc[o], 0, 0, 0);
-          }
-      }
-      __syncthreads();
+    };
+    for (int tb = c0 & ~31;;) {
+      round(tb, 0, s0, s1);
+      if ((tb += kTokens) >= c1) break;
+      round(tb, 1, s1, s0);
+      if ((tb += kTokens) >= c1) break;
     }
 
     // ---- back through R_V
@@ -515,17 +572,17 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
   y.sum = add_rows32(y.sum);
   if (y.sum != y.sum && !(y.ref > kNone)) y.ref = 0.f;  // NaN logits move no reference, but attend
 
-  const q4::TileRows<D, kRows> place{a, g};
-  float *const part = place.part();
+  const q4::TileRows<D, kRows> rows{a, g};
+  float *const part = rows.part();
   const int r = row - g.row0;
   if (on) {
-    const float f = part ? 1.f : place.inverse(r, y.ref, y.sum);
+    const float f = part ? 1.f : rows.inverse(r, y.ref, y.sum);
     for (int x = 0; x < D / 8; ++x) {  // four coordinates from 4 times the row (D = 64: and its 16) on
       const int m = tile_row(x, j);
       const float4 v = D == 128 ? make_float4(y.acc[0][x], y.acc[1][x], y.acc[kTiles - 2][x], y.acc[kTiles - 1][x])
                                 : make_float4(y.acc[0][x], y.acc[1][x], y.acc[0][(x + 8) & 15], y.acc[1][(x + 8) & 15]);
       if (part) q4::publish4(part + r * D + 4 * m, v);
-      else q4::store_out(a, place.out_at(r) + 4 * m, place.scaled(v, f));
+      else q4::store_out(a, rows.out_at(r) + 4 * m, rows.scaled(v, f));
     }
     if (part && j == 0) q4::publish2(part + kRows * D + 2 * r, y.ref, y.sum);
   }
