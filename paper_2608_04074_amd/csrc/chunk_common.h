@@ -32,7 +32,8 @@ struct Blocks {
     table = layout.block_table ? layout.block_table + static_cast<size_t>(b) * layout.blocks_per_seq : readable;
     first = layout.block_table ? 0 : b * layout.blocks_per_seq;
   }
-  __device__ __forceinline__ int phys(const int blk) const { return table[mapped * blk] * mapped + (1 - mapped) * blk + first; }
+  __device__ __forceinline__ int entry(const int blk) const { return table[mapped * blk]; }
+  __device__ __forceinline__ int phys(const int entry, const int blk) const { return entry * mapped + (1 - mapped) * blk + first; }
 };
 
 // log2 of the largest probability (times its value's scale) after a rescale, and how far it may grow

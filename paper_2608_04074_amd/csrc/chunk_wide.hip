@@ -60,12 +60,9 @@ struct Lds {
   static constexpr int kLoopEnd = kValues + 2 * kValueFrags * 1024;
   // in front of and behind the loop: a transform's parts [tile][step][hi, lo][lane] 16 bytes, made of its rows [D][D + 1]
   static constexpr int kRaw = kTiles * kSteps * 2 * 1024, kTops = kRaw + D * (D + 1) * 4, kTransformEnd = kTops + kWaves * 4;
-  // at the end: the splits' merge
-  using Finish = q4::FinishLds<D, 2, kWaves, true>;
-  static_assert(Finish::kRows == kRows, "rows of a workgroup");
-  static constexpr int kInv = Finish::kMerge * 4, kLast = kInv + kRows * 4, kMergeEnd = kLast + 16;
   static constexpr int kMost = kLoopEnd > kTransformEnd ? kLoopEnd : kTransformEnd;
-  static constexpr int kBytes = kMost > kMergeEnd ? kMost : kMergeEnd;
+  static constexpr int kLast = 0;  // at the end
+  static constexpr int kBytes = kMost;
   static_assert(kBytes <= 160 * 1024, "LDS of a workgroup");
   static_assert(kKeyFrags % kWaves == 0, "the waves share the gathers evenly");
 };
@@ -172,21 +169,26 @@ struct Band32 {
   // Positions [from, to) of the 32 from tb on, for rows that attend [row_lo, row_hi).
   __device__ __forceinline__ void attend(const int tb, const int from, const int to, const int row_lo, const int row_hi, Sums32<D> &y) const {
     auto row_of = [&](const int tok) { return (rows + band_slot(min(max(tok, from), to - 1), a.n_sink, a.n_rec)) * D; };
+    // all loads in front of their first use
+    const uint16_t *k = a.band_k + row_of(tb + n) + 8 * j;
+    bf16x8 keys[kSteps];
+    for (int st = 0; st < kSteps; ++st) keys[st] = *reinterpret_cast<const bf16x8 *>(k + 16 * st);
+    uint32_t v[16][kTiles / 2];  // a lane's 16 tokens, its coordinates in all tiles
+    for (int i = 0; i < 16; ++i) {
+      const uint16_t *p = a.band_v + row_of(tb + tile_row(i, j));
+      for (int w = 0; w < kTiles / 2; ++w) v[i][w] = *reinterpret_cast<const uint32_t *>(p + coord<D>(2 * w, n));
+    }
     float16_t s;
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
-    const uint16_t *k = a.band_k + row_of(tb + n) + 8 * j;
     for (int st = 0; st < kSteps; ++st) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k + 16 * st);
+      const bf16x8 kf = keys[st];
       for (int p = 0; p < kQParts; ++p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[st][p], s, 0, 0, 0);
     }
     float bound = kNone;
-    uint32_t v[16][kTiles / 2];  // a lane's 16 tokens, its coordinates in all tiles
     for (int i = 0; i < 16; ++i) {
       const int tok = tb + tile_row(i, j);
-      const uint16_t *p = a.band_v + row_of(tok);
       bool bad = false;
       for (int w = 0; w < kTiles / 2; ++w) {
-        v[i][w] = *reinterpret_cast<const uint32_t *>(p + coord<D>(2 * w, n));
         bad |= (v[i][w] & 0x7f80u) == 0x7f80u || (v[i][w] & 0x7f800000u) == 0x7f800000u;
       }
       // A value that is not finite would reach the rows it is hidden from (0 * NaN): the token's
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
     // lane's key, its values and its extras' tokens.
     constexpr int kPlaces = ALIGNED ? 1 : 1 + kValueTokens + kRuns;
     struct Look {
-      int phys[kPlaces], row[kPlaces];
+      int entry[kPlaces], block[kPlaces], row[kPlaces];  // as loaded: arithmetic on it would wait for it
     };
     struct Places {
       size_t key[2], value[ALIGNED ? 1 : kValueTokens], extra[2 * kRuns];  // key, extra: of both runs of 16 (else: [0] the lane's own)
@@ -330,7 +332,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       auto find = [&](const int i, const int tok) {
         const int blk = a.block_of(tok);
         k.row[i] = tok - blk * bs;
-        k.phys[i] = blocks.phys(blk);
+        k.block[i] = blk;
+        k.entry[i] = blocks.entry(blk);
       };
       if constexpr (ALIGNED) {
         find(0, min(max(look_tb + 16 * ((lane >> 4) & (2 * kRuns - 1)), c0 & ~15), (c1 - 1) & ~15));
@@ -348,28 +351,31 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       Places p;
       if constexpr (ALIGNED) {
         auto first_of = [&](const int run16) {
-          return row_of(__builtin_amdgcn_readlane(k.phys[0], 16 * run16), __builtin_amdgcn_readlane(k.row[0], 16 * run16));
+          return row_of(blocks.phys(__builtin_amdgcn_readlane(k.entry[0], 16 * run16), __builtin_amdgcn_readlane(k.block[0], 16 * run16)),
+                        __builtin_amdgcn_readlane(k.row[0], 16 * run16));
         };
         p.key[0] = first_of(2 * run), p.key[1] = first_of(2 * run + 1), p.value[0] = first_of(step16);
         for (int i = 0; i < 2 * kRuns; ++i) p.extra[i] = KS || SQ ? first_of(i) : 0;
       } else {
-        p.key[0] = row_of(k.phys[0], k.row[0]);
-        for (int i = 0; i < kValueTokens; ++i) p.value[i] = row_of(k.phys[1 + i], k.row[1 + i]);
-        for (int x = 0; x < kRuns; ++x) p.extra[2 * x] = KS || SQ ? row_of(k.phys[kPlaces - kRuns + x], k.row[kPlaces - kRuns + x]) : 0;
+        p.key[0] = row_of(blocks.phys(k.entry[0], k.block[0]), k.row[0]);
+        for (int i = 0; i < kValueTokens; ++i) p.value[i] = row_of(blocks.phys(k.entry[1 + i], k.block[1 + i]), k.row[1 + i]);
+        for (int x = 0; x < kRuns; ++x) {
+          const int i = kPlaces - kRuns + x;
+          p.extra[2 * x] = KS || SQ ? row_of(blocks.phys(k.entry[i], k.block[i]), k.row[i]) : 0;
+        }
       }
       return p;
     };
     // row of a lane's token of a run of 32
     auto row_in = [&](const size_t first, const size_t second, const int tok) { return ALIGNED ? (tok & 16 ? second : first) + (tok & 15) : first; };
     struct KeyCodes {
-      uint16_t code[kKeyUnits];
+      uint32_t code[kKeyUnits];
     };
     struct ValueCodes {
-      uint8_t code[kValueTokens];
+      uint32_t code[kValueTokens];
     };
     struct Extras {
-      uint16_t rho[kRuns];
-      uint32_t sq[kRuns];
+      uint32_t rho[kRuns], sq[kRuns];
     };
     auto request_keys = [&](const Places &p, KeyCodes &c) {
       const uint8_t *from = a.k_codes + row_in(p.key[0], p.key[1], n) * L + (L / 2) * j + 2 * key_step;
@@ -431,7 +437,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       if constexpr (KS || SQ) {
         for (int x = 0; x < kRuns; ++x) {
           float rho = 1.f;
-          if constexpr (KS) rho = bf16_bits_to_float(extra.rho[x]);
+          if constexpr (KS) rho = __uint_as_float(extra.rho[x] << 16);
           if constexpr (SQ) {
             const int tok = tb + 32 * x + extra_token;
             const Grid v = grid_of(extra.sq[x], tok >= c0 && tok < c1, rho);
@@ -572,24 +578,64 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
   y.sum = add_rows32(y.sum);
   if (y.sum != y.sum && !(y.ref > kNone)) y.ref = 0.f;  // NaN logits move no reference, but attend
 
+  // A lane's values in fours of coordinates from 4 tile_row(x, j) on (D = 64: registers x and x + 8).
   const q4::TileRows<D, kRows> rows{a, g};
   float *const part = rows.part();
-  const int r = row - g.row0;
-  if (on) {
-    const float f = part ? 1.f : rows.inverse(r, y.ref, y.sum);
-    for (int x = 0; x < D / 8; ++x) {  // four coordinates from 4 times the row (D = 64: and its 16) on
-      const int m = tile_row(x, j);
-      const float4 v = D == 128 ? make_float4(y.acc[0][x], y.acc[1][x], y.acc[kTiles - 2][x], y.acc[kTiles - 1][x])
-                                : make_float4(y.acc[0][x], y.acc[1][x], y.acc[0][(x + 8) & 15], y.acc[1][(x + 8) & 15]);
-      if (part) q4::publish4(part + r * D + 4 * m, v);
-      else q4::store_out(a, rows.out_at(r) + 4 * m, rows.scaled(v, f));
-    }
-    if (part && j == 0) q4::publish2(part + kRows * D + 2 * r, y.ref, y.sum);
+  auto four = [&](const int x) {
+    return D == 128 ? make_float4(y.acc[0][x], y.acc[1][x], y.acc[kTiles - 2][x], y.acc[kTiles - 1][x])
+                    : make_float4(y.acc[0][x], y.acc[1][x], y.acc[0][(x + 8) & 15], y.acc[1][(x + 8) & 15]);
+  };
+  if (!part) {
+    if (!on) return;
+    const float f = rows.inverse(row - g.row0, y.ref, y.sum);
+    for (int x = 0; x < D / 8; ++x) q4::store_out(a, rows.out_at(row - g.row0) + 4 * tile_row(x, j), rows.scaled(four(x), f));
+    return;
   }
-  if (!part) return;
-  __syncthreads();  // the transform is done with
-  q4::merge_splits<D, 2, kWaves, true>(a, g, {reinterpret_cast<float *>(s_lds), nullptr, nullptr, reinterpret_cast<float *>(s_lds + M::kInv),
-                                              reinterpret_cast<int *>(s_lds + M::kLast)}, lane & 15);
+  // Splits: their values lie as the lanes hold them, so that the words of a store (8 bytes each, with device
+  // coherence) follow each other; the last workgroup of the tile to arrive merges them, in their order.
+  if (!idle) {
+    uint64_t *words = reinterpret_cast<uint64_t *>(part) + wave * (D / 4) * 64 + lane;
+    for (int x = 0; x < D / 8; ++x) {
+      const float4 v = four(x);
+      q4::publish2(reinterpret_cast<float *>(words + 2 * x * 64), v.x, v.y);
+      q4::publish2(reinterpret_cast<float *>(words + (2 * x + 1) * 64), v.z, v.w);
+    }
+    if (j == 0) q4::publish2(part + kRows * D + 2 * (32 * wave + n), y.ref, y.sum);
+  }
+  int *const s_last = reinterpret_cast<int *>(s_lds + M::kLast);
+  __builtin_amdgcn_s_waitcnt(0);  // this thread's words have landed
+  __syncthreads();
+  int *const counter = a.counters + static_cast<size_t>(g.unit) * a.row_tiles + g.tile;
+  if (threadIdx.x == 0)
+    *s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.n_split - 1;
+  __syncthreads();
+  if (!*s_last) return;
+  if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (idle) return;
+  const float *const parts = part - g.split * rows.kSlot;
+  float most = kNone, l = 0.f;
+  for (int u = 0; u < a.n_split; ++u) most = fmaxf(most, q4::fetch2(parts + u * rows.kSlot + kRows * D + 2 * (32 * wave + n)).x);
+  for (int o = 0; o < kTiles; ++o)
+    for (int i = 0; i < 16; ++i) y.acc[o][i] = 0.f;
+  for (int u = 0; u < a.n_split; ++u) {
+    const float *from = parts + u * rows.kSlot;
+    const float2 ml = q4::fetch2(from + kRows * D + 2 * (32 * wave + n));
+    const bool some = ml.x != kNone;  // a split of no weight counts all the same: it may hold a NaN
+    const float f = some ? half_factor(ml.x - most) : 0.f;
+    if (some) l += f * ml.y * f;
+    const uint64_t *words = reinterpret_cast<const uint64_t *>(from) + wave * (D / 4) * 64 + lane;
+    for (int x = 0; x < D / 8; ++x) {
+      const float2 v = q4::fetch2(reinterpret_cast<const float *>(words + 2 * x * 64)),
+                   w = q4::fetch2(reinterpret_cast<const float *>(words + (2 * x + 1) * 64));
+      auto of = [&](const float value) { return some ? f * value * f : 0.f; };
+      y.acc[0][x] += of(v.x), y.acc[1][x] += of(v.y);
+      if constexpr (D == 128) y.acc[kTiles - 2][x] += of(w.x), y.acc[kTiles - 1][x] += of(w.y);
+      else y.acc[0][(x + 8) & 15] += of(w.x), y.acc[1][(x + 8) & 15] += of(w.y);
+    }
+  }
+  if (!on) return;
+  const float f = rows.inverse(row - g.row0, most, l);
+  for (int x = 0; x < D / 8; ++x) q4::store_out(a, rows.out_at(row - g.row0) + 4 * tile_row(x, j), rows.scaled(four(x), f));
 }
 
 }  // namespace

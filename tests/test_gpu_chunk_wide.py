@@ -1,0 +1,39 @@
+"""nova_kv_chunk_attn with more than 128 rows per KV head (tiles of 256 rows) in every format: the bounds and the
+oracle of test_gpu_chunk_attn.py."""
+
+import numpy as np
+import pytest
+import torch
+
+from chunk_cases import FORMATS
+from test_gpu_chunk_attn import BF, F32, check, nk  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,dtype", ((64, BF), (64, F32), (128, BF), (128, F32)))
+def test_formats(nk, fmt, D, dtype):  # noqa: F811
+    """Two tiles, the second of few rows; lengths that end inside a round; idle and short sequences."""
+    check(nk, [333, 70, 0, 5], 66, 4, 1, D, dtype, block=16, fmt=fmt, q_lens=[66, 33, 0, 5])
+    check(nk, [1100, 130], 130, 2, 1, D, dtype, fmt=fmt, q_lens=[130, 129])
+
+
+@pytest.mark.parametrize("block", (1, 7, 24, 48))
+@pytest.mark.parametrize("D,dtype,fmt", ((64, BF, "scaled"), (128, F32, "plain"), (128, BF, "deployed"), (64, F32, "sq")))
+def test_pages(nk, block, D, dtype, fmt):  # noqa: F811
+    check(nk, [515, 131], 67, 4, 2, D, dtype, block=block, fmt=fmt)
+
+
+@pytest.mark.parametrize("window", (1, 33, 128, 400))
+@pytest.mark.parametrize("D,dtype,fmt", ((64, BF, "plain"), (128, F32, "deployed"), (128, BF, "band")))
+def test_windows_and_sinks(nk, window, D, dtype, fmt):  # noqa: F811
+    """Windows shorter than a tile's positions: waves of one workgroup attend spans apart."""
+    sinks = np.array([-np.inf, 3.0])
+    check(nk, [700, 150], 150, 2, 2, D, dtype, block=16, fmt=fmt, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("seq,n,window", ((5000, 40, 0), (5000, 300, 700)))
+@pytest.mark.parametrize("D,dtype,fmt", ((64, F32, "deployed"), (128, BF, "plain"), (128, F32, "scaled")))
+def test_splits(nk, seq, n, window, D, dtype, fmt):  # noqa: F811
+    check(nk, [seq, seq // 3], n, 8, 1, D, dtype, block=16, fmt=fmt, window=window)
