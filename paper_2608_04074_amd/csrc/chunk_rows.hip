@@ -14,6 +14,7 @@
 // Positions that a band holds are attended first, with their exact bf16 rows on the bf16
 // cores; their share joins behind R_V.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "chunk_common.h"
@@ -494,6 +495,11 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
   auto most = [&](const long long s) { return std::max(1LL, std::min<long long>({limit, (s + 127) / 128, q4::kMaxCounters / tiles})); };
   // splits until the CUs have a workgroup each
   p.n_split = static_cast<int>(std::max(1LL, std::min({most(span), (span + 511) / 512, 256 / tiles})));
+  // One workgroup merges a tile's splits, for about as long a split as 32 (of 256 rows: 45) of its tokens take.
+  if (p.tile_rows >= 128) {
+    const double per = p.tile_rows == 128 ? 32. : 45.;
+    p.n_split = std::max(1, std::min(p.n_split, static_cast<int>(std::sqrt(static_cast<double>(span) / per))));
+  }
   p.off_part = q4::kMaxCounters * sizeof(int);
   const long long all = most(max_seq_len);
   if (all > 1) {

@@ -1,13 +1,15 @@
-// Attention of many query rows over the 2-bit cache (nova_kv_chunk_attn with more than 32 rows
-// per KV head: chunks of prompts).
+// Attention of 33 to 128 query rows per KV head over the 2-bit cache (nova_kv_chunk_attn: short chunks of prompts).
 //
-// A workgroup of eight waves takes 256 (128) rows, 32 (16) a wave, and 32 or 64 tokens a round. The
-// waves gather the tokens' codewords once, between them, from the codebooks in LDS to fragments
+// A workgroup of eight waves takes 128 rows, 16 a wave, and 32 or 64 tokens a round. The waves
+// gather the tokens' codewords once, between them, from the codebooks in LDS to fragments
 // in LDS, in the order in which the matrix cores take them: a key's pairs of groups as they
 // come, values transposed in registers, two tokens at a time. Both codebooks of head_dim 128 leave
 // 32 KiB beside them, so keys and values have one buffer each, used and filled in turn: while a
 // round's scores are made its values are gathered, while its weights meet the values the next
 // round's keys are.
+//
+// Tiles of 256 rows (chunk_wide.hip) for such calls leave half of their waves idle: 32 queries of 4 heads over 16384
+// tokens 104 us here, 240 there; over 8192 tokens of 16 sequences 233 and 220.
 //
 // Queries go through R_K^-T and sums back through R_V on the matrix cores, without leaving the
 // wave: the transform's rows are dealt to the tiles so that a lane's results are its next operand.
@@ -439,11 +441,9 @@ hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStrea
   auto by_keys = [&](auto d, auto wide, auto nt, auto sq) {
     return a.k_scales ? by_blocks(d, wide, nt, sq, true_type{}) : by_blocks(d, wide, nt, sq, false_type{});
   };
-  auto by_values = [&](auto d, auto wide, auto nt) { return a.v_sq ? by_keys(d, wide, nt, true_type{}) : by_keys(d, wide, nt, false_type{}); };
-  auto by_rows = [&](auto d, auto wide) {
-    return plan.tile_rows == 128 ? by_values(d, wide, integral_constant<int, 1>{}) : by_values(d, wide, integral_constant<int, 2>{});
-  };
-  auto by_type = [&](auto d) { return a.q_bf16 ? by_rows(d, false_type{}) : by_rows(d, true_type{}); };
+  const integral_constant<int, 1> one;  // tile of 16 rows a wave
+  auto by_values = [&](auto d, auto wide) { return a.v_sq ? by_keys(d, wide, one, true_type{}) : by_keys(d, wide, one, false_type{}); };
+  auto by_type = [&](auto d) { return a.q_bf16 ? by_values(d, false_type{}) : by_values(d, true_type{}); };
   return a.head_dim == 128 ? by_type(integral_constant<int, 128>{}) : by_type(integral_constant<int, 64>{});
 }
 

@@ -613,24 +613,33 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
   if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if (idle) return;
   const float *const parts = part - g.split * rows.kSlot;
+  auto stat = [&](const int u) { return q4::fetch2(parts + u * rows.kSlot + kRows * D + 2 * (32 * wave + n)); };
   float most = kNone, l = 0.f;
-  for (int u = 0; u < a.n_split; ++u) most = fmaxf(most, q4::fetch2(parts + u * rows.kSlot + kRows * D + 2 * (32 * wave + n)).x);
+#pragma unroll 8
+  for (int u = 0; u < a.n_split; ++u) most = fmaxf(most, stat(u).x);
   for (int o = 0; o < kTiles; ++o)
     for (int i = 0; i < 16; ++i) y.acc[o][i] = 0.f;
-  for (int u = 0; u < a.n_split; ++u) {
-    const float *from = parts + u * rows.kSlot;
-    const float2 ml = q4::fetch2(from + kRows * D + 2 * (32 * wave + n));
-    const bool some = ml.x != kNone;  // a split of no weight counts all the same: it may hold a NaN
-    const float f = some ? half_factor(ml.x - most) : 0.f;
-    if (some) l += f * ml.y * f;
-    const uint64_t *words = reinterpret_cast<const uint64_t *>(from) + wave * (D / 4) * 64 + lane;
-    for (int x = 0; x < D / 8; ++x) {
-      const float2 v = q4::fetch2(reinterpret_cast<const float *>(words + 2 * x * 64)),
-                   w = q4::fetch2(reinterpret_cast<const float *>(words + (2 * x + 1) * 64));
+  constexpr int kAhead = 256 / D;  // splits whose words are requested at once
+  for (int first = 0; first < a.n_split; first += kAhead) {
+    float2 ml[kAhead], v[kAhead][D / 4];
+    for (int z = 0; z < kAhead; ++z) {
+      const int u = min(first + z, a.n_split - 1);
+      ml[z] = stat(u);
+      const uint64_t *words = reinterpret_cast<const uint64_t *>(parts + u * rows.kSlot) + wave * (D / 4) * 64 + lane;
+      for (int x = 0; x < D / 4; ++x) v[z][x] = q4::fetch2(reinterpret_cast<const float *>(words + x * 64));
+    }
+    for (int z = 0; z < kAhead; ++z) {
+      // a split of no weight counts all the same: it may hold a NaN
+      const bool some = first + z < a.n_split && ml[z].x != kNone;
+      const float f = some ? half_factor(ml[z].x - most) : 0.f;
+      if (some) l += f * ml[z].y * f;
       auto of = [&](const float value) { return some ? f * value * f : 0.f; };
-      y.acc[0][x] += of(v.x), y.acc[1][x] += of(v.y);
-      if constexpr (D == 128) y.acc[kTiles - 2][x] += of(w.x), y.acc[kTiles - 1][x] += of(w.y);
-      else y.acc[0][(x + 8) & 15] += of(w.x), y.acc[1][(x + 8) & 15] += of(w.y);
+      for (int x = 0; x < D / 8; ++x) {
+        const float2 p = v[z][2 * x], q = v[z][2 * x + 1];
+        y.acc[0][x] += of(p.x), y.acc[1][x] += of(p.y);
+        if constexpr (D == 128) y.acc[kTiles - 2][x] += of(q.x), y.acc[kTiles - 1][x] += of(q.y);
+        else y.acc[0][(x + 8) & 15] += of(q.x), y.acc[1][(x + 8) & 15] += of(q.y);
+      }
     }
   }
   if (!on) return;
