@@ -467,7 +467,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
       for (int x = 0; x < kRuns; ++x)
         each16([&](auto i) {
           float p = exp2_raw(__builtin_fmaf(s[x][i()], alpha, -r));
-          if constexpr (SQ || WIDE) y.sum += p;
+          y.sum += p;  // not of fp16 parts: small weights of many tokens would be lost
           if constexpr (SQ) {
             y.off_sum = __builtin_fmaf(of_row16<i()>(offset[x]), p, y.off_sum);
             p *= of_row16<i()>(scale[x]);
@@ -481,11 +481,6 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_wide_kernel(const ChunkArgs
             to[0][i() % 8] = static_cast<_Float16>(p);
           }
         });
-      if constexpr (!SQ && !WIDE) {  // the weights as they meet the values
-        const half2_t ones = {static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
-        for (int u = 0; u < 2 * kRuns; ++u)
-          for (int e = 0; e < 8; e += 2) y.sum = __builtin_amdgcn_fdot2(half2_t{pf[u][0][e], pf[u][0][e + 1]}, ones, y.sum, false);
-      }
       for (int u = 0; u < 2 * kRuns; ++u)
         for (int o = 0; o < kTiles; ++o) {
           const half8_t v = s_values[(parity * M::kValueFrags + u * kTiles + o) * 64 + lane];

@@ -5,8 +5,9 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_cases import FORMATS
-from test_gpu_chunk_attn import BF, F32, check, nk  # noqa: F401
+from chunk_cases import FORMATS, Cache
+from oracle.q4 import to_bf16_bits
+from test_gpu_chunk_attn import BF, F32, call, check, nk  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +38,23 @@ def test_windows_and_sinks(nk, window, D, dtype, fmt):  # noqa: F811
 @pytest.mark.parametrize("D,dtype,fmt", ((64, F32, "deployed"), (128, BF, "plain"), (128, F32, "scaled")))
 def test_splits(nk, seq, n, window, D, dtype, fmt):  # noqa: F811
     check(nk, [seq, seq // 3], n, 8, 1, D, dtype, block=16, fmt=fmt, window=window)
+
+
+@pytest.mark.parametrize("dtype", (BF, F32))
+@pytest.mark.parametrize("n", (1, 40, 150))
+def test_a_long_tail_of_small_weights(nk, n, dtype):  # noqa: F811
+    """One key's weight is e^10.5 times that of each of 40000 others, which together weigh more than it: weights
+    below fp16's normal numbers count, in sums as beside values."""
+    S, D = 40000, 64
+    c = Cache(nk, 11, [S], 1, D, 16, "key_scale", kbar_size=0.0)
+    phys, row = c.where[0]
+    c.ks[phys, :, row] = to_bf16_bits(np.full((S, 1), 2.0 ** -20))
+    c.ks[phys[7], :, row[7]] = to_bf16_bits(np.ones(1))
+    c.k_scales = torch.as_tensor(c.ks.view(np.int16)).cuda().view(BF)
+    key = c.rows(0, 0)[0][7]
+    q = torch.as_tensor(np.broadcast_to(key * (10.5 * np.sqrt(D) / (key @ key)), (1, n, 1, D)).copy()).to(dtype).cuda()
+    got = call(c, q).double().cpu().numpy()
+    ref, tol = c.attend(q.double().cpu().numpy(), [n], bf16=dtype == BF)
+    assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) - tol).max()
+    # the bound tells a lost tail: without it the outputs are the one value
+    assert (np.abs(c.rows(0, 0)[1][7] - ref) > 4 * tol).any()
