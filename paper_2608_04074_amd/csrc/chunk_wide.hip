@@ -11,7 +11,7 @@
 // tokens, so a round has one barrier, and makes the next round's scores beside its own weights.
 //
 // Bound by issue: of a round's cycles the matrix cores, the vector units (four instructions a score, an
-// exponential counting twice, and the gathers) and LDS are busy 45, 55 and 40 percent, and overlap in part. Two
+// exponential counting twice, and the gathers) and LDS are busy 39, 47 and 41 percent, and overlap in part. Two
 // sequences' 2048 queries of 4 heads over 8192 tokens take 560 us (871 TFLOP/s); one buffer and two barriers 650,
 // the two waves of a SIMD in opposite phases 777, each wave gathering for itself 902.
 //

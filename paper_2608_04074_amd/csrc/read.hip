@@ -8,10 +8,11 @@
 // arm's levels enter as level - 1.5, exact, and meet the transform's row sums with the
 // token's offset + 1.5 scale.
 //
-// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 182 us, of
+// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 170 us, of
 // which the matrix cores work 62 and a copy of as many bytes would take 123. On the way there (241 us at first):
-// stores of 64 bytes of a row instead of 16, marked as streamed; no branch around them; the transform's
-// rows through LDS; one workgroup a CU for the whole call.
+// stores of whole lines of a row instead of 16 bytes, marked as streamed (in halves of lines 180 us, with 753 MB
+// written instead of 537); no branch around them; the transform's rows through LDS; one workgroup a CU for the
+// whole call.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,7 +27,7 @@ using namespace chunk;
 // ------------------------------------------------------------------ 2 bits
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kStream = 2;  // stores of rows that are not read again here: 230 -> 198 us for 16 sequences' 8192 tokens
+constexpr int kStream = 2;  // (nt) of stores that are not read again here: 230 -> 198 us when it came
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -217,33 +218,46 @@ __device__ __forceinline__ void read_side(const ReadArgs &a, uint2 *s_book, floa
         }
       }
     }
-    // Runs of two tokens 16 apart change places, so that a store has 64 bytes of a row from four lanes.
-    int to[2];
-    for (int x = 0; x < 2; ++x) {
-      const int i = tile + 16 * x + (n & 15);
-      to[x] = there(i) ? static_cast<int>((i - first) * row_bytes) + (kv * D + 64 * half + 2 * kRun * (n >> 4) + kRun * j) * kBytes : kOutside;
-    }
-    for (int h = 0; h < 32 / kRun; h += 2) {
-      uint32_t w[2][4];
-      for (int x = 0; x < 2; ++x)
+    // Runs of two tokens 16 apart change places, then those of two that are 8 apart, so that a store has 128
+    // bytes of a row (whole lines) from eight lanes.
+    int to[2][2];  // tokens 16 x + 8 z + n % 8
+    for (int x = 0; x < 2; ++x)
+      for (int z = 0; z < 2; ++z) {
+        const int i = tile + 16 * x + 8 * z + (n & 7);
+        const int at = kv * D + 64 * half + 4 * kRun * ((n >> 3) & 1) + 2 * kRun * (n >> 4) + kRun * j;
+        to[x][z] = there(i) ? static_cast<int>((i - first) * row_bytes) + at * kBytes : kOutside;
+      }
+    for (int h = 0; h < 32 / kRun; h += 4) {
+      uint32_t w[4][4];
+      for (int x = 0; x < 4; ++x)
         for (int u = 0; u < 4; ++u) {
           const float *from = y + kRun * (h + x) + (BF16 ? 2 * u : u);
           if constexpr (BF16) w[x][u] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(from[0]), static_cast<__bf16>(from[1])});
           else w[x][u] = __float_as_uint(from[0]);
         }
       for (int u = 0; u < 4; ++u) {
-        const auto s = __builtin_amdgcn_permlane16_swap(w[0][u], w[1][u], false, false);
-        w[0][u] = s[0], w[1][u] = s[1];
+        for (int x = 0; x < 4; x += 2) {
+          const auto s = __builtin_amdgcn_permlane16_swap(w[x][u], w[x + 1][u], false, false);
+          w[x][u] = s[0], w[x + 1][u] = s[1];
+        }
+        for (int x = 0; x < 2; ++x) {  // lanes 8 .. 15 of a row for 0 .. 7 of the other (DPP row_ror:8)
+          const int low = w[x][u], high = w[x + 2][u];
+          w[x][u] = __builtin_amdgcn_update_dpp(low, high, 0x128, 0xf, 0xc, false);
+          w[x + 2][u] = __builtin_amdgcn_update_dpp(high, low, 0x128, 0xf, 0x3, false);
+        }
       }
       for (int x = 0; x < 2; ++x)
-        __builtin_amdgcn_raw_buffer_store_b128(uint4_t{w[x][0], w[x][1], w[x][2], w[x][3]}, rows, to[x], 2 * kRun * kBytes * h, kStream);
+        for (int z = 0; z < 2; ++z) {
+          const uint32_t(&v)[4] = w[x + 2 * z];
+          __builtin_amdgcn_raw_buffer_store_b128(uint4_t{v[0], v[1], v[2], v[3]}, rows, to[x][z], 2 * kRun * kBytes * h, kStream);
+        }
     }
   }
 }
 
 // SQ: values are the scalar arm's levels.
 template <int D, int PARTS, bool SQ, bool BAND, bool BF16>
-__global__ __launch_bounds__(kThreads, D == 64 && PARTS == 1 ? 4 : 2) void read_kernel(const ReadArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void read_kernel(const ReadArgs a) {
   __shared__ __align__(16) uint2 s_book[D / kGroupDim * kCodebookSize];
   __shared__ __align__(16) float s_rows[D * (D + 4)];
   // (chunk, side, KV head fastest): the heads of a token, whose output rows follow each other, run together
@@ -332,8 +346,8 @@ hipError_t launch_read(const ReadArgs &args, hipStream_t stream) {
   const long long units = static_cast<long long>(a.batch) * a.num_kv_heads * sides;
   const int step = 32 * kWaves / (a.head_dim / 64);
   // Chunks: their number c that takes the least time, a workgroup's set-up being worth about 128 tokens; a CU holds
-  // one workgroup at head_dim 128, two at 64.
-  const long long seats = a.head_dim == 128 ? 256 : 512, rounds = (a.n + step - 1) / step;
+  // one workgroup (two at head_dim 64 spilled: 15.5 us for parts of six sequences in the deployed format, 13.2 so).
+  const long long seats = 256, rounds = (a.n + step - 1) / step;
   long long best = 0;
   for (int k = 0; k < 8; ++k) {
     const long long c = std::max(1LL, k < 4 ? k + 1 : (k - 3) * seats / units);
