@@ -8,7 +8,7 @@
 // arm's levels enter as level - 1.5, exact, and meet the transform's row sums with the
 // token's offset + 1.5 scale.
 //
-// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 170 us, of
+// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 158 us, of
 // which the matrix cores work 62 and a copy of as many bytes would take 123. On the way there (241 us at first):
 // stores of whole lines of a row instead of 16 bytes, marked as streamed (in halves of lines 180 us, with 753 MB
 // written instead of 537); no branch around them; the transform's rows through LDS; one workgroup a CU for the

@@ -58,3 +58,36 @@ def test_a_long_tail_of_small_weights(nk, n, dtype):  # noqa: F811
     assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) - tol).max()
     # the bound tells a lost tail: without it the outputs are the one value
     assert (np.abs(c.rows(0, 0)[1][7] - ref) > 4 * tol).any()
+
+
+@pytest.mark.parametrize("n", (30, 70))
+def test_replays_with_other_lengths(nk, n):  # noqa: F811
+    """A captured call in splits is replayed with lengths that shrink and grow on the device, eager calls between
+    the replays in the same workspace: the same outputs every time."""
+    c = Cache(nk, 14, [6000, 4000], 1, 128, 16)
+    q = torch.as_tensor(2.0 * c.rng.standard_normal((2, n, 8, 128))).to(BF).cuda()
+    need = nk.chunk_attn_workspace_bytes(c.params, 2, n, 8, c.top)
+    assert need
+    ws, out = torch.zeros(need, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    q_lens = torch.tensor([n, n], dtype=torch.int32, device="cuda")
+    args = (c.params, c.layout, q, c.k_codes, c.v_codes, c.seq_lens, c.top, out, ws)
+    eager = nk.prepare_chunk_attn(*args, q_lens=q_lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nk.prepare_chunk_attn(*args, q_lens=q_lens)()
+    for lens, seqs in (([n, n], [6000, 4000]), ([1, n], [33, 2]), ([0, 5], [6000, 0]), ([n, n - 1], [n, 3999]), ([n, n], [6000, 4000])):
+        q_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        c.seq_lens.copy_(torch.tensor(seqs, dtype=torch.int32))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone()
+        for _ in range(3):
+            out.fill_(7.0)
+            eager()
+            torch.cuda.synchronize()
+            assert torch.equal(replayed, out)
+        for b in range(2):
+            assert (out[b, lens[b]:] == 7).all() and out[b, :lens[b]].isfinite().all()
+    ref, tol = c.attend(q.double().cpu().numpy(), [n, n])
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
