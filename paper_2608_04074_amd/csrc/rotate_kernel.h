@@ -62,14 +62,17 @@ __device__ __forceinline__ void to_floats(const uint2 w, float *x) {
   x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
 }
 __device__ __forceinline__ void to_floats(const float4 w, float *x) { x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w; }
+// Streamed (nt): the rows are not read again here. 32 x 4096 tokens on three axes 569 -> 543 us, appended 916 -> 894 us.
 template <bool BF16>
 __device__ __forceinline__ void store4(char *p, const float *x) {
   if constexpr (BF16) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<bf16x4 *>(p) =
-        bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])};
+    __builtin_nontemporal_store(
+        bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])},
+        reinterpret_cast<bf16x4 *>(p));
   } else {
-    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    typedef float floatx4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<floatx4 *>(p));
   }
 }
 
