@@ -67,6 +67,7 @@ nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout 
     if (static_cast<long long>(max_seq_len) > static_cast<long long>(layout->block_size) * layout->blocks_per_seq)
       return fail(NOVA_KV_ERR_INVALID_ARG, "max_seq_len exceeds the per-sequence capacity");
     if (window < 0) return fail(NOVA_KV_ERR_INVALID_ARG, "window must be >= 0");
+    window = window_within(window, max_seq_len);
     if (!(softmax_scale >= 0.f) || softmax_scale > 1e30f)
       return fail(NOVA_KV_ERR_INVALID_ARG, "softmax_scale must be in [0, 1e30]");
     if (batch == 0 || n_q == 0) return ok();

@@ -495,7 +495,7 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
   p.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   p.row_tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
   const long long tiles = static_cast<long long>(p.row_tiles) * batch * num_kv_heads;
-  const long long span = window > 0 ? std::min<long long>(max_seq_len, window + n_q) : max_seq_len;
+  const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
   const long long limit = p.tile_rows >= 128 ? q4::kMaxSplitsTiled : q4::kMaxSplits;
   auto most = [&](const long long s) { return std::max(1LL, std::min<long long>({limit, (s + 127) / 128, q4::kMaxCounters / tiles})); };
   // splits until the CUs have a workgroup each

@@ -62,6 +62,11 @@ nova_kv_status check_metadata(const nova_kv_layout *lay, int32_t num_blocks, int
                               const int32_t *seq_lens, int32_t max_seq_len, const int32_t *start_pos,
                               int32_t n_new, const int32_t *new_lens = nullptr, bool may_be_absent = false);
 
+// The window of a call of several query tokens, for its plan and its kernels: 0 (none) for one of max_seq_len
+// positions or more, which hides nothing. Query tokens lie down to 2^24 in front of position 0, and a position
+// less a window near 2^31 would leave 32 bits.
+inline int32_t window_within(int32_t window, int32_t max_seq_len) { return window < max_seq_len ? window : 0; }
+
 // Dense rows [batch][n][heads][head_dim] that a cache is read to: either may be NULL.
 nova_kv_status check_read_outputs(nova_kv_dtype dtype, int32_t batch, int32_t n, int32_t heads, int32_t head_dim,
                                   const void *k_out, const void *v_out);
