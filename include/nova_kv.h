@@ -752,14 +752,18 @@ nova_kv_status nova_kv_check_metadata(const nova_kv_layout *layout, int32_t num_
  * nova_kv_q4_attn and nova_kv_q4_read wait for their stream, copy seq_lens /
  * start_pos / new_lens / the block table to the host and run
  * nova_kv_check_metadata (with num_blocks as given here, <= 0: unknown)
- * before launching; a failing check launches nothing.  (The reading calls check
- * the positions that they read: sequences may share blocks there.)  This synchronizes,
- * so it is for debugging and not for graph capture.
+ * before launching; a failing check launches nothing.  (nova_kv_chunk_attn and the
+ * reading calls check the blocks of the positions that they attend or read, and no
+ * others: sequences may share blocks there, and those in front of a window, of a
+ * band's positions only or of sequences without queries may hold anything.)
+ * This synchronizes, so it is for debugging and not for graph capture.
  *
- * The 4-bit cache's calls check against its own num_blocks.  A negative block-table entry (a block not held yet, or released in
- * front of a window) passes.  What else these calls would leave out or cut is
+ * The 4-bit cache's calls check against its own num_blocks.  A negative block-table
+ * entry (a block not held yet, or released in front of a window) passes there.  What
+ * else these calls, nova_kv_chunk_attn and nova_kv_read would leave out or cut is
  * reported, as a likely mistake: entries from num_blocks on, new tokens outside
- * the capacity (beyond new_lens), lengths outside [0, max_seq_len].
+ * the capacity (beyond new_lens), tokens to read outside the sequence, lengths
+ * outside [0, max_seq_len].
  */
 void nova_kv_set_debug(int32_t on, int32_t num_blocks);
 

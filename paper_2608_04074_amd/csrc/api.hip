@@ -57,31 +57,57 @@ nova_kv_status debug_check(const nova_kv_layout *lay, int32_t batch, const int32
   return NOVA_KV_OK;
 }
 
-nova_kv_status debug_check_reads(const nova_kv_layout *lay, int32_t batch, const int32_t *start_pos, int32_t n,
-                                 const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
-                                 hipStream_t stream, int32_t num_blocks) {
-  if (!debug_enabled() || batch <= 0) return NOVA_KV_OK;
-  hipError_t e = hipStreamSynchronize(stream);
-  auto to_host = [&](const int32_t *d, size_t count, std::vector<int32_t> &h) -> const int32_t * {
+namespace {
+
+// Host copies of a call's metadata, in front of which its stream is waited for.
+struct HostCopies {
+  hipError_t e;
+  explicit HostCopies(hipStream_t stream) : e(hipStreamSynchronize(stream)) {}
+  const int32_t *get(const int32_t *d, size_t count, std::vector<int32_t> &h) {
     if (!d) return nullptr;
     h.resize(count);
     if (e == hipSuccess) e = hipMemcpy(h.data(), d, count * sizeof(int32_t), hipMemcpyDeviceToHost);
     return h.data();
-  };
-  std::vector<int32_t> starts, counts, sizes, table;
-  to_host(start_pos, batch, starts);
-  const int32_t *const c = to_host(lens, batch, counts), *const z = to_host(seq_lens, batch, sizes);
-  nova_kv_layout hl = *lay;
-  hl.block_table = to_host(lay->block_table, static_cast<size_t>(batch) * lay->blocks_per_seq, table);
-  if (e != hipSuccess) return fail(NOVA_KV_ERR_HIP, "debug mode: metadata copy: %s", hipGetErrorString(e));
-  const nova_kv_status st = check_reads(&hl, num_blocks > 0 ? num_blocks : debug_num_blocks(), batch, starts.data(), n, c, z,
-                                        band, num_blocks > 0);
-  if (st != NOVA_KV_OK) {
-    std::string d = "debug mode: ";
-    d += nova_kv_last_error();
-    return fail(st, "%s", d.c_str());
   }
-  return NOVA_KV_OK;
+};
+
+nova_kv_status copies_failed(hipError_t e) { return fail(NOVA_KV_ERR_HIP, "debug mode: metadata copy: %s", hipGetErrorString(e)); }
+
+// A check's status, its text marked.
+nova_kv_status in_debug_mode(nova_kv_status st) {
+  if (st == NOVA_KV_OK) return st;
+  std::string d = "debug mode: ";
+  d += nova_kv_last_error();
+  return fail(st, "%s", d.c_str());
+}
+
+}  // namespace
+
+nova_kv_status debug_check_reads(const nova_kv_layout *lay, int32_t batch, const int32_t *start_pos, int32_t n,
+                                 const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
+                                 hipStream_t stream, int32_t num_blocks) {
+  if (!debug_enabled() || batch <= 0) return NOVA_KV_OK;
+  HostCopies host(stream);
+  std::vector<int32_t> starts, counts, sizes, table;
+  const int32_t *const at = host.get(start_pos, batch, starts);
+  const int32_t *const c = host.get(lens, batch, counts), *const z = host.get(seq_lens, batch, sizes);
+  nova_kv_layout hl = *lay;
+  hl.block_table = host.get(lay->block_table, static_cast<size_t>(batch) * lay->blocks_per_seq, table);
+  if (host.e != hipSuccess) return copies_failed(host.e);
+  return in_debug_mode(check_reads(&hl, num_blocks > 0 ? num_blocks : debug_num_blocks(), batch, at, n, c, z, band, num_blocks > 0));
+}
+
+nova_kv_status debug_check_attended(const nova_kv_layout *lay, int32_t batch, int32_t n_q, const int32_t *q_lens,
+                                    const int32_t *seq_lens, int32_t max_seq_len, int32_t window,
+                                    const nova_kv_band *band, hipStream_t stream) {
+  if (!debug_enabled() || batch <= 0) return NOVA_KV_OK;
+  HostCopies host(stream);
+  std::vector<int32_t> counts, sizes, table;
+  const int32_t *const c = host.get(q_lens, batch, counts), *const z = host.get(seq_lens, batch, sizes);
+  nova_kv_layout hl = *lay;
+  hl.block_table = host.get(lay->block_table, static_cast<size_t>(batch) * lay->blocks_per_seq, table);
+  if (host.e != hipSuccess) return copies_failed(host.e);
+  return in_debug_mode(check_attended(&hl, debug_num_blocks(), batch, n_q, c, z, max_seq_len, window, band));
 }
 
 }  // namespace novakv

@@ -90,7 +90,8 @@ nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout 
       if (!aligned(workspace, 256)) return fail(NOVA_KV_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     }
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if ((st = novakv::debug_check(layout, batch, seq_lens, max_seq_len, nullptr, 0, stream)) != NOVA_KV_OK) return st;
+    if ((st = novakv::debug_check_attended(layout, batch, n_q, q_lens, seq_lens, max_seq_len, window, band, stream)) != NOVA_KV_OK)
+      return st;
     novakv::ChunkArgs a{};
     a.batch = batch;
     a.n_q = n_q;

@@ -21,4 +21,9 @@ nova_kv_status debug_check_reads(const nova_kv_layout *lay, int32_t batch, const
                                  const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
                                  hipStream_t stream, int32_t num_blocks = 0);
 
+// The same for several query tokens over the 2-bit cache (check_attended).
+nova_kv_status debug_check_attended(const nova_kv_layout *lay, int32_t batch, int32_t n_q, const int32_t *q_lens,
+                                    const int32_t *seq_lens, int32_t max_seq_len, int32_t window,
+                                    const nova_kv_band *band, hipStream_t stream);
+
 }  // namespace novakv

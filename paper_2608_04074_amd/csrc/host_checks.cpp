@@ -360,6 +360,32 @@ nova_kv_status check_reads(const nova_kv_layout *lay, int32_t num_blocks, int32_
   return NOVA_KV_OK;
 }
 
+nova_kv_status check_attended(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch, int32_t n_q,
+                              const int32_t *q_lens, const int32_t *seq_lens, int32_t max_seq_len, int32_t window,
+                              const nova_kv_band *band) {
+  for (int b = 0; b < batch; ++b) {
+    const long long size = seq_lens[b];
+    if (size < 0 || size > max_seq_len)
+      return fail(NOVA_KV_ERR_INVALID_ARG, "seq_lens[%d] = %d outside [0, max_seq_len = %d]", b, seq_lens[b], max_seq_len);
+    const long long queries = !q_lens ? n_q : q_lens[b] < 0 ? 0 : q_lens[b] < n_q ? q_lens[b] : n_q;
+    if (queries == 0) continue;
+    long long from = window > 0 && size - queries + 1 > window ? size - queries + 1 - window : 0, to = size;
+    if (band) {
+      if (from < band->n_sink) from = band->n_sink;
+      if (to > size - band->n_rec) to = size - band->n_rec;
+    }
+    // Kernels that look up aligned runs of 16 positions do so in blocks of a multiple of 16 rows: the same blocks.
+    for (long long blk = from / lay->block_size; from < to && blk <= (to - 1) / lay->block_size; ++blk) {
+      const long long logical = static_cast<long long>(b) * lay->blocks_per_seq + blk;
+      const long long p = lay->block_table ? lay->block_table[logical] : logical;
+      if (p < 0 || (num_blocks > 0 && p >= num_blocks))
+        return fail(NOVA_KV_ERR_INVALID_ARG, "sequence %d: block %lld maps to physical block %lld outside [0, %d)", b, blk,
+                    p, num_blocks > 0 ? num_blocks : 0x7fffffff);
+    }
+  }
+  return NOVA_KV_OK;
+}
+
 namespace {
 
 int32_t env_debug() {

@@ -77,6 +77,12 @@ nova_kv_status check_reads(const nova_kv_layout *lay, int32_t num_blocks, int32_
                            int32_t n, const int32_t *lens, const int32_t *seq_lens, const nova_kv_band *band,
                            bool may_be_absent);
 
+// The blocks that n_q query tokens (the first q_lens[b] of a sequence, NULL: n_q) attend, on host copies: of the
+// positions that a query's window holds and that are not the band's. Lengths must lie in [0, max_seq_len].
+nova_kv_status check_attended(const nova_kv_layout *lay, int32_t num_blocks, int32_t batch, int32_t n_q,
+                              const int32_t *q_lens, const int32_t *seq_lens, int32_t max_seq_len, int32_t window,
+                              const nova_kv_band *band);
+
 // Debug mode (nova_kv_set_debug; initially on when the environment variable
 // NOVA_KV_DEBUG is a nonzero number): entry points copy their metadata to
 // the host and check it before launching.
