@@ -286,8 +286,13 @@ __global__ __launch_bounds__(kThreads, 2) void read_kernel(const ReadArgs a) {
 constexpr int kHeads = 4;  // heads of a workgroup, whose rows are requested at once
 
 // D / 8 lanes hold a row, 8 coordinates each; a wave's rows are tokens that follow each
-// other, so their codes do too. Bound by HBM: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 127 us, 5.3 TB/s (132 without streamed stores).
-template <int D, bool BF16>
+// other, so their codes do too. Bound by HBM: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 127 us, 5.3 TB/s (132
+// without streamed stores).
+// STREAMED: large bf16 outputs. A lane's 16 bytes of bf16 are parts of whole lines; the two 16 bytes of its fp32
+// coordinates lie apart, and streamed they leave as parts of lines (16 sequences' 8192 tokens of 8 heads of 64: 246 us,
+// 167 through the caches). What fits the caches is left there for the next call: 4 sequences' 4096 tokens with a copy of
+// them 32 us, 41 streamed; 8 x 4096 67 and 76, 8 x 8192 (256 MiB) 174 and 171.
+template <int D, bool BF16, bool STREAMED>
 __global__ __launch_bounds__(256) void q4_read_kernel(const ReadArgs a) {
   constexpr int kLanes = D / 8, kTokens = 256 / kLanes;
   const int lane = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
@@ -328,11 +333,13 @@ __global__ __launch_bounds__(256) void q4_read_kernel(const ReadArgs a) {
       if constexpr (BF16) {
         bf16x8 v;
         for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[e]);
-        __builtin_nontemporal_store(v, reinterpret_cast<bf16x8 *>(static_cast<__bf16 *>(out) + to));
+        bf16x8 *p = reinterpret_cast<bf16x8 *>(static_cast<__bf16 *>(out) + to);
+        if constexpr (STREAMED) __builtin_nontemporal_store(v, p);
+        else *p = v;
       } else {
         float4_t *p = reinterpret_cast<float4_t *>(static_cast<float *>(out) + to);
-        __builtin_nontemporal_store(float4_t{x[0], x[1], x[2], x[3]}, p);
-        __builtin_nontemporal_store(float4_t{x[4], x[5], x[6], x[7]}, p + 1);
+        p[0] = float4_t{x[0], x[1], x[2], x[3]};
+        p[1] = float4_t{x[4], x[5], x[6], x[7]};
       }
     }
   }
@@ -380,11 +387,18 @@ hipError_t launch_read(const ReadArgs &args, hipStream_t stream) {
 hipError_t launch_q4_read(const ReadArgs &a, hipStream_t stream) {
   const int tokens = 256 / (a.head_dim / 8);
   const dim3 grid(static_cast<unsigned>(a.batch) * ((a.n + tokens - 1) / tokens), (a.num_kv_heads + kHeads - 1) / kHeads);
-  auto go = [&](auto d, auto bf16) {
-    q4_read_kernel<d(), bf16()><<<grid, 256, 0, stream>>>(a);
+  const long long sides = (a.k_out ? 1 : 0) + (a.v_out ? 1 : 0);
+  const bool streamed = sides * a.batch * a.n * a.num_kv_heads * a.head_dim * 2 >= 256LL << 20;  // bytes of bf16
+  auto go = [&](auto d, auto bf16, auto nt) {
+    q4_read_kernel<d(), bf16(), nt()><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
   };
-  auto by_type = [&](auto d) { return a.bf16 ? go(d, std::true_type{}) : go(d, std::false_type{}); };
+  using std::false_type;
+  using std::true_type;
+  auto by_type = [&](auto d) {
+    if (!a.bf16) return go(d, false_type{}, false_type{});
+    return streamed ? go(d, true_type{}, true_type{}) : go(d, true_type{}, false_type{});
+  };
   return a.head_dim == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
 }
 
