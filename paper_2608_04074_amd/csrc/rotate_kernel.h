@@ -62,20 +62,22 @@ __device__ __forceinline__ void to_floats(const uint2 w, float *x) {
   x[2] = __uint_as_float(w.y << 16), x[3] = __uint_as_float(w.y & 0xffff0000u);
 }
 __device__ __forceinline__ void to_floats(const float4 w, float *x) { x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w; }
-// Streamed (nt): the rows are not read again here. 32 x 4096 tokens on three axes 569 -> 543 us, appended 916 -> 894 us.
-template <bool BF16>
+// STREAMED: past the caches (launch_rows says when).
+template <bool STREAMED, typename T>
+__device__ __forceinline__ void store_at(char *p, const T v) {
+  if constexpr (STREAMED) __builtin_nontemporal_store(v, reinterpret_cast<T *>(p));
+  else *reinterpret_cast<T *>(p) = v;
+}
+template <bool BF16, bool STREAMED>
 __device__ __forceinline__ void store4(char *p, const float *x) {
   if constexpr (BF16) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(
-        bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])},
-        reinterpret_cast<bf16x4 *>(p));
+    store_at<STREAMED>(p, bf16x4{static_cast<__bf16>(x[0]), static_cast<__bf16>(x[1]), static_cast<__bf16>(x[2]), static_cast<__bf16>(x[3])});
   } else {
     typedef float floatx4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<floatx4 *>(p));
+    store_at<STREAMED>(p, floatx4{x[0], x[1], x[2], x[3]});
   }
 }
-
 // Norm and rotation of a lane's 8 coordinates, in T; the mean square with eps (1 without a norm).
 template <int D, bool IL, typename T>
 __device__ __forceinline__ T norm_rotate(T *y, const float *w, const bool norm, const float eps, const float *cs,
@@ -218,8 +220,8 @@ __device__ __forceinline__ void quantize(const float *x, const float *w, const b
 // lane requested at once. FAST: quantize in fp32 where that decides the codes.
 // AXES: each rotated pair is turned by its own axis' position. The token's angles then
 // are gathered once by the workgroup, an element a thread, whatever order the pairs
-// follow the axes in, and handed to the lanes through LDS.
-template <int D, bool BF16, bool IL, bool Q4, bool VEC, int AHEAD, bool FAST, bool AXES>
+// follow the axes in, and handed to the lanes through LDS. STREAMED: rows go past the caches.
+template <int D, bool BF16, bool IL, bool Q4, bool VEC, int AHEAD, bool FAST, bool STREAMED, bool AXES>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   constexpr int kLanes = D / 8, kSlots = kThreads / kLanes, kElem = BF16 ? 2 : 4;
   const int tok = blockIdx.x;
@@ -314,8 +316,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     const int to0 = (hh * D + c0) * kElem, to1 = (hh * D + c1) * kElem;
     if (!Q4 || side == 0) {
       norm_rotate<D, IL, float>(x, w, weight != nullptr, a.eps, cs, sn, turns && side < 2);
-      store4<BF16>(out + to0, x);
-      store4<BF16>(out + to1, x + 4);
+      store4<BF16, STREAMED>(out + to0, x);
+      store4<BF16, STREAMED>(out + to1, x + 4);
       continue;
     }
     float code[8];
@@ -345,8 +347,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     if (out) {
       const float scale = bf16_bits_to_float(sq & 0xffffu), offset = bf16_bits_to_float(sq >> 16);
       for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(scale, code[j], offset);
-      store4<BF16>(out + to0, x);
-      store4<BF16>(out + to1, x + 4);
+      store4<BF16, STREAMED>(out + to0, x);
+      store4<BF16, STREAMED>(out + to1, x + 4);
     }
   }
 }
@@ -370,18 +372,31 @@ hipError_t launch_rows(const RotateArgs &a, hipStream_t stream) {
   // tokens 11.9 us against 12.8 us), and quantizes in fp32 with a second look in fp64
   // (716 us against 1568 us; of 64 tokens some wave always takes both ways: 5.5 us
   // against 4.9 us in fp64 alone).
+  // Outputs that the caches cannot hold for the next call go past them, in whole lines: 32 x 4096 tokens on three
+  // axes 543 us, 569 through the caches, appended 894 and 916. From 1 GiB on (the last cache holds 256 MiB): of 4 x 8192
+  // tokens (403 MB) alone 139 and 144 us, with a copy of the rows behind it 308 and 299; 64 tokens appended and
+  // attended 18.6 us streamed, 17.6 not. In parts of lines streamed stores cost more: 16 x 8192 tokens in fp32,
+  // neighbouring pairs, 1609 and 1182 us.
+  const long long rows_out = (a.q_out ? a.nq : 0) + (a.k_out ? a.nk : 0) + (a.v_out ? a.nv : 0);
+  const bool streamed = rows_out * a.head_dim * elem * tokens >= 1LL << 30 &&
+                        rotate::whole_lines(a.head_dim, a.rotary_dim, a.interleaved, a.bf16);
   auto go = [&](auto d, auto bf16, auto il, auto q4, auto vec) {
-    const auto launch = [&](auto ahead, auto fast) {
+    const auto launch = [&](auto ahead, auto fast, auto nt) {
       const dim3 grid(tokens, (heads + slots * ahead() - 1) / (slots * ahead()));
-      rotate_kernel<d(), bf16(), il(), q4(), vec(), ahead(), fast(), AXES><<<grid, kThreads, 0, stream>>>(a);
+      rotate_kernel<d(), bf16(), il(), q4(), vec(), ahead(), fast(), nt(), AXES><<<grid, kThreads, 0, stream>>>(a);
       return hipGetLastError();
     };
     constexpr std::integral_constant<int, 1> one{};
     constexpr std::integral_constant<int, 3> three{};
-    if (tokens >= 8192) return launch(three, std::bool_constant<q4()>{});
+    constexpr std::bool_constant<q4()> quick{};
+    if (tokens >= 8192) {
+      if constexpr (rotate::whole_lines(d(), d(), il(), bf16()))
+        if (streamed) return launch(three, quick, std::true_type{});
+      return launch(three, quick, std::false_type{});
+    }
     if constexpr (q4())
-      if (tokens >= 512) return launch(one, std::true_type{});
-    return launch(one, std::false_type{});
+      if (tokens >= 512) return launch(one, std::true_type{}, std::false_type{});
+    return launch(one, std::false_type{}, std::false_type{});
   };
   using std::false_type;
   using std::true_type;

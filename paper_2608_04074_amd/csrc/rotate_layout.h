@@ -17,6 +17,13 @@ constexpr LaneChunks lane_chunks(const int lane, const int rotary_dim, const boo
   return {turns, c0, halves ? c0 + rotary_dim / 2 : c0 + 4};
 }
 
+// Whether the lanes' stores of a row write whole lines of 64 bytes: those of one chunk each (16 bytes of fp32, 8 of
+// bf16) where the lower ends of pairs of halves follow each other all through the head, and the upper ones; those of
+// both chunks of neighbouring pairs where one store takes them (16 bytes of bf16).
+constexpr bool whole_lines(const int head_dim, const int rotary_dim, const bool interleaved, const bool bf16) {
+  return interleaved ? bf16 : rotary_dim == head_dim;
+}
+
 // Codes take half a byte each, so a chunk two bytes.
 enum class CodeStore {
   kBoth,      // four bytes: the chunks follow each other
