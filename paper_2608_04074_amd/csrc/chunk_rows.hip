@@ -497,16 +497,18 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
   const long long tiles = static_cast<long long>(p.row_tiles) * batch * num_kv_heads;
   const long long span = window > 0 ? std::min<long long>(max_seq_len, static_cast<long long>(window) + n_q) : max_seq_len;
   const long long limit = p.tile_rows >= 128 ? q4::kMaxSplitsTiled : q4::kMaxSplits;
-  auto most = [&](const long long s) { return std::max(1LL, std::min<long long>({limit, (s + 127) / 128, q4::kMaxCounters / tiles})); };
-  // splits until the CUs have a workgroup each
-  p.n_split = static_cast<int>(std::max(1LL, std::min({most(span), (span + 511) / 512, 256 / tiles})));
-  // One workgroup merges a tile's splits, for about as long a split as 32 (of 256 rows: 45) of its tokens take.
-  if (p.tile_rows >= 128) {
+  auto splits = [&](const long long s) {
+    // until the CUs have a workgroup each (so no more counters are used than there are)
+    long long n = std::min({limit, (s + 511) / 512, 256 / tiles});
+    // One workgroup merges a tile's splits, for about as long a split as 32 (of 256 rows: 45) of its tokens take.
     const double per = p.tile_rows == 128 ? 32. : 45.;
-    p.n_split = std::max(1, std::min(p.n_split, static_cast<int>(std::sqrt(static_cast<double>(span) / per))));
-  }
+    if (p.tile_rows >= 128) n = std::min(n, static_cast<long long>(std::sqrt(static_cast<double>(s) / per)));
+    return static_cast<int>(std::max(1LL, n));
+  };
+  static_assert(q4::kMaxCounters >= 256, "a split tile has a counter");
+  p.n_split = splits(span);
   p.off_part = q4::kMaxCounters * sizeof(int);
-  const long long all = most(max_seq_len);
+  const int all = splits(max_seq_len);  // longer spans have no fewer: the most of any window
   if (all > 1) {
     const size_t part = static_cast<size_t>(tiles) * all * p.tile_rows * (head_dim + 2) * sizeof(float);
     p.total = p.off_part + ((part + 255) & ~static_cast<size_t>(255));
