@@ -40,9 +40,7 @@ size_t nova_kv_chunk_attn_workspace_bytes(const nova_kv_params *p, int32_t batch
       (p->head_dim != 64 && p->head_dim != 128) || num_q_heads % p->num_kv_heads != 0 ||
       too_many_rows(batch, n_q, num_q_heads, p->num_kv_heads))
     return 0;
-  const size_t narrow = novakv::plan_chunk(batch, n_q, num_q_heads, p->num_kv_heads, p->head_dim, 1, max_seq_len, 0).total;
-  const size_t wide = novakv::plan_chunk(batch, n_q, num_q_heads, p->num_kv_heads, p->head_dim, 0, max_seq_len, 0).total;
-  return narrow > wide ? narrow : wide;
+  return novakv::plan_chunk(batch, n_q, num_q_heads, p->num_kv_heads, p->head_dim, max_seq_len, 0).total;
 }
 
 nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout *layout, const void *q,
@@ -81,8 +79,7 @@ nova_kv_status nova_kv_chunk_attn(const nova_kv_params *p, const nova_kv_layout 
       return fail(NOVA_KV_ERR_INVALID_ARG, "code pools must be 16-byte aligned");
     if (too_many_rows(batch, n_q, num_q_heads, p->num_kv_heads))
       return fail(NOVA_KV_ERR_UNSUPPORTED, "too many query rows in a call");
-    const novakv::ChunkPlan plan = novakv::plan_chunk(batch, n_q, num_q_heads, p->num_kv_heads, p->head_dim,
-                                                      q_dtype == NOVA_KV_BF16, max_seq_len, window);
+    const novakv::ChunkPlan plan = novakv::plan_chunk(batch, n_q, num_q_heads, p->num_kv_heads, p->head_dim, max_seq_len, window);
     if (plan.n_split > 1) {
       if (!workspace || workspace_bytes < plan.total)
         return fail(NOVA_KV_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", plan.total,

@@ -108,8 +108,7 @@ template <int D>
 __device__ __forceinline__ int code_coord(const int o, const int m) {
   return D == 128 ? 16 * (m & 7) + 8 * (m >> 3) + o : 16 * (m & 3) + 4 * (m >> 2) + o;
 }
-// The value group whose codewords a lane n mod 16 makes tiles 4 p .. 4 p + 3 of, and its code byte in
-// the word of codes that it shares with others, from byte value_word on.
+// The value group whose codewords a lane n mod 16 makes tiles 4 p .. 4 p + 3 of.
 template <int D>
 __device__ __forceinline__ int value_group(const int n, const int p) {
   return D == 128 ? 4 * (n & 7) + 2 * (n >> 3) + p : 4 * (n & 3) + (n >> 2);

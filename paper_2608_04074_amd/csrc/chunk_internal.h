@@ -61,10 +61,9 @@ struct ChunkArgs : Q4AttnArgs {
 // of tile_rows, each tile's span in n_split splits.
 struct ChunkPlan {
   int tile_rows, row_tiles, n_split;
-  double cost;  // estimated time, ns
   size_t off_part, total;  // workspace: arrival counters, then the split partials (needed when n_split > 1)
 };
-ChunkPlan plan_chunk(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int q_bf16, int max_seq_len, int window);
+ChunkPlan plan_chunk(int batch, int n_q, int num_q_heads, int num_kv_heads, int head_dim, int max_seq_len, int window);
 hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // tiles of 128 rows; launch_chunk calls it
 hipError_t launch_chunk_wide(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);  // of 256
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream);

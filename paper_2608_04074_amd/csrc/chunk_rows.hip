@@ -31,16 +31,17 @@ namespace {
 using namespace chunk;
 
 constexpr int kRound = 32;  // tokens a wave takes at a time
+constexpr int W = 8;        // waves
 
-template <int D, bool WIDE, int NT, bool SQ, int W>
+template <int D, bool WIDE, int NT, bool SQ, bool ALIGNED>
 struct Lds {
   static constexpr int kRows = 16 * NT, kParts = WIDE ? 2 : 1, kStride = D + 4, kQStride = D + 8;
   static constexpr int kBook = D / kGroupDim * kCodebookSize * 8;
   // while codes are attended
   static constexpr int kQ = (SQ ? 1 : 2) * kBook;                       // q' [part][row][D + 8] fp16
   static constexpr int kTok = kQ + kParts * kRows * kQStride * 2;       // [wave][rho, scale, offset, exponent][32] fp32
-  static constexpr int kRowAt = kTok + W * 4 * kRound * 4;              // [wave][32] rows of tokens, 64 bits
-  static constexpr int kLoopEnd = kRowAt + W * kRound * 8;
+  static constexpr int kRowAt = kTok + W * 4 * kRound * 4;              // [wave][32] rows of tokens, 64 bits (ALIGNED: none)
+  static constexpr int kLoopEnd = kRowAt + (ALIGNED ? 0 : W * kRound * 8);
   // while waves are merged
   static constexpr int kPart = 0;                                       // [wave][row][D + 4] fp32
   static constexpr int kMerged = W * kRows * kStride * 4;               // [row][D + 4]
@@ -53,11 +54,11 @@ struct Lds {
   static_assert(kBytes <= 160 * 1024, "LDS of a workgroup");
 };
 
-// D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows. SQ: the scalar value arm. W: waves.
+// D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows. SQ: the scalar value arm.
 // ALIGNED: blocks of a multiple of 16 rows.
-template <int D, bool WIDE, int NT, bool SQ, int W, bool ALIGNED>
+template <int D, bool WIDE, int NT, bool SQ, bool ALIGNED>
 __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a) {
-  using M = Lds<D, WIDE, NT, SQ, W>;
+  using M = Lds<D, WIDE, NT, SQ, ALIGNED>;
   constexpr int kThreads = 64 * W, kRows = M::kRows, kParts = M::kParts;
   constexpr int L = D / kGroupDim, kSteps = D / 32, kTiles = D / 16, kWords = D / 64;
   __shared__ __align__(16) uint8_t s_lds[M::kBytes];
@@ -463,11 +464,10 @@ __global__ __launch_bounds__(64 * W, 1) void chunk_rows_kernel(const ChunkArgs a
   q4::merge_splits<D, NT, W, false>(a, g, {s_part, nullptr, nullptr, s_inv, s_last}, n);
 }
 
-template <int W>
 hipError_t launch_few(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
   const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
   auto go = [&](auto d, auto wide, auto nt, auto sq, auto aligned) {
-    chunk_rows_kernel<d(), wide(), nt(), sq(), W, aligned()><<<groups, 64 * W, 0, stream>>>(a);
+    chunk_rows_kernel<d(), wide(), nt(), sq(), aligned()><<<groups, 64 * W, 0, stream>>>(a);
     return hipGetLastError();
   };
   using std::false_type;
@@ -488,7 +488,7 @@ hipError_t launch_few(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t str
 
 // Rows per workgroup: up to 16 (32) rows take one (two) matrix tiles, the workgroup's waves dividing the
 // tokens; more rows take 16 or 32 a wave, 128 or 256 a workgroup (both sides measured: chunk_tile.hip).
-ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads, const int head_dim, const int q_bf16,
+ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, const int num_kv_heads, const int head_dim,
                      const int max_seq_len, const int window) {
   ChunkPlan p{};
   const long long rows = static_cast<long long>(n_q) * (num_q_heads / num_kv_heads);
@@ -519,7 +519,7 @@ ChunkPlan plan_chunk(const int batch, const int n_q, const int num_q_heads, cons
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
   return plan.tile_rows == 256   ? launch_chunk_wide(a, plan, stream)
          : plan.tile_rows == 128 ? launch_chunk_tile(a, plan, stream)
-                                 : launch_few<8>(a, plan, stream);
+                                 : launch_few(a, plan, stream);
 }
 
 }  // namespace novakv

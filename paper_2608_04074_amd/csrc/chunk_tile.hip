@@ -24,8 +24,9 @@ namespace {
 using namespace chunk;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int NT = 1;  // tiles of 16 rows a wave
 
-template <int D, int NT, bool SQ>
+template <int D, bool SQ>
 struct Lds {
   static constexpr int kTiles = D / 16, kSteps = D / 32;
   static constexpr int kHalves = D == 128 && !SQ ? 1 : 2;  // 32 tokens each of a round
@@ -96,11 +97,11 @@ __device__ __forceinline__ void transform_rows(const half8_t *t, const int lane,
   }
 }
 
-// D: head_dim. WIDE: fp32 queries. NT: tiles of 16 rows a wave. SQ: the scalar value arm. KS: key scales.
+// D: head_dim. WIDE: fp32 queries. SQ: the scalar value arm. KS: key scales.
 // ALIGNED: blocks of a multiple of 16 rows.
-template <int D, bool WIDE, int NT, bool SQ, bool KS, bool ALIGNED>
+template <int D, bool WIDE, bool SQ, bool KS, bool ALIGNED>
 __global__ __launch_bounds__(kThreads, 2) void chunk_tile_kernel(const ChunkArgs a) {
-  using M = Lds<D, NT, SQ>;
+  using M = Lds<D, SQ>;
   constexpr int kParts = WIDE ? 2 : 1, L = D / kGroupDim, kSteps = M::kSteps, kTiles = M::kTiles;
   constexpr int kHalves = M::kHalves, kTokens = M::kTokens, kRuns = M::kRuns;
   constexpr int kKeyUnits = M::kKeyFrags / kWaves, kValueUnits = kRuns * 2 * (kTiles / 4) / kWaves;
@@ -427,22 +428,18 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_tile_kernel(const ChunkArgs
 
 hipError_t launch_chunk_tile(const ChunkArgs &a, const ChunkPlan &plan, hipStream_t stream) {
   const unsigned groups = static_cast<unsigned>(a.batch) * a.num_kv_heads * plan.row_tiles * plan.n_split;
-  using std::bool_constant;
   using std::false_type;
   using std::integral_constant;
   using std::true_type;
-  auto go = [&](auto d, auto wide, auto nt, auto sq, auto ks, auto aligned) {
-    chunk_tile_kernel<d(), wide(), nt(), sq(), ks(), aligned()><<<groups, kThreads, 0, stream>>>(a);
+  auto go = [&](auto d, auto wide, auto sq, auto ks, auto aligned) {
+    chunk_tile_kernel<d(), wide(), sq(), ks(), aligned()><<<groups, kThreads, 0, stream>>>(a);
     return hipGetLastError();
   };
-  auto by_blocks = [&](auto d, auto wide, auto nt, auto sq, auto ks) {
-    return a.layout.block_size % 16 == 0 ? go(d, wide, nt, sq, ks, true_type{}) : go(d, wide, nt, sq, ks, false_type{});
+  auto by_blocks = [&](auto d, auto wide, auto sq, auto ks) {
+    return a.layout.block_size % 16 == 0 ? go(d, wide, sq, ks, true_type{}) : go(d, wide, sq, ks, false_type{});
   };
-  auto by_keys = [&](auto d, auto wide, auto nt, auto sq) {
-    return a.k_scales ? by_blocks(d, wide, nt, sq, true_type{}) : by_blocks(d, wide, nt, sq, false_type{});
-  };
-  const integral_constant<int, 1> one;  // tile of 16 rows a wave
-  auto by_values = [&](auto d, auto wide) { return a.v_sq ? by_keys(d, wide, one, true_type{}) : by_keys(d, wide, one, false_type{}); };
+  auto by_keys = [&](auto d, auto wide, auto sq) { return a.k_scales ? by_blocks(d, wide, sq, true_type{}) : by_blocks(d, wide, sq, false_type{}); };
+  auto by_values = [&](auto d, auto wide) { return a.v_sq ? by_keys(d, wide, true_type{}) : by_keys(d, wide, false_type{}); };
   auto by_type = [&](auto d) { return a.q_bf16 ? by_values(d, false_type{}) : by_values(d, true_type{}); };
   return a.head_dim == 128 ? by_type(integral_constant<int, 128>{}) : by_type(integral_constant<int, 64>{});
 }
