@@ -7,14 +7,19 @@
 // has 16 (32) rows, turns their queries into the key transform's coordinates once, and its
 // waves divide the tokens, 32 a round: a lane gathers a token's key codewords from the
 // codebook in LDS, which are a matrix operand as they come, and eight tokens' codewords of a
-// value group, which it transposes in registers. Queries and probabilities enter as one fp16
-// part, those of fp32 calls as two (22 bits). The sums go back through R_V once, merged over
+// value group, which it transposes in registers. The sums go back through R_V once, merged over
 // the waves.
 //
-// Bound by the gathers, 64 reads of eight bytes a token and head at random banks, with one workgroup a CU
-// beside 128 KiB of codebooks: 64 sequences of up to 16K tokens, four drafted tokens of 4 heads each, take 174 us
-// (2.3 TB/s of the cache). A short call is the workgroup's setup: 20 us over 2000 tokens, whether in splits of
-// 512, 256 or 128 tokens.
+// Queries and probabilities (times the scalar arm's scales) enter as one fp16 part in bf16 calls: half a step of them is
+// 2^-12, an eighth of the half step that their outputs are rounded by, and a second part would double the matrix
+// instructions. Those of fp32 calls enter as two parts (22 bits): 64 sequences of up to 16K tokens, four drafted
+// tokens of 4 heads each, take 452 us in fp32. Weights are summed in fp32 before they are rounded.
+//
+// The same in bf16 takes 173 us (2.3 TB/s of the cache). No unit is at its limit: LDS is busy in 39% of the cycles (the
+// gathers, 64 reads of eight bytes a token and head, two thirds of it bank conflicts), the vector units in 43, the
+// matrix cores in 11; one workgroup a CU beside 128 KiB of codebooks leaves two waves a SIMD, and a round's gathers,
+// products, weights and gathers follow each other. A short call is the workgroup's setup: 20 us over 2000 tokens,
+// whether in splits of 512, 256 or 128 tokens.
 //
 // Positions that a band holds are attended first, with their exact bf16 rows on the bf16
 // cores; their share joins behind R_V.

@@ -9,7 +9,9 @@
 // round's keys are.
 //
 // Tiles of 256 rows (chunk_wide.hip) for such calls leave half of their waves idle: 32 queries of 4 heads over 16384
-// tokens 104 us here, 240 there; over 8192 tokens of 16 sequences 233 and 220.
+// tokens 101 us here, 240 there; over 8192 tokens of 16 sequences 220 in both. Far from the matrix cores' 7 and 58 us:
+// 25 us are a workgroup's setup (over 64 tokens), whose transforms come in element by element, and a round of
+// 32 tokens has two barriers. Parts of queries and probabilities: as in chunk_rows.hip.
 //
 // Queries go through R_K^-T and sums back through R_V on the matrix cores, without leaving the
 // wave: the transform's rows are dealt to the tiles so that a lane's results are its next operand.

@@ -12,8 +12,9 @@
 //
 // Bound by issue: of a round's cycles the matrix cores, the vector units (four instructions a score, an
 // exponential counting twice, and the gathers) and LDS are busy 39, 47 and 41 percent, and overlap in part. Two
-// sequences' 2048 queries of 4 heads over 8192 tokens take 560 us (871 TFLOP/s); one buffer and two barriers 650,
-// the two waves of a SIMD in opposite phases 777, each wave gathering for itself 902.
+// sequences' 2048 queries of 4 heads over 8192 tokens take 551 us (889 TFLOP/s); one buffer and two barriers 650,
+// the two waves of a SIMD in opposite phases 777, each wave gathering for itself 902. Parts of queries and
+// probabilities: as in chunk_rows.hip; two of each (fp32) take 1023 us.
 //
 // Queries go through R_K^-T and sums back through R_V on the matrix cores, without leaving the
 // wave: the transform's rows are dealt to the tiles so that a lane's results are its next operand.

@@ -8,8 +8,8 @@
 // arm's levels enter as level - 1.5, exact, and meet the transform's row sums with the
 // token's offset + 1.5 scale.
 //
-// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 158 us, of
-// which the matrix cores work 62 and a copy of as many bytes would take 123. On the way there (241 us at first):
+// Bound by its stores and by the products: 16 sequences' 8192 tokens of 8 heads of 128 in bf16 take 159 us; the matrix
+// cores work 45% of the cycles, the vector units 43, and a copy of as many bytes would take 123 us. On the way there (241 us at first):
 // stores of whole lines of a row instead of 16 bytes, marked as streamed (in halves of lines 180 us, with 753 MB
 // written instead of 537); no branch around them; the transform's rows through LDS; one workgroup a CU for the
 // whole call.
@@ -27,7 +27,10 @@ using namespace chunk;
 // ------------------------------------------------------------------ 2 bits
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kStream = 2;  // (nt) of stores that are not read again here: 230 -> 198 us when it came
+// (nt) of stores that are not read again here: 230 -> 198 us when it came; now 183 and 211 alone, with a copy of the rows
+// behind the call 381 and 399. Of 17 MB with a copy 25 and 27 us; between, where the caches would have held the rows
+// for the copy, 54 and 50 (67 MB).
+constexpr int kStream = 2;
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

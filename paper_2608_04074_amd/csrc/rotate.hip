@@ -9,7 +9,7 @@
 // [8i, 8i + 8).  Both ways its angles are 4i .. 4i + 3.
 //
 // Memory bounds it: 32 x 4096 tokens of 32 query and 8 + 8 KV heads of 128 in bf16 are
-// rotated in 566 us, 3.22 GB read and written at 5.7 TB/s; to a cache (3.37 GB) 716 us, where
+// rotated in 556 us, 3.22 GB read and written at 5.8 TB/s; to a cache (3.37 GB) 702 us, where
 // the vector instructions of the codes take about 580 us beside it. One token: 3.8 to 4.7 us,
 // 64 sequences' to a cache 5.0 us, launch and latency.
 #include "rotate_kernel.h"

@@ -373,7 +373,7 @@ hipError_t launch_rows(const RotateArgs &a, hipStream_t stream) {
   // (716 us against 1568 us; of 64 tokens some wave always takes both ways: 5.5 us
   // against 4.9 us in fp64 alone).
   // Outputs that the caches cannot hold for the next call go past them, in whole lines: 32 x 4096 tokens on three
-  // axes 543 us, 569 through the caches, appended 894 and 916. From 1 GiB on (the last cache holds 256 MiB): of 4 x 8192
+  // axes 537 us, 569 through the caches, appended 897 and 916. From 1 GiB on (the last cache holds 256 MiB): of 4 x 8192
   // tokens (403 MB) alone 139 and 144 us, with a copy of the rows behind it 308 and 299; 64 tokens appended and
   // attended 18.6 us streamed, 17.6 not. In parts of lines streamed stores cost more: 16 x 8192 tokens in fp32,
   // neighbouring pairs, 1609 and 1182 us.
